@@ -342,6 +342,8 @@ KVEV_API int kvev_plan_debug_stall_unit(kvev_plan *plan, int unit);
  *   - The call allocates nothing: no cudaMalloc/cudaFree and no allocating
  *     library routine.  Inputs and outputs are the caller's, as for
  *     kvev_evict_prefill().
+ *   - num_pages * page_size and max_pages * page_size stay below 2^31, and a call
+ *     takes at most KVEV_PAGED_MAX_REQUESTS requests (ENOTSUP).
  *   - device_status: required device int32 (4-byte aligned; NULL is
  *     EINVAL) that the call zeroes on `stream` and in which the kernels
  *     record their status bits (1 = a bounded wait ran out, 2 = an in-kernel
@@ -438,6 +440,152 @@ KVEV_API int kvev_decode_step(kvev_plan *plan, int B, int growth, void *dec_K, v
 KVEV_API int kvev_decode_step_attn(kvev_plan *plan, int B, int growth, void *dec_K, void *dec_V,
                                    void *dec_state, const void *const *k_new,
                                    const void *const *v_new, const float *const *attn, void *stream);
+
+/* ---- paged caches --------------------------------------------------------------- */
+
+/* What stands before the eviction in a serving program: K/V held in pages while
+ * prompts are prefilled in chunks (and, for FULL layers, for good), the
+ * attention over them, and the way from pages to the contiguous caches that
+ * kvev_evict_prefill() reads.  No counterpart in the paper, which takes the
+ * model's own prefill attention as given.
+ *
+ * A request s of B holds its tokens' K/V rows in pages of page_size tokens: the
+ * token at position t is row t % page_size of page block_table[s][t / page_size]
+ * (int32 [B][max_pages] on the device, the same for every layer).
+ *   - page_size is a power of two from 8 to 256.
+ *   - The slot of a token is page * page_size + row: its row in the pool.
+ *   - All calls are asynchronous on `stream`, read lengths and tables on the
+ *     device and allocate nothing, so a captured graph can be replayed with
+ *     other lengths.  They need no plan.
+ *   - num_pages * page_size and max_pages * page_size stay below 2^31, and a call
+ *     takes at most KVEV_PAGED_MAX_REQUESTS requests (ENOTSUP).
+ *   - device_status: required device int32 in which the kernels record status
+ *     bits (1 = a bounded wait ran out, 2 = a length, slot or page out of range,
+ *     which the kernels skip); the calls only add bits, the caller clears it. */
+
+#define KVEV_BF16 0
+#define KVEV_FP16 1
+
+/* One layer's pages.  Row (page p, token row r, KV head h) starts at element
+ * p * page_stride + r * token_stride + h * head_stride of K and of V and holds d
+ * contiguous elements: [page][H_kv][d] and [H_kv][page][d] pages, pages of
+ * several layers in one tensor and K next to V are all strides.  K and V are
+ * 16-byte aligned device memory and the strides multiples of 8, positive. */
+typedef struct kvev_paged_cache {
+  void *K, *V;
+  int64_t page_stride, token_stride, head_stride; /* in elements */
+  int32_t num_pages, page_size, H_kv, d;
+  int32_t dtype; /* KVEV_BF16 or KVEV_FP16 */
+} kvev_paged_cache;
+
+/* Most requests of one call. */
+#define KVEV_PAGED_MAX_REQUESTS 8192
+
+/* Block tables, slots and positions of a step's new tokens.
+ *   lens, new_lens   device int32 [B]: tokens in the cache, and new tokens.
+ *   free_pages       device int32 [num_pages]: a stack of free pages,
+ *   free_count       device int32: of which this many are on it.
+ *   block_table      device int32 [B][max_pages], read and completed: request s
+ *                    holds ceil(lens[s] / page_size) pages and gets the ones its
+ *                    new tokens need, from the top of the stack, in request
+ *                    order: entry by entry, the k-th page given out is
+ *                    free_pages[*free_count - 1 - k].
+ *   granted          device int32 [B]: 0 for a request whose pages, with those
+ *                    of the requests before it, are more than the stack holds,
+ *                    or that would need more than max_pages; it gets none.  A
+ *                    request that needs no new page is always granted.
+ *   kv_lens          device int32 [B]: lens + new_lens, lens where not granted.
+ *                    May be lens itself.
+ *   cu_new           device int32 [B + 1]: first token of each request among the
+ *                    new tokens, laid out request after request; cu_new[B] is
+ *                    their number (refused requests' tokens included).
+ *   slots, positions device int32 [T]: the slot and the position of each new
+ *                    token; -1 for a refused request's tokens and for the rows
+ *                    from cu_new[B] to T.
+ *   free_count_out   device int32: what is left on the stack.  May be free_count.
+ * A negative length counts as 0, more new tokens than T are cut off, both with
+ * status bit 2.  Asynchronous.  EINVAL: a NULL pointer, B or T < 0, page_size or
+ * sizes out of range. */
+KVEV_API int kvev_paged_tables(const int32_t *lens, const int32_t *new_lens, int B, int page_size,
+                               int num_pages, const int32_t *free_pages, const int32_t *free_count,
+                               int32_t *block_table, int max_pages, int T, int32_t *kv_lens,
+                               int32_t *cu_new, int32_t *slots, int32_t *positions, int32_t *granted,
+                               int32_t *free_count_out, int32_t *device_status, void *stream);
+
+/* The pages of finished requests (done[s] != 0, device int32 [B]) go back on the
+ * stack, request after request and entry after entry, and their lengths become 0:
+ * lens_out[s] = done[s] ? 0 : lens[s] (may be lens itself), *free_count_out = the
+ * stack's new height (may be free_count).  block_table is only read.  Entries
+ * that would not fit on a stack of num_pages are dropped with status bit 2.
+ * Errors as kvev_paged_tables. */
+KVEV_API int kvev_paged_release(const int32_t *lens, const int32_t *done, int B, int page_size,
+                                int num_pages, const int32_t *block_table, int max_pages,
+                                int32_t *free_pages, const int32_t *free_count, int32_t *lens_out,
+                                int32_t *free_count_out, int32_t *device_status, void *stream);
+
+/* The new tokens' rows into their slots: row slots[t] of the pool takes k[t] and
+ * v[t], for t < T; tokens with a negative slot are left out.
+ *   k, v   device [T][H_kv][d] of the cache's type, with token_stride and
+ *          head_stride elements (multiples of 8) from token to token and head to
+ *          head, 16-byte aligned: slices of a fused projection need no copy.
+ * Two tokens with one slot leave either's row.  A slot past the pool is skipped
+ * with status bit 2.  EINVAL: NULL or misaligned pointers, strides or sizes out
+ * of range. */
+KVEV_API int kvev_paged_write(const kvev_paged_cache *cache, const void *k, const void *v,
+                              int64_t token_stride, int64_t head_stride, const int32_t *slots, int T,
+                              int32_t *device_status, void *stream);
+
+/* The first lens[s] tokens of every request as contiguous caches, the layout
+ * kvev_evict_prefill() reads: out_K, out_V device [B][H_kv][S_cap][d] (16-byte
+ * aligned); rows from lens[s] on are not written.  A length outside
+ * 0..min(S_cap, max_pages * page_size) is cut to it, and the rows of a page
+ * outside the pool are left out, both with status bit 2.  EINVAL as above. */
+KVEV_API int kvev_paged_gather(const kvev_paged_cache *cache, const int32_t *block_table, int max_pages,
+                               const int32_t *lens, int B, int S_cap, void *out_K, void *out_V,
+                               int32_t *device_status, void *stream);
+
+/* Scratch of kvev_paged_attention(), whatever the lengths: *bytes (256-byte
+ * aligned device memory).  Its first KVEV_PAGED_SYNC_BYTES must be zero before
+ * the first call and are left zero by every call that ends without a status
+ * bit; the rest needs no initialisation.  Calls whose GPU work overlaps need a
+ * workspace each.  EINVAL: H_q not a multiple of H_kv, or bytes NULL; ENOTSUP
+ * as below. */
+#define KVEV_PAGED_SYNC_BYTES 4096
+KVEV_API int kvev_paged_attention_workspace(int H_q, int H_kv, int d, size_t *bytes);
+
+/* Causal attention of the step's new tokens over the pages, their own rows
+ * included (write them first): a prompt's chunk, single tokens, or both in one
+ * call.  Request s has q = cu_new[s + 1] - cu_new[s] rows, the last q of its
+ * kv_lens[s] positions; row i is at t = kv_lens[s] - q + i and
+ *   lse = ln sum_k exp(scale q_row . K[k]),  out = sum_k exp(scale q_row . K[k] - lse) V[k]
+ * over the keys k <= t, with window > 0 only the last `window` of them.
+ *   q, out   device [T][H_q][d] of the cache's type, element strides from token to
+ *            token and head to head (multiples of 8; d contiguous), 16-byte
+ *            aligned.  Query head j reads KV head j / (H_q / H_kv).
+ *   T        rows of q and out; cu_new[B] <= T.  Rows past cu_new[B] are not
+ *            written.
+ *   lse      device fp32 [T][H_q] or NULL: natural log, scale included, what
+ *            kvev_evict_prefill_lse() takes for the window rows.
+ *   scale    0 = 1 / sqrt(d).
+ *   window   0 = every key.
+ * A row without keys (kv_lens[s] < q leaves rows at t < 0) gets out = 0 and lse =
+ * -inf.  The pool's rows past kv_lens[s], and those before the window of every row
+ * of the request, may hold anything; a NaN or infinite K or V row that some row
+ * of a request sees may also reach the request's rows that do not.  Softmax
+ * weights are rounded to the cache's type before the product with V; sums and
+ * statistics are fp32.  The result does not depend on timing.
+ * A request whose lengths are out of range (negative, more than max_pages * page_size,
+ * cu_new decreasing or past T) is left out, and pages outside the pool count as
+ * zero rows, both with status bit 2.  Asynchronous.
+ * EINVAL: NULL or misaligned pointers, strides or sizes out of range, scale
+ * negative or not finite; ENOTSUP: d not 64 or 128, or more than 128 query heads
+ * to a KV head; ENOMEM: workspace too small. */
+KVEV_API int kvev_paged_attention(const kvev_paged_cache *cache, const void *q, int64_t q_token_stride,
+                                  int64_t q_head_stride, const int32_t *cu_new, const int32_t *kv_lens,
+                                  const int32_t *block_table, int max_pages, int B, int T, int H_q,
+                                  float scale, int window, void *out, int64_t out_token_stride,
+                                  int64_t out_head_stride, float *lse, void *workspace,
+                                  size_t workspace_bytes, int32_t *device_status, void *stream);
 
 /* ---- measurement ---------------------------------------------------------- */
 

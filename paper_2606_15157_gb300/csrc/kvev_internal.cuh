@@ -5,6 +5,7 @@
 
 #include <cuda.h>
 #include <cuda_runtime.h>
+#include <cudaTypedefs.h>
 #include <stdint.h>
 
 #include "../../include/kvev.h"
@@ -591,6 +592,8 @@ cudaError_t launch_overlapped(void (*fn)(const P), const P& p, int grid, int thr
   return cudaLaunchKernelEx(&cfg, fn, p);
 }
 
+// The driver's tensor map encoder, null without a driver (api.cu).
+PFN_cuTensorMapEncodeTiled_v12000 encode_fn();
 cudaError_t launch_prologue(const PrologueParams& p, cudaStream_t s);
 cudaError_t launch_score(const ScoreParams& p, int d, int grid, size_t smem, cudaStream_t s);
 int score_smem_bytes(int d, int q_rows, int q_bufs, int R_pad, int stages);

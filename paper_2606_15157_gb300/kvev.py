@@ -21,6 +21,8 @@ OK, EINVAL, ENOMEM, ECUDA, ETIMEOUT, EDEVICE, ENOTSUP = range(7)
 FULL, SNAPKV, H2O, STREAMING, TOVA = 0, 1, 2, 3, 4
 POOL_MAX, POOL_AVG = 0, 1
 T_IDENTITY, T_CAP_Q95 = 0, 1
+BF16, FP16 = 0, 1
+PAGED_SYNC_BYTES, PAGED_MAX_REQUESTS = 4096, 8192
 SCOPE_PREFILL, SCOPE_DECODE, SCOPE_BOTH = 1, 2, 3
 
 STATUS_NAMES = {OK: "OK", EINVAL: "EINVAL", ENOMEM: "ENOMEM", ECUDA: "ECUDA",
@@ -35,7 +37,8 @@ EXPORTS = ["kvev_alloc_from_scores", "kvev_alloc_rescale", "kvev_plan_create",
            "kvev_decode_step", "kvev_decode_step_attn", "kvev_evict_prefill_scored", "kvev_evict_prefill_lse",
            "kvev_profile_cosine", "kvev_score_ppl", "kvev_score_entropy",
            "kvev_route_toprank", "kvev_route_install", "kvev_plan_save", "kvev_plan_load",
-           "kvev_plan_set_h2o_full_prompt"]
+           "kvev_plan_set_h2o_full_prompt", "kvev_paged_tables", "kvev_paged_release", "kvev_paged_write",
+           "kvev_paged_gather", "kvev_paged_attention_workspace", "kvev_paged_attention"]
 KERNEL_NAMES = ["prologue", "score", "select", "gather"]
 
 
@@ -97,6 +100,14 @@ def load(path: str = LIB_PATH):
         L.kvev_plan_save.argtypes = [vp, vp, P(sz)]
         L.kvev_plan_load.argtypes = [P(vp), vp, sz]
         L.kvev_plan_set_h2o_full_prompt.argtypes = [vp, C.c_int]
+        L.kvev_paged_tables.argtypes = [vp, vp, C.c_int, C.c_int, C.c_int, vp, vp, vp, C.c_int, C.c_int,
+                                        vp, vp, vp, vp, vp, vp, vp, vp]
+        L.kvev_paged_release.argtypes = [vp, vp, C.c_int, C.c_int, C.c_int, vp, C.c_int, vp, vp, vp, vp, vp, vp]
+        L.kvev_paged_write.argtypes = [vp, vp, vp, i64, i64, vp, C.c_int, vp, vp]
+        L.kvev_paged_gather.argtypes = [vp, vp, C.c_int, vp, C.c_int, C.c_int, vp, vp, vp, vp]
+        L.kvev_paged_attention_workspace.argtypes = [C.c_int, C.c_int, C.c_int, P(sz)]
+        L.kvev_paged_attention.argtypes = [vp, vp, i64, i64, vp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_int,
+                                           C.c_float, C.c_int, vp, i64, i64, vp, vp, sz, vp, vp]
         for name in EXPORTS:
             if name != "kvev_plan_destroy":
                 getattr(L, name).restype = C.c_int
@@ -386,6 +397,49 @@ def kvev_plan_load(data: bytes) -> int:
     buf = C.create_string_buffer(bytes(data), len(data))
     _check(load().kvev_plan_load(C.byref(h), buf, len(data)), "kvev_plan_load")
     return h.value
+
+
+class PagedCacheDesc(C.Structure):
+    """``kvev_paged_cache``: one layer's pages (strides in elements)."""
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("page_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("num_pages", C.c_int32), ("page_size", C.c_int32), ("H_kv", C.c_int32),
+                ("d", C.c_int32), ("dtype", C.c_int32)]
+
+
+def kvev_paged_tables(lens, new_lens, B, page_size, num_pages, free_pages, free_count, block_table, max_pages, T,
+                      kv_lens, cu_new, slots, positions, granted, free_count_out, device_status, stream) -> int:
+    """Pointer-level call; returns the status code (does not raise)."""
+    return load().kvev_paged_tables(lens, new_lens, B, page_size, num_pages, free_pages, free_count, block_table,
+                                    max_pages, T, kv_lens, cu_new, slots, positions, granted, free_count_out,
+                                    device_status, stream)
+
+
+def kvev_paged_release(lens, done, B, page_size, num_pages, block_table, max_pages, free_pages, free_count, lens_out,
+                       free_count_out, device_status, stream) -> int:
+    return load().kvev_paged_release(lens, done, B, page_size, num_pages, block_table, max_pages, free_pages,
+                                     free_count, lens_out, free_count_out, device_status, stream)
+
+
+def kvev_paged_write(cache, k, v, token_stride, head_stride, slots, T, device_status, stream) -> int:
+    return load().kvev_paged_write(cache, k, v, token_stride, head_stride, slots, T, device_status, stream)
+
+
+def kvev_paged_gather(cache, block_table, max_pages, lens, B, S_cap, out_K, out_V, device_status, stream) -> int:
+    return load().kvev_paged_gather(cache, block_table, max_pages, lens, B, S_cap, out_K, out_V, device_status, stream)
+
+
+def kvev_paged_attention_workspace(H_q: int, H_kv: int, d: int) -> int:
+    n = C.c_size_t()
+    _check(load().kvev_paged_attention_workspace(H_q, H_kv, d, C.byref(n)), "kvev_paged_attention_workspace")
+    return n.value
+
+
+def kvev_paged_attention(cache, q, q_token_stride, q_head_stride, cu_new, kv_lens, block_table, max_pages, B, T, H_q,
+                         scale, window, out, out_token_stride, out_head_stride, lse, workspace, workspace_bytes,
+                         device_status, stream) -> int:
+    return load().kvev_paged_attention(cache, q, q_token_stride, q_head_stride, cu_new, kv_lens, block_table, max_pages,
+                                       B, T, H_q, scale, window, out, out_token_stride, out_head_stride, lse, workspace,
+                                       workspace_bytes, device_status, stream)
 
 
 # ---------------------------------------------------------------------------
