@@ -1,93 +1,955 @@
 // paged_attn.cu -- causal attention of new tokens over paged caches.
+//
+// A row r (one query head of one new token, at position t) needs
+//   m = max_k x_k,  l = sum_k exp2(x_k - m),  o = sum_k exp2(x_k - m) V[k] / l,
+// x_k = log2(e) scale q.K[k] over its keys k, and lse = ln 2 (m + log2 l).  All
+// of it comes from one pass over the keys in tiles of 128, with the row's m and
+// l kept in registers and o in tensor memory.
+//
+// Work.  The G query heads of a KV head and neighbouring tokens share K and V, so
+// their rows fill the 128 lanes of a tensor-core tile: P = 128 / G tokens x G
+// heads.  A unit is up to two such tiles (2 P tokens of a request and KV head)
+// against its key tiles; a CTA runs two "sides", each a tile of rows with its own
+// scores, output accumulator and softmax warpgroup, so that one side's softmax
+// runs while the tensor core works for the other:
+//   - full unit (more than P tokens): side x holds the x-th tile of rows, and
+//     both take every key tile;
+//   - paired unit (a single tile of rows: single tokens, short chunks): both
+//     sides hold the same rows and take the key tiles in turn, and are merged.
+// All units' key tiles are laid end to end and cut into equal shares, one per CTA
+// (cost of a tile: 2 in a full unit, 1 in a paired one, kUnitCost for a unit's
+// start and end), so that any mix of lengths keeps every SM busy to the end and a
+// long context is split where there are few rows.  The pieces of a unit that
+// was cut leave (m, l, o) records in the workspace; the piece that arrives last
+// merges them in order, so the result does not depend on who that is.
+//
+// Roles (384 threads): warp 0 loads Q tiles and pages by TMA (a lane per page
+// box), warp 1 issues the MMAs, warp 2 deals the entries (pieces of units) to the
+// others through a ring, warps 4-7 and 8-11 are the sides' softmax warpgroups, a
+// thread per row.  S = Q K^T is read from tensor memory into registers, and the
+// weights go back into the same columns as the A operand of O += P V.
 #include <climits>
 #include <cmath>
+#include <mutex>
 
 #include "paged.cuh"
 
 namespace kvev {
 namespace {
 
+constexpr int kAttnThreads = 384;
+constexpr int kRegsAttnControl = 72, kRegsAttnSoftmax = 216;
+constexpr int kRegsAttnNeeded = 128 * kRegsAttnControl + 256 * kRegsAttnSoftmax;
+constexpr int kMaxCtas = 152;
+constexpr int kEntries = 4;         // ring of dealt entries
+constexpr int kUnitCost = 1;        // cost of a unit's start and end, in paired tiles
+constexpr int kMinShare = 2;        // least cost of a share: no piece of a cut unit is empty
+constexpr int kRows = 128;          // rows of a side
+constexpr float kRaise = 8.f;       // a row's maximum is raised when a tile's is this much (log2) above it
+constexpr uint64_t kAttnWaitNs = 2000000000ull;
+
 struct PagedAttnParams {
-  PagedView c;
-  const uint4* q;
-  uint4* out;
+  CUtensorMap qmap;   // {d, H_q, T}, box {64, G, P}
+  CUtensorMap qmap1;  // the same, box {64, G, 1}
+  CUtensorMap kmap;   // {d, page rows, H_kv, pages}, box {64, min(page, 128), 1, 1}
+  CUtensorMap vmap;
+  uint8_t* out;
   float* lse;
-  long long q_token, q_head, out_token, out_head;  // strides in vectors
+  long long out_token, out_head;  // strides in bytes
   const int *cu, *kv_lens, *table;
-  int B, T, H_q, G, max_pages, window;
+  int B, T, H_q, H_kv, G, P, page_shift, num_pages, max_pages, window;
   float scale_log2;
   int* status;
+  int* sync;       // [2 kMaxCtas] pieces arrived of the unit whose first piece is the CTA's, per side
+  uint8_t* parts;  // [2 kMaxCtas][2] records
 };
 
-__device__ __forceinline__ float2 unpack2(uint32_t u, int fp16) {
-  if (fp16) {
-    float2 f;
-    asm("{.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;}" : "=f"(f.x), "=f"(f.y) : "r"(u));
-    return f;
+// One piece of a unit.
+struct Entry {
+  int tok0, rows, pos0, h;         // first token, rows (0: no more entries), the first token's position, KV head
+  int s, t0, t1, klo;              // request, key tiles [t0, t1), first key any row sees
+  int khi, paired, pieces, first;  // end of the keys, paired unit, pieces of the unit and the first one's CTA
+};
+
+template <int D>
+struct AttnSmem {
+  static constexpr int kTileBytes = kRows * D * 2;
+  static constexpr int kStages = D == 128 ? 5 : 10;
+  uint8_t q[2][kTileBytes];
+  uint8_t kv[kStages][kTileBytes];
+  float2 ml[2][kRows];   // the sides' (m, l) of a paired unit's rows
+  Entry ring[kEntries];
+  uint64_t qfull[2], qempty[2], full[kStages], empty[kStages];
+  uint64_t sfull[2], pfull[2], ofull[2];
+  uint64_t efull[kEntries], eempty[kEntries];
+  uint64_t xfull, xfree;             // paired units: both sides' (m, l) are there; both sides are done with O
+  uint64_t wrote[2], told[2];        // a side's records are written; the count of arrivals is known
+  uint64_t done;
+  long long carry, start;
+  int last[2];
+  int abort_flag;
+  uint32_t tmem_slot;
+  long long scan[kAttnThreads / 32];
+};
+
+// ---- waits, bounded -------------------------------------------------------------
+
+template <class S>
+__device__ __forceinline__ bool attn_wait(S& sm, uint64_t* bar, uint32_t parity, int* status) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = globaltimer_ns();
+  while (!mbar_try_wait_sleep(bar, parity, 20000)) {
+    if (ld_volatile(&sm.abort_flag)) return false;
+    if (globaltimer_ns() - t0 > kAttnWaitNs) {
+      atomicExch(&sm.abort_flag, 1);
+      atomicOr(status, kStatusTimeout);
+      return false;
+    }
   }
-  return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+  return true;
 }
 
-// One warp per (token, query head): lane i holds 2 * D / 64 elements of the row.
-template <int D, int kFp16>
-__global__ void __launch_bounds__(256) attn_kernel(const __grid_constant__ PagedAttnParams p) {
-  const long long w = (static_cast<long long>(blockIdx.x) * 256 + threadIdx.x) >> 5;
-  const int lane = threadIdx.x & 31;
-  const int t = static_cast<int>(w / p.H_q), j = static_cast<int>(w % p.H_q);
-  if (t >= p.T || t >= p.cu[p.B]) return;
-  int lo = 0, n = p.B;
-  while (n > 1) {
-    const int h = n >> 1;
-    if (p.cu[lo + h] <= t) lo += h;
-    n -= h;
+template <class S>
+__device__ __forceinline__ bool attn_wait_warp(S& sm, uint64_t* bar, uint32_t parity, int* status) {
+  return __all_sync(0xffffffffu, attn_wait(sm, bar, parity, status));
+}
+
+__device__ __forceinline__ void attn_drain(uint64_t* bar, uint32_t parity) {
+  const uint64_t t0 = globaltimer_ns();
+  while (!mbar_try_wait_sleep(bar, parity, 20000))
+    if (globaltimer_ns() - t0 > 1000000000ull) return;
+}
+
+// ---- PTX ------------------------------------------------------------------------
+
+__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+      : "memory");
+}
+
+// D(tmem) (+)= A(tmem) * B(smem), from a whole converged warp.
+__device__ __forceinline__ void umma_ts_elect(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                              uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]),
+      "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+      "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+template <bool kFp16>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  uint32_t u;
+  if (kFp16) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(b), "f"(a));
+  else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(b), "f"(a));
+  return u;
+}
+
+// Instruction descriptor: kind::f16, A and B of one 16-bit type, fp32 D; A K-major,
+// B K-major or (kBn) with its N index contiguous.
+template <bool kFp16, bool kBn>
+__host__ __device__ constexpr uint32_t attn_idesc(int M, int N) {
+  return (1u << 4) | (kFp16 ? 0u : (1u << 7) | (1u << 10)) | (kBn ? 1u << 16 : 0u) |
+         (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+// Descriptor of a V tile as the B operand: [D / 64][128 keys][64 elements], 128-byte
+// swizzle, N (the elements) contiguous: 64-element blocks `block` bytes apart, groups
+// of 8 keys 1024 bytes apart.
+__device__ __forceinline__ uint64_t sw128_n_desc(uint32_t saddr, uint32_t block) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(block >> 4) << 16;
+  d |= static_cast<uint64_t>(1024u >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(2) << 61;
+  return d;
+}
+
+// ---- the schedule ------------------------------------------------------------------
+
+// A request's rows and lengths; q = 0 if it has none or they are out of range.
+struct Request {
+  int c0, q, kv;
+};
+__device__ __forceinline__ Request request(const PagedAttnParams& p, int s, bool* bad) {
+  Request r;
+  r.c0 = __ldg(p.cu + s);
+  const int c1 = __ldg(p.cu + s + 1);
+  r.kv = __ldg(p.kv_lens + s);
+  const bool ok = r.c0 >= 0 && c1 >= r.c0 && c1 <= p.T && r.kv >= 0 && r.kv <= (p.max_pages << p.page_shift);
+  r.q = ok ? c1 - r.c0 : 0;
+  if (!ok) *bad = true;
+  return r;
+}
+
+// Unit m of a request: tokens [2 P m, 2 P m + n), keys [lo, hi), key tiles [t0, t0 + tiles).
+struct Unit {
+  int n, lo, hi, t0, tiles, weight;
+};
+__device__ __forceinline__ Unit unit_of(const PagedAttnParams& p, const Request& r, int m) {
+  Unit u;
+  const int i0 = 2 * p.P * m;
+  u.n = min(2 * p.P, r.q - i0);
+  const int pos0 = r.kv - r.q + i0;
+  u.hi = max(0, pos0 + u.n);
+  u.lo = p.window > 0 ? max(0, pos0 - p.window + 1) : 0;
+  u.t0 = u.lo >> 7;
+  u.tiles = max(1, ((u.hi + 127) >> 7) - u.t0);
+  u.weight = u.n > p.P ? 2 : 1;
+  return u;
+}
+__device__ __forceinline__ int units_of(const PagedAttnParams& p, int q) { return (q + 2 * p.P - 1) / (2 * p.P); }
+
+// Cost of a request's units for one KV head.
+__device__ __forceinline__ long long head_cost(const PagedAttnParams& p, const Request& r) {
+  long long c = 0;
+  const int M = units_of(p, r.q);
+  for (int m = 0; m < M; ++m) {
+    const Unit u = unit_of(p, r, m);
+    c += static_cast<long long>(u.weight) * u.tiles + kUnitCost;
   }
-  const int s = lo, c0 = p.cu[s], q_len = p.cu[s + 1] - c0, len = p.kv_lens[s];
-  if (q_len <= 0 || c0 < 0 || c0 + q_len > p.T || len < 0 || len > (p.max_pages << p.c.page_shift)) {
-    if (lane == 0) atomicOr(p.status, kStatusDevice);
+  return c;
+}
+
+// Sum of v over the block's threads before this one (total: over all).
+template <class S>
+__device__ __forceinline__ long long block_prefix(S& sm, long long v, long long* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  long long a = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long x = __shfl_up_sync(0xffffffffu, a, o);
+    if (lane >= o) a += x;
+  }
+  __syncthreads();
+  if (lane == 31) sm.scan[warp] = a;
+  __syncthreads();
+  long long before = 0, all = 0;
+  for (int w = 0; w < kAttnThreads / 32; ++w) {
+    if (w < warp) before += sm.scan[w];
+    all += sm.scan[w];
+  }
+  *total = all;
+  return before + a - v;
+}
+
+// The CTA's share [x0, x1) of the total cost, and the request that holds x0 with the
+// cost before it (all threads; the block's result).
+struct Share {
+  long long x0, x1, before, share;
+  int s;
+};
+template <class S>
+__device__ __forceinline__ Share share_of(const PagedAttnParams& p, S& sm) {
+  const int tid = threadIdx.x;
+  bool bad = false;
+  long long total = 0, mine = 0, first_before = 0;
+  for (int s0 = 0; s0 < p.B; s0 += kAttnThreads) {
+    mine = 0;
+    if (s0 + tid < p.B) mine = head_cost(p, request(p, s0 + tid, &bad)) * p.H_kv;
+    long long all;
+    const long long before = block_prefix(sm, mine, &all);
+    if (s0 == 0) first_before = before;
+    total += all;
+  }
+  if (bad && blockIdx.x == 0) atomicOr(p.status, kStatusDevice);
+  Share r;
+  r.share = max(static_cast<long long>(kMinShare), (total + gridDim.x - 1) / gridDim.x);
+  r.x0 = min(total, r.share * blockIdx.x);
+  r.x1 = min(total, r.x0 + r.share);
+  // the thread whose request holds x0 says so
+  if (p.B <= kAttnThreads) {
+    if (mine > 0 && first_before <= r.x0 && r.x0 < first_before + mine) {
+      sm.start = tid;
+      sm.carry = first_before;
+    }
+  } else {
+    long long sum = 0;
+    for (int s0 = 0; s0 < p.B; s0 += kAttnThreads) {
+      bool b = false;
+      const long long c = s0 + tid < p.B ? head_cost(p, request(p, s0 + tid, &b)) * p.H_kv : 0;
+      long long all;
+      const long long before = sum + block_prefix(sm, c, &all);
+      if (c > 0 && before <= r.x0 && r.x0 < before + c) {
+        sm.start = s0 + tid;
+        sm.carry = before;
+      }
+      sum += all;
+      if (sum > r.x0) break;
+    }
+  }
+  __syncthreads();
+  r.s = static_cast<int>(sm.start);
+  r.before = sm.carry;
+  return r;
+}
+
+// Warp 2: the CTA's entries in order.
+template <class S>
+__device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, const Share& sh) {
+  uint32_t e = 0;
+  const int lane = threadIdx.x & 31;
+  auto put = [&](const Entry& en) {
+    if (!attn_wait_warp(sm, &sm.eempty[e % kEntries], ((e / kEntries) & 1) ^ 1, p.status)) return false;
+    if (lane == 0) {
+      sm.ring[e % kEntries] = en;
+      mbar_arrive(&sm.efull[e % kEntries]);
+    }
+    __syncwarp();
+    ++e;
+    return true;
+  };
+  if (sh.x0 < sh.x1) {
+    bool bad = false;
+    int s = sh.s;
+    Request r = request(p, s, &bad);
+    long long a = sh.before;  // cost before the unit
+    const long long hc = head_cost(p, r);
+    int h = static_cast<int>((sh.x0 - a) / hc), m = 0;
+    a += h * hc;
+    Unit u = unit_of(p, r, m);
+    auto cost = [&] { return static_cast<long long>(u.weight) * u.tiles + kUnitCost; };
+    while (a + cost() <= sh.x0) {
+      a += cost();
+      u = unit_of(p, r, ++m);
+    }
+    while (a < sh.x1) {
+      // boundary x cuts a unit before tile ceil((x - a) / weight)
+      auto cut = [&](long long x) {
+        const long long o = x - a;
+        return o <= 0 ? 0 : static_cast<int>(min(static_cast<long long>(u.tiles), (o + u.weight - 1) / u.weight));
+      };
+      const int c0 = cut(sh.x0), c1 = cut(sh.x1);
+      if (c0 < c1) {
+        Entry en;
+        en.tok0 = r.c0 + 2 * p.P * m;
+        en.rows = u.n * p.G;
+        en.pos0 = r.kv - r.q + 2 * p.P * m;
+        en.h = h;
+        en.s = s;
+        en.t0 = u.t0 + c0;
+        en.t1 = u.t0 + c1;
+        en.klo = u.lo;
+        en.khi = u.hi;
+        en.paired = u.weight == 1;
+        en.first = static_cast<int>(a / sh.share);
+        en.pieces = static_cast<int>((a + static_cast<long long>(u.weight) * (u.tiles - 1)) / sh.share) - en.first + 1;
+        if (!put(en)) return;
+      }
+      a += cost();
+      if (a >= sh.x1) break;
+      if (2 * p.P * ++m >= r.q) {
+        m = 0;
+        if (++h == p.H_kv) {
+          h = 0;
+          do r = request(p, ++s, &bad);
+          while (r.q == 0);
+        }
+      }
+      u = unit_of(p, r, m);
+    }
+  }
+  Entry end = {};
+  put(end);
+}
+
+// The next entry; every warp that takes entries calls it in order.  rows = 0: no more.
+template <class S>
+__device__ __forceinline__ Entry take(const PagedAttnParams& p, S& sm, uint32_t e) {
+  Entry en = {};
+  if (attn_wait_warp(sm, &sm.efull[e % kEntries], (e / kEntries) & 1, p.status)) {
+    en = sm.ring[e % kEntries];
+    __syncwarp();
+    mbar_arrive_elect(&sm.eempty[e % kEntries]);
+  }
+  return en;
+}
+
+// ---- warp 0: loads -------------------------------------------------------------------
+// Order of an entry's tiles in the ring: A K tiles ahead of V (A = 2 for a paired unit,
+// whose sides work on two tiles at once; 1 for a full one).
+template <int D>
+__device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>& sm) {
+  using S = AttnSmem<D>;
+  const int lane = threadIdx.x & 31;
+  const int box_shift = min(p.page_shift, 7);           // rows of a page box
+  const int boxes = kRows >> box_shift;                 // page boxes of a tile
+  const int pi = lane / (D / 64), kc = lane % (D / 64); // the lane's page box and 64-element column
+  uint32_t st = 0, ph = 0, qs = 0, qn = 0, issued = 0;
+  bool ok = true;
+  for (uint32_t e = 0; ok; ++e) {
+    const Entry en = take(p, sm, e);
+    if (en.rows == 0) break;
+    // ---- Q tiles ----
+    const int sides = en.paired ? 1 : 2;
+    for (int x = 0; ok && x < sides; ++x) {
+      if (!attn_wait_warp(sm, &sm.qempty[qs], ((qn >> 1) & 1) ^ 1, p.status)) { ok = false; break; }
+      const bool one = en.rows == p.G;
+      const uint32_t bytes = static_cast<uint32_t>(p.G) * (one ? 1 : p.P) * D * 2;
+      if (lane == 0) {
+        mbar_expect_tx(&sm.qfull[qs], bytes);
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c)
+          tma_load_3d(sm.q[qs] + c * (kRows * 128), one ? &p.qmap1 : &p.qmap, c * 64, en.h * p.G, en.tok0 + x * p.P,
+                      &sm.qfull[qs]);
+      }
+      __syncwarp();
+      ++qn;
+      qs ^= 1;
+    }
+    // ---- pages ----
+    // the page of the lane's box in tile t (its number; num_pages = zeros)
+    const int* row = p.table + static_cast<long long>(en.s) * p.max_pages;
+    auto page_of = [&](int t) {
+      const int k = t * kRows + (pi << box_shift);
+      if (t >= en.t1 || pi >= boxes || k >= en.khi || k + (1 << box_shift) <= en.klo) return p.num_pages;
+      const int id = __ldg(row + (k >> p.page_shift));
+      if (static_cast<unsigned>(id) < static_cast<unsigned>(p.num_pages)) return id;
+      atomicOr(p.status, kStatusDevice);
+      return p.num_pages;
+    };
+    auto load = [&](const CUtensorMap* map, int t, int page) {
+      if (!attn_wait_warp(sm, &sm.empty[st], ph ^ 1, p.status)) { ok = false; return; }
+      if (lane == 0) mbar_expect_tx(&sm.full[st], S::kTileBytes);
+      __syncwarp();
+      const int y = (t * kRows + (pi << box_shift)) & ((1 << p.page_shift) - 1);
+      if (pi < boxes)
+        tma_load_4d(sm.kv[st] + kc * (kRows * 128) + (pi << (box_shift + 7)), map, kc * 64, y, en.h, page, &sm.full[st]);
+      ++issued;
+      if (++st == S::kStages) { st = 0; ph ^= 1; }
+    };
+    const int A = en.paired ? 2 : 1;
+    int p0 = page_of(en.t0), p1 = page_of(en.t0 + 1), p2 = page_of(en.t0 + 2);  // of tiles t, t + 1, t + 2
+    for (int a = 0; ok && a < A && en.t0 + a < en.t1; ++a) load(&p.kmap, en.t0 + a, a == 0 ? p0 : p1);
+    for (int t = en.t0; ok && t < en.t1; ++t) {
+      const int next = page_of(t + 3);
+      load(&p.vmap, t, p0);
+      if (ok && t + A < en.t1) load(&p.kmap, t + A, A == 1 ? p1 : p2);
+      p0 = p1;
+      p1 = p2;
+      p2 = next;
+    }
+  }
+  // After an abort, wait (bounded) for the copies still landing before the CTA retires.
+  if (!ok || ld_volatile(&sm.abort_flag)) {
+    for (uint32_t b = 0; b < 2 && b < qn; ++b) attn_drain(&sm.qfull[(qn - 1 - b) & 1], ((qn - 1 - b) >> 1) & 1);
+    for (uint32_t b = 0; b < S::kStages && b < issued; ++b) {
+      const uint32_t n = issued - 1 - b;
+      attn_drain(&sm.full[n % S::kStages], (n / S::kStages) & 1);
+    }
+  }
+}
+
+// ---- warp 1: MMAs --------------------------------------------------------------------
+
+template <int D>
+__device__ __forceinline__ uint32_t s_col(int side) { return side * 128; }
+template <int D>
+__device__ __forceinline__ uint32_t o_col(int side) { return 256 + side * 128; }
+
+// Zeroes the rows of a V tile that hold no key of the unit, [128 t, lo) and [hi, 128 t + 128):
+// what lies there is any value, and 0 weight times NaN is NaN.  Only rows of a box that
+// also holds keys need it: the others were loaded as zeros.
+template <int D>
+__device__ __forceinline__ void mend_v(uint8_t* v, int t, int lo, int hi, int box) {
+  const int lane = threadIdx.x & 31;
+  const int k0 = t * kRows;
+  const int a = max(lo - k0, 0), b = min(hi - k0, kRows);
+  if (a == 0 && b == kRows) return;
+  auto zero = [&](int r0, int r1) {
+    for (int i = r0 * (D / 8) + lane; i < r1 * (D / 8); i += 32) {
+      const int r = i / (D / 8), c = i % (D / 8);
+      *reinterpret_cast<uint4*>(v + (c >> 3) * (kRows * 128) + r * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+    }
+  };
+  zero(a & ~(box - 1), a);
+  if (b > 0) zero(b, min(kRows, (b + box - 1) & ~(box - 1)));
+  fence_proxy_async();
+  __syncwarp();
+}
+
+template <int D, bool kFp16>
+__device__ __forceinline__ void mma_warp(const PagedAttnParams& p, AttnSmem<D>& sm, uint32_t tmem) {
+  using S = AttnSmem<D>;
+  constexpr uint32_t kBlock = kRows * 128;  // bytes of a 64-element column block
+  constexpr uint32_t kIdescQK = attn_idesc<kFp16, false>(128, 128), kIdescPV = attn_idesc<kFp16, true>(128, D);
+  const int box = 1 << min(p.page_shift, 7);
+  uint32_t st = 0, ph = 0, qn = 0;
+  uint32_t pph[2] = {0, 0};
+  bool ok = true;
+  auto advance = [&] { if (++st == S::kStages) { st = 0; ph ^= 1; } };
+  auto qk = [&](int x, uint32_t qslot, uint32_t stage) {
+    const uint64_t a = sw128_desc(smem_u32(sm.q[qslot])), b = sw128_desc(smem_u32(sm.kv[stage]));
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      const uint32_t off = (k >> 2) * (kBlock / 16) + (k & 3) * 2;
+      umma_bf16_elect(tmem + s_col<D>(x), a + off, b + off, kIdescQK, k > 0);
+    }
+    umma_commit_elect(&sm.sfull[x]);
+  };
+  auto pv = [&](int x, uint32_t stage, bool first) {
+    const uint64_t b = sw128_n_desc(smem_u32(sm.kv[stage]), kBlock);
+#pragma unroll
+    for (int k = 0; k < kRows / 16; ++k)
+      umma_ts_elect(tmem + o_col<D>(x), tmem + s_col<D>(x) + k * 8, b + k * (16 * 128 / 16), kIdescPV, !first || k > 0);
+  };
+  for (uint32_t e = 0; ok; ++e) {
+    const Entry en = take(p, sm, e);
+    if (en.rows == 0) break;
+    const int sides = en.paired ? 1 : 2, A = en.paired ? 2 : 1;
+    const uint32_t q0 = qn & 1;
+    for (int x = 0; ok && x < sides; ++x, ++qn) ok = attn_wait_warp(sm, &sm.qfull[qn & 1], (qn >> 1) & 1, p.status);
+    if (!ok) break;
+    const int n = en.t1 - en.t0;
+    uint32_t kstage = 0;
+    // the K tile is done with, and after the last one the rows' Q tiles
+    auto k_done = [&](int j) {
+      umma_commit_elect(&sm.empty[kstage]);
+      if (j == n - 1)
+        for (int x = 0; x < sides; ++x) umma_commit_elect(&sm.qempty[q0 ^ x]);
+    };
+    auto next_tile = [&]() {
+      ok = ok && attn_wait_warp(sm, &sm.full[st], ph, p.status);
+      tc_fence_after();
+      const uint32_t s = st;
+      advance();
+      return s;
+    };
+    if (en.paired) {
+      for (int j = 0; ok && j < 2 && j < n; ++j) {
+        kstage = next_tile();
+        if (!ok) break;
+        qk(j, q0, kstage);
+        k_done(j);
+      }
+    } else {
+      kstage = next_tile();
+      if (ok) {
+        qk(0, q0, kstage);
+        qk(1, q0 ^ 1, kstage);
+        k_done(0);
+      }
+    }
+    for (int j = 0; ok && j < n; ++j) {
+      const uint32_t vs = next_tile();
+      if (!ok) break;
+      mend_v<D>(sm.kv[vs], en.t0 + j, en.klo, en.khi, box);
+      const bool more = j + A < n;
+      for (int i = 0; ok && i < sides; ++i) {
+        const int x = en.paired ? (j & 1) : i;
+        ok = attn_wait_warp(sm, &sm.pfull[x], pph[x], p.status);
+        if (!ok) break;
+        pph[x] ^= 1;
+        tc_fence_after();
+        pv(x, vs, en.paired ? j < 2 : j == 0);
+        if (i == sides - 1) umma_commit_elect(&sm.empty[vs]);
+        if (more) {
+          if (i == 0) kstage = next_tile();
+          if (!ok) break;
+          qk(x, en.paired ? q0 : q0 ^ i, kstage);
+          if (i == sides - 1) k_done(j + A);
+        } else {
+          umma_commit_elect(&sm.ofull[x]);
+        }
+      }
+    }
+  }
+  umma_commit_elect(&sm.done);
+  attn_drain(&sm.done, 0);
+}
+
+// ---- softmax warpgroups ------------------------------------------------------------------
+
+template <int D>
+__device__ __forceinline__ size_t part_bytes() { return kRows * D * 4 + kRows * sizeof(float2); }
+
+template <int D, bool kFp16>
+__device__ __forceinline__ void softmax_group(const PagedAttnParams& p, AttnSmem<D>& sm, uint32_t tmem, int x) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int r = (warp & 3) * 32 + lane;  // row of the side = TMEM lane
+  const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+  const uint32_t ts = tmem + lanes + s_col<D>(x);
+  const float c = p.scale_log2;
+  // half precision: the weights are kept 2^7 larger, clear of its subnormals (a lagging maximum adds 2^kRaise)
+  constexpr float kUp = kFp16 ? 7.f : 0.f;
+  uint32_t sph = 0, oph = 0, xph = 0, wph = 0;
+  bool ok = true;
+  for (uint32_t e = 0; ok; ++e) {
+    const Entry en = take(p, sm, e);
+    if (en.rows == 0) break;
+    const int base = en.paired ? 0 : x * p.P * p.G;  // first row of the side in the unit
+    const int rows = min(en.rows - base, p.P * p.G);
+    const bool valid = r < rows;
+    const bool work = (warp & 3) * 32 < rows;  // the warp has rows
+    const int i = (base + r) / p.G;            // token of the row
+    const int t = en.pos0 + i;
+    const int lo = p.window > 0 ? t - p.window + 1 : 0;
+    // tiles [f0, f1) need no mask: every row of the side sees all of their keys
+    const int tok0 = base / p.G, tokn = (base + rows - 1) / p.G;
+    const int f1 = (en.pos0 + tok0 + 1) >> 7;
+    const int f0 = p.window > 0 ? (max(0, en.pos0 + tokn - p.window + 1) + 127) >> 7 : 0;
+    float m = -INFINITY, l = 0.f;
+    const int step = en.paired ? 2 : 1;
+    const int first = en.t0 + (en.paired ? x : 0);
+    for (int j = first; j < en.t1; j += step) {
+      ok = attn_wait_warp(sm, &sm.sfull[x], sph, p.status);
+      if (!ok) break;
+      sph ^= 1;
+      tc_fence_after();
+      if (work) {
+        uint32_t u[4][32];
+        tmem_ld64_async(ts, u[0], u[1]);
+        tmem_ld64_async(ts + 64, u[2], u[3]);
+        tmem_wait64(u[0], u[1]);
+        tmem_wait64(u[2], u[3]);
+        if (j < f0 || j >= f1) {
+          const int a = lo - j * kRows, b = t - j * kRows;  // the row sees keys a..b of the tile
+#pragma unroll
+          for (int q = 0; q < 128; ++q)
+            if (q < a || q > b) u[q >> 5][q & 31] = 0xff800000u;
+        }
+        float mx[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float v = fmax3(__uint_as_float(u[q][0]), __uint_as_float(u[q][1]), __uint_as_float(u[q][2]));
+#pragma unroll
+          for (int k = 3; k < 31; k += 2) v = fmax3(v, __uint_as_float(u[q][k]), __uint_as_float(u[q][k + 1]));
+          mx[q] = fmaxf(v, __uint_as_float(u[q][31]));
+        }
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+        if (j == first) {
+          m = top;
+        } else {
+          const bool raise = valid && top > m + kRaise;
+          if (__any_sync(0xffffffffu, raise)) {
+            // S of this tile is complete, so is O += P V of the side's tile before it, and the next waits for us
+            const float f = raise ? ex2_approx(m - top) : 1.f;
+            if (raise) { m = top; l *= f; }
+#pragma unroll 1
+            for (int q = 0; q < D; q += 32) {
+              uint32_t o[32];
+              tmem_ld32_async(tmem + lanes + o_col<D>(x) + q, o);
+              tmem_wait32(o);
+#pragma unroll
+              for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+              tmem_st32(tmem + lanes + o_col<D>(x) + q, o);
+            }
+          }
+        }
+        const float nb = (m == -INFINITY ? 0.f : -m) + kUp;
+        const float2 cc = make_float2(c, c), bb = make_float2(nb, nb);
+        float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          uint32_t w[32];
+#pragma unroll
+          for (int q = 0; q < 32; ++q) {
+            const int k = hh * 64 + 2 * q;
+            const float2 y = ffma2(make_float2(__uint_as_float(u[k >> 5][k & 31]), __uint_as_float(u[k >> 5][(k & 31) + 1])), cc, bb);
+            const float2 z = make_float2(ex2_approx(y.x), ex2_approx(y.y));
+            acc[q & 3] = fadd2(acc[q & 3], z);
+            w[q] = pack2<kFp16>(z.x, z.y);
+          }
+          tmem_st32(ts + hh * 32, w);
+        }
+        const float2 sum = fadd2(fadd2(acc[0], acc[1]), fadd2(acc[2], acc[3]));
+        l += sum.x + sum.y;
+        tmem_wait_st();
+      }
+      tc_fence_before();
+      __syncwarp();
+      mbar_arrive_elect(&sm.pfull[x]);
+    }
+    if (!ok) break;
+    // ---- the rows' output ----
+    const bool any = first < en.t1;  // the side had a tile (side 1 of a paired unit's single tile has none)
+    if (any) {
+      ok = attn_wait_warp(sm, &sm.ofull[x], oph, p.status);
+      if (!ok) break;
+      oph ^= 1;
+      tc_fence_after();
+    }
+    // factors of the two accumulators, and the columns that this side writes
+    float f0x = 1.f, f1x = 0.f;
+    int col0 = 0, cols = D;
+    uint32_t o0 = o_col<D>(x), o1 = 0;
+    bool both = false;
+    if (en.paired) {
+      sm.ml[x][r] = make_float2(m, l);
+      tc_fence_before();
+      __syncwarp();
+      mbar_arrive_elect(&sm.xfull);
+      ok = attn_wait_warp(sm, &sm.xfull, xph, p.status);
+      if (!ok) break;
+      tc_fence_after();
+      const float2 a = sm.ml[0][r], b = sm.ml[1][r];
+      both = en.t0 + 1 < en.t1;
+      m = both ? fmaxf(a.x, b.x) : a.x;
+      const float bs = m == -INFINITY ? 0.f : m;
+      f0x = ex2_approx(a.x - bs);
+      f1x = both ? ex2_approx(b.x - bs) : 0.f;
+      l = a.y * f0x + (both ? b.y * f1x : 0.f);
+      o0 = o_col<D>(0);
+      o1 = o_col<D>(1);
+      cols = D / 2;
+      col0 = x * cols;
+    }
+    const bool whole = en.pieces == 1;
+    const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
+    f0x *= inv;
+    f1x *= inv;
+    const long long piece = 2 * blockIdx.x + (en.first == static_cast<int>(blockIdx.x) ? 1 : 0);
+    uint8_t* part = p.parts + (piece * 2 + x) * part_bytes<D>();
+    uint8_t* orow = p.out + static_cast<long long>(en.tok0 + i) * p.out_token +
+                    static_cast<long long>(en.h * p.G + (base + r) - i * p.G) * p.out_head;
+    if (work) {
+#pragma unroll 1
+      for (int q = col0; q < col0 + cols; q += 32) {
+        uint32_t o[32];
+        float v[32];
+        tmem_ld32_async(tmem + lanes + o0 + q, o);
+        tmem_wait32(o);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(o[k]) * f0x;
+        if (both) {
+          tmem_ld32_async(tmem + lanes + o1 + q, o);
+          tmem_wait32(o);
+#pragma unroll
+          for (int k = 0; k < 32; ++k) v[k] = fmaf(__uint_as_float(o[k]), f1x, v[k]);
+        }
+        if (l == 0.f) {  // no key (or none above the type's range): nothing to weigh
+#pragma unroll
+          for (int k = 0; k < 32; ++k) v[k] = 0.f;
+        }
+        if (valid) {
+          if (whole) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 8) {
+              uint4 w;
+              w.x = pack2<kFp16>(v[k], v[k + 1]);
+              w.y = pack2<kFp16>(v[k + 2], v[k + 3]);
+              w.z = pack2<kFp16>(v[k + 4], v[k + 5]);
+              w.w = pack2<kFp16>(v[k + 6], v[k + 7]);
+              *reinterpret_cast<uint4*>(orow + (q + k) * 2) = w;
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 32; k += 4)
+              __stcg(reinterpret_cast<float4*>(part) + ((q - col0 + k) / 4) * kRows + r, make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]));
+          }
+        }
+      }
+    }
+    if (en.paired) {  // both sides have read both accumulators before either is written again
+      tc_fence_before();
+      __syncwarp();
+      mbar_arrive_elect(&sm.xfree);
+    }
+    constexpr float kLn2 = 0.6931471805599453f;
+    if (whole) {
+      if (p.lse && valid && (!en.paired || x == 0))
+        p.lse[static_cast<long long>(en.tok0 + i) * p.H_q + en.h * p.G + (base + r) - i * p.G] =
+            l > 0.f ? (m - kUp + lg2_approx(l)) * kLn2 : (l == 0.f ? -INFINITY : l);
+    } else {
+      float2* mlp = reinterpret_cast<float2*>(part + kRows * D * 4);
+      if (valid) __stcg(mlp + r, make_float2(m, l));
+      __threadfence();
+      __syncwarp();
+      mbar_arrive_elect(&sm.wrote[x]);
+      ok = attn_wait_warp(sm, &sm.wrote[x], wph, p.status);
+      if (!ok) break;
+      if ((warp & 3) == 0 && lane == 0) {
+        __threadfence();
+        int* cnt = p.sync + 2 * en.first + x;
+        const int n = atomicAdd(cnt, 1);
+        sm.last[x] = n == en.pieces - 1;
+        if (n == en.pieces - 1) atomicExch(cnt, 0);
+        __threadfence();
+        mbar_arrive(&sm.told[x]);
+      }
+      __syncwarp();
+      ok = attn_wait_warp(sm, &sm.told[x], wph, p.status);
+      wph ^= 1;
+      if (!ok) break;
+      if (sm.last[x] && rows > 0) {
+        // merge: record i of the unit is CTA first + i's; a row's factors first, then (row, 4 columns) per thread
+        auto rec = [&](int q) {
+          const long long cta = en.first + q;
+          return p.parts + ((2 * cta + (q == 0 ? 1 : 0)) * 2 + x) * part_bytes<D>();
+        };
+        const int tid = (warp & 3) * 32 + lane;
+        const int items = rows * (cols / 4);
+        for (int it = tid; it < items; it += 128) {
+          const int c4 = it / rows, rr = it - c4 * rows;
+          float mm = -INFINITY, ll = 0.f;
+          float4 acc4 = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int q0 = 0; q0 < en.pieces; q0 += 4) {
+            float2 z[4];
+            float4 v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              if (q0 + q < en.pieces) {
+                const uint8_t* rc = rec(q0 + q);
+                z[q] = __ldcg(reinterpret_cast<const float2*>(rc + kRows * D * 4) + rr);
+                v[q] = __ldcg(reinterpret_cast<const float4*>(rc) + c4 * kRows + rr);
+              } else {
+                z[q] = make_float2(-INFINITY, 0.f);
+                v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+              }
+            }
+            const float mn = fmaxf(fmaxf(fmaxf(z[0].x, z[1].x), fmaxf(z[2].x, z[3].x)), mm);
+            const float bs = mn == -INFINITY ? 0.f : mn;
+            float f = ex2_approx(mm - bs);
+            ll *= f;
+            acc4.x *= f; acc4.y *= f; acc4.z *= f; acc4.w *= f;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              f = ex2_approx(z[q].x - bs);
+              ll = fmaf(z[q].y, f, ll);
+              acc4.x = fmaf(v[q].x, f, acc4.x);
+              acc4.y = fmaf(v[q].y, f, acc4.y);
+              acc4.z = fmaf(v[q].z, f, acc4.z);
+              acc4.w = fmaf(v[q].w, f, acc4.w);
+            }
+            mm = mn;
+          }
+          const float iv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
+          const int ii = (base + rr) / p.G;
+          const int head = en.h * p.G + base + rr - ii * p.G;
+          uint2 w;
+          w.x = pack2<kFp16>(acc4.x * iv, acc4.y * iv);
+          w.y = pack2<kFp16>(acc4.z * iv, acc4.w * iv);
+          *reinterpret_cast<uint2*>(p.out + static_cast<long long>(en.tok0 + ii) * p.out_token +
+                                    static_cast<long long>(head) * p.out_head + (col0 + c4 * 4) * 2) = w;
+          if (p.lse && c4 == 0 && (!en.paired || x == 0))
+            p.lse[static_cast<long long>(en.tok0 + ii) * p.H_q + head] =
+                ll > 0.f ? (mm - kUp + lg2_approx(ll)) * kLn2 : (ll == 0.f ? -INFINITY : ll);
+        }
+      }
+    }
+    if (en.paired) {
+      ok = attn_wait_warp(sm, &sm.xfree, xph, p.status);
+      xph ^= 1;
+      tc_fence_after();
+    }
+  }
+}
+
+template <int D, bool kFp16>
+__global__ void __launch_bounds__(kAttnThreads, 1) paged_attn_kernel(const __grid_constant__ PagedAttnParams p) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  using S = AttnSmem<D>;
+  if (smem_u32(smem_raw) & 1023u) {  // the 128-byte swizzle needs 1024-byte aligned buffers
+    if (threadIdx.x == 0) atomicOr(p.status, kStatusDevice);
     return;
   }
-  const int pos = len - q_len + t - c0, h = j / p.G;
-  const int k0 = p.window > 0 ? max(0, pos + 1 - p.window) : 0;
-  constexpr int E = D / 64;
-  float2 q[E], o[E];
-  const uint32_t* qr = reinterpret_cast<const uint32_t*>(p.q + t * p.q_token + j * p.q_head);
-  for (int e = 0; e < E; ++e) { q[e] = unpack2(qr[lane * E + e], kFp16); o[e] = make_float2(0.f, 0.f); }
-  float m = -INFINITY, z = 0.f;
-  for (int k = k0; k <= pos; ++k) {
-    const int page = p.table[static_cast<long long>(s) * p.max_pages + (k >> p.c.page_shift)];
-    const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.c.num_pages);
-    if (!there && lane == 0) atomicOr(p.status, kStatusDevice);
-    const long long at = page * p.c.page_stride + (k & ((1 << p.c.page_shift) - 1)) * p.c.token_stride + h * p.c.head_stride;
-    const uint32_t* kr = reinterpret_cast<const uint32_t*>(p.c.K + at);
-    const uint32_t* vr = reinterpret_cast<const uint32_t*>(p.c.V + at);
-    float x = 0.f;
-    for (int e = 0; e < E; ++e) {
-      const float2 f = there ? unpack2(kr[lane * E + e], kFp16) : make_float2(0.f, 0.f);
-      x = fmaf(q[e].x, f.x, fmaf(q[e].y, f.y, x));
+  S& sm = *reinterpret_cast<S*>(smem_raw);
+  const int warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sm.qfull[i], 1);
+      mbar_init(&sm.qempty[i], 1);
+      mbar_init(&sm.sfull[i], 1);
+      mbar_init(&sm.pfull[i], 4);
+      mbar_init(&sm.ofull[i], 1);
+      mbar_init(&sm.wrote[i], 4);
+      mbar_init(&sm.told[i], 1);
     }
-    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    x *= p.scale_log2;
-    const float mn = fmaxf(m, x), a = exp2f(m - mn), b = exp2f(x - mn);
-    z = z * a + b;
-    for (int e = 0; e < E; ++e) {
-      const float2 f = there ? unpack2(vr[lane * E + e], kFp16) : make_float2(0.f, 0.f);
-      o[e].x = o[e].x * a + b * f.x;
-      o[e].y = o[e].y * a + b * f.y;
+    for (int i = 0; i < S::kStages; ++i) {
+      mbar_init(&sm.full[i], 1);
+      mbar_init(&sm.empty[i], 1);
     }
-    m = mn;
+    for (int i = 0; i < kEntries; ++i) {
+      mbar_init(&sm.efull[i], 1);
+      mbar_init(&sm.eempty[i], 10);  // the load and MMA warps and eight softmax warps
+    }
+    mbar_init(&sm.xfull, 8);
+    mbar_init(&sm.xfree, 8);
+    mbar_init(&sm.done, 1);
+    sm.abort_flag = 0;
+    fence_barrier_init();
+    fence_proxy_async();
   }
-  const float inv = z > 0.f ? 1.f / z : 0.f;
-  uint32_t* orow = reinterpret_cast<uint32_t*>(p.out + t * p.out_token + j * p.out_head);
-  for (int e = 0; e < E; ++e) {
-    uint32_t u;
-    if (kFp16) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(o[e].y * inv), "f"(o[e].x * inv));
-    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(o[e].y * inv), "f"(o[e].x * inv));
-    orow[lane * E + e] = u;
+  if (warp == 1) {
+    tmem_alloc(&sm.tmem_slot, 512);
+    tmem_relinquish();
   }
-  if (p.lse && lane == 0) p.lse[static_cast<long long>(t) * p.H_q + j] = z > 0.f ? (m + log2f(z)) * 0.6931471805599453f : -INFINITY;
+  pdl_wait();
+  pdl_trigger();
+  const Share sh = share_of(p, sm);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sm.tmem_slot;
+  if (warp < 4) {
+    regs_dealloc<kRegsAttnControl>();
+    if (warp == 0) load_warp<D>(p, sm);
+    if (warp == 1) mma_warp<D, kFp16>(p, sm, tmem);
+    if (warp == 2) deal(p, sm, sh);
+  } else {
+    regs_alloc<kRegsAttnSoftmax>();
+    softmax_group<D, kFp16>(p, sm, tmem, (warp - 4) >> 2);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+using AttnFn = void (*)(const PagedAttnParams);
+AttnFn attn_fn(int d, bool fp16) {
+  if (d == 64) return fp16 ? paged_attn_kernel<64, true> : paged_attn_kernel<64, false>;
+  return fp16 ? paged_attn_kernel<128, true> : paged_attn_kernel<128, false>;
+}
+size_t attn_smem(int d) { return d == 64 ? sizeof(AttnSmem<64>) : sizeof(AttnSmem<128>); }
+
+// Whether the compiled kernel's registers cover the warpgroups' split (an increase that
+// the launch's registers cannot cover would never complete).
+bool attn_regs_ok(int d, bool fp16) {
+  static std::once_flag once[4];
+  static bool ok[4] = {};
+  const int i = (d == 64 ? 0 : 2) + (fp16 ? 1 : 0);
+  std::call_once(once[i], [&] {
+    cudaFuncAttributes a = {};
+    ok[i] = cudaFuncGetAttributes(&a, attn_fn(d, fp16)) == cudaSuccess && a.numRegs * kAttnThreads >= kRegsAttnNeeded;
+  });
+  return ok[i];
+}
+
+bool encode16(CUtensorMap* m, bool fp16, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
+              const cuuint32_t* box) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  const cuuint32_t ones[4] = {1, 1, 1, 1};
+  return fn(m, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims,
+            strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+size_t attn_part_bytes(int d) { return kRows * d * 4 + kRows * sizeof(float2); }
 
 }  // namespace
 }  // namespace kvev
@@ -97,7 +959,8 @@ using namespace kvev;
 extern "C" int kvev_paged_attention_workspace(int H_q, int H_kv, int d, size_t* bytes) {
   if (!bytes || H_kv < 1 || H_q < 1 || H_q % H_kv) return KVEV_EINVAL;
   if ((d != 64 && d != 128) || H_q / H_kv > 128) return KVEV_ENOTSUP;
-  *bytes = KVEV_PAGED_SYNC_BYTES;
+  static_assert(2 * kMaxCtas * sizeof(int) <= KVEV_PAGED_SYNC_BYTES, "arrival counts");
+  *bytes = KVEV_PAGED_SYNC_BYTES + 4 * kMaxCtas * attn_part_bytes(d);
   return KVEV_OK;
 }
 
@@ -107,8 +970,8 @@ extern "C" int kvev_paged_attention(const kvev_paged_cache* cache, const void* q
                                     int window, void* out, int64_t out_token_stride, int64_t out_head_stride,
                                     float* lse, void* workspace, size_t workspace_bytes, int32_t* device_status,
                                     void* stream) {
-  PagedAttnParams p = {};
-  int rc = paged_view(cache, &p.c);
+  PagedView view = {};
+  int rc = paged_view(cache, &view);
   if (rc != KVEV_OK) return rc;
   size_t need = 0;
   rc = kvev_paged_attention_workspace(H_q, cache->H_kv, cache->d, &need);
@@ -125,31 +988,59 @@ extern "C" int kvev_paged_attention(const kvev_paged_cache* cache, const void* q
   if (!q || !out || !aligned16(q) || !aligned16(out) || !cu_new || !kv_lens || !block_table ||
       (reinterpret_cast<uintptr_t>(lse) & 3u))
     return KVEV_EINVAL;
-  p.q = static_cast<const uint4*>(q);
-  p.out = static_cast<uint4*>(out);
+
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return KVEV_ECUDA;
+  const int d = cache->d;
+  const bool fp16 = cache->dtype == KVEV_FP16;
+  if (!attn_regs_ok(d, fp16)) return KVEV_ENOTSUP;
+  PagedAttnParams p = {};
+  p.G = H_q / cache->H_kv;
+  p.P = kRows / p.G;
+  const cuuint64_t du = d;
+  {
+    const cuuint64_t dims[3] = {du, static_cast<cuuint64_t>(H_q), static_cast<cuuint64_t>(T)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(q_head_stride) * 2, static_cast<cuuint64_t>(q_token_stride) * 2};
+    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(p.G), static_cast<cuuint32_t>(p.P)};
+    const cuuint32_t box1[3] = {64, static_cast<cuuint32_t>(p.G), 1};
+    if (!encode16(&p.qmap, fp16, q, 3, dims, strides, box) || !encode16(&p.qmap1, fp16, q, 3, dims, strides, box1))
+      return KVEV_ECUDA;
+  }
+  {
+    const cuuint64_t dims[4] = {du, static_cast<cuuint64_t>(cache->page_size), static_cast<cuuint64_t>(cache->H_kv),
+                                static_cast<cuuint64_t>(cache->num_pages)};
+    const cuuint64_t strides[3] = {static_cast<cuuint64_t>(cache->token_stride) * 2, static_cast<cuuint64_t>(cache->head_stride) * 2,
+                                   static_cast<cuuint64_t>(cache->page_stride) * 2};
+    const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(cache->page_size < kRows ? cache->page_size : kRows), 1, 1};
+    if (!encode16(&p.kmap, fp16, cache->K, 4, dims, strides, box) || !encode16(&p.vmap, fp16, cache->V, 4, dims, strides, box))
+      return KVEV_ECUDA;
+  }
+  p.out = static_cast<uint8_t*>(out);
   p.lse = lse;
-  p.q_token = q_token_stride / 8;
-  p.q_head = q_head_stride / 8;
-  p.out_token = out_token_stride / 8;
-  p.out_head = out_head_stride / 8;
+  p.out_token = out_token_stride * 2;
+  p.out_head = out_head_stride * 2;
   p.cu = cu_new;
   p.kv_lens = kv_lens;
   p.table = block_table;
   p.B = B;
   p.T = T;
   p.H_q = H_q;
-  p.G = H_q / cache->H_kv;
+  p.H_kv = cache->H_kv;
+  p.page_shift = view.page_shift;
+  p.num_pages = view.num_pages;
   p.max_pages = max_pages;
   p.window = window;
-  p.scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt(static_cast<float>(cache->d))) * 1.4426950408889634f;
+  p.scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt(static_cast<float>(d))) * 1.4426950408889634f;
   p.status = device_status;
-  const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(T) * H_q + 7) / 8);
-  const bool h = cache->dtype == KVEV_FP16;
-  if (cache->d == 64) {
-    if (h) attn_kernel<64, 1><<<grid, 256, 0, st>>>(p); else attn_kernel<64, 0><<<grid, 256, 0, st>>>(p);
-  } else {
-    if (h) attn_kernel<128, 1><<<grid, 256, 0, st>>>(p); else attn_kernel<128, 0><<<grid, 256, 0, st>>>(p);
-  }
-  return cudaGetLastError() == cudaSuccess ? KVEV_OK : KVEV_ECUDA;
+  p.sync = static_cast<int*>(workspace);
+  p.parts = static_cast<uint8_t*>(workspace) + KVEV_PAGED_SYNC_BYTES;
+  const AttnFn fn = attn_fn(d, fp16);
+  const size_t smem = attn_smem(d);
+  if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
+    return KVEV_ECUDA;
+  const int grid = sms < kMaxCtas ? sms : kMaxCtas;
+  return launch_overlapped(fn, p, grid, kAttnThreads, smem, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KVEV_OK
+                                                                                                           : KVEV_ECUDA;
 }
