@@ -24,8 +24,8 @@
 // merges them in order, so the result does not depend on who that is.
 //
 // Roles (384 threads): warp 0 loads Q tiles and pages by TMA (a lane per page
-// box), warp 1 issues the MMAs, warp 2 deals the entries (pieces of units) to the
-// others through a ring, warps 4-7 and 8-11 are the sides' softmax warpgroups, a
+// box), warp 1 issues the MMAs, warp 2 deals the entries
+// (pieces of units) to the others through a ring, warps 4-7 and 8-11 are the sides' softmax warpgroups, a
 // thread per row.  S = Q K^T is read from tensor memory into registers, and the
 // weights go back into the same columns as the A operand of O += P V.
 #include <climits>
@@ -42,9 +42,14 @@ constexpr int kRegsAttnControl = 72, kRegsAttnSoftmax = 216;
 constexpr int kRegsAttnNeeded = 128 * kRegsAttnControl + 256 * kRegsAttnSoftmax;
 constexpr int kMaxCtas = 152;
 constexpr int kEntries = 4;         // ring of dealt entries
-constexpr int kUnitCost = 1;        // cost of a unit's start and end, in paired tiles
-constexpr int kMinShare = 2;        // least cost of a share: no piece of a cut unit is empty
+// Kinds of unit, and the cost of a key tile and of a unit's start and end in each.
+enum Kind : int { kFew = 0, kPaired = 1, kFull = 2 };
+constexpr int kFewRows = 16;
+__host__ __device__ constexpr int tile_cost(int kind) { return kind == kFull ? 2 : 1; }
+__host__ __device__ constexpr int unit_cost(int kind) { return kind == kFull ? 1 : 1; }
+constexpr int kMinShare = 2;        // least cost of a share, a tile's or more: no piece of a cut unit is empty
 constexpr int kRows = 128;          // rows of a side
+constexpr int kParts = 2;           // parts of a tile's weights that the second product takes as they come
 constexpr float kRaise = 8.f;       // a row's maximum is raised when a tile's is this much (log2) above it
 constexpr uint64_t kAttnWaitNs = 2000000000ull;
 
@@ -68,35 +73,39 @@ struct PagedAttnParams {
 struct Entry {
   int tok0, rows, pos0, h;         // first token, rows (0: no more entries), the first token's position, KV head
   int s, t0, t1, klo;              // request, key tiles [t0, t1), first key any row sees
-  int khi, paired, pieces, first;  // end of the keys, paired unit, pieces of the unit and the first one's CTA
+  int khi, kind, pieces, first;    // end of the keys, kind of unit, pieces of the unit and the first one's CTA
 };
 
 template <int D>
 struct AttnSmem {
   static constexpr int kTileBytes = kRows * D * 2;
   static constexpr int kStages = D == 128 ? 5 : 10;
-  uint8_t q[2][kTileBytes];
+  // (with 64-element rows the transposed products also read the tile's size of
+  // bytes after a V tile, for lanes that nothing reads: the Q tiles, after the last)
   uint8_t kv[kStages][kTileBytes];
-  float2 ml[2][kRows];   // the sides' (m, l) of a paired unit's rows
+  uint8_t q[2][kTileBytes];
+  float2 ml[2][kRows];   // the sides' (m, l) of the rows they share
   Entry ring[kEntries];
   uint64_t qfull[2], qempty[2], full[kStages], empty[kStages];
-  uint64_t sfull[2], pfull[2], ofull[2];
+  uint64_t sfull[2], pfull[2][kParts], ofull[2];
   uint64_t efull[kEntries], eempty[kEntries];
   uint64_t xfull, xfree;             // paired units: both sides' (m, l) are there; both sides are done with O
-  uint64_t wrote[2], told[2];        // a side's records are written; the count of arrivals is known
   uint64_t done;
   long long carry, start;
+  union {
+    float red[2][4][kFewRows];  // a side's warps' maxima or sums of a few rows
+    long long scan[kAttnThreads / 32];  // the schedule's sums, at the start
+  };
   int last[2];
   int abort_flag;
   uint32_t tmem_slot;
-  long long scan[kAttnThreads / 32];
 };
+static_assert(sizeof(AttnSmem<64>) <= 227 * 1024 && sizeof(AttnSmem<128>) <= 227 * 1024, "shared memory of a CTA");
 
 // ---- waits, bounded -------------------------------------------------------------
 
 template <class S>
 __device__ __forceinline__ bool attn_wait(S& sm, uint64_t* bar, uint32_t parity, int* status) {
-  if (mbar_try_wait(bar, parity)) return true;
   const uint64_t t0 = globaltimer_ns();
   while (!mbar_try_wait_sleep(bar, parity, 20000)) {
     if (ld_volatile(&sm.abort_flag)) return false;
@@ -109,8 +118,10 @@ __device__ __forceinline__ bool attn_wait(S& sm, uint64_t* bar, uint32_t parity,
   return true;
 }
 
+// By every lane of a warp; the warp agrees on the outcome.
 template <class S>
 __device__ __forceinline__ bool attn_wait_warp(S& sm, uint64_t* bar, uint32_t parity, int* status) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
   return __all_sync(0xffffffffu, attn_wait(sm, bar, parity, status));
 }
 
@@ -122,17 +133,30 @@ __device__ __forceinline__ void attn_drain(uint64_t* bar, uint32_t parity) {
 
 // ---- PTX ------------------------------------------------------------------------
 
-__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
+// From a whole converged warp; the operands are the same in every lane.
+__device__ __forceinline__ void tma_load_4d_elect(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w,
+                                                  uint32_t bar) {
   asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@e cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
       : "memory");
 }
 
-// D(tmem) (+)= A(tmem) * B(smem), from a whole converged warp.
-__device__ __forceinline__ void umma_ts_elect(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
-                                              uint32_t accumulate) {
+// D(tmem) (+)= A * B, 16-bit operands, fp32 sums; A in shared memory (ss) or tensor memory
+// (ts), B in shared memory.  From a whole converged warp, the operands the same in every lane.
+__device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p, e;\n\t"
       "elect.sync _|e, 0xffffffff;\n\t"
@@ -141,7 +165,6 @@ __device__ __forceinline__ void umma_ts_elect(uint32_t d_tmem, uint32_t a_tmem, 
       "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
@@ -153,6 +176,38 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+// R consecutive columns (4, 8 or 16) of this thread's lane.
+template <int R>
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[R]) {
+  if constexpr (R == 4)
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
+  else if constexpr (R == 8)
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr) : "memory");
+  else
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr) : "memory");
+}
+template <int R>
+__device__ __forceinline__ void tmem_st_cols(uint32_t taddr, const uint32_t (&r)[R]) {
+  if constexpr (R == 4)
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])
+                 : "memory");
+  else if constexpr (R == 8)
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+                 "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+  else
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+                 "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+                 "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 template <bool kFp16>
@@ -163,18 +218,18 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return u;
 }
 
-// Instruction descriptor: kind::f16, A and B of one 16-bit type, fp32 D; A K-major,
-// B K-major or (kBn) with its N index contiguous.
-template <bool kFp16, bool kBn>
+// Instruction descriptor: kind::f16, A and B of one 16-bit type, fp32 D; A and B
+// K-major, or with their M (kAm) or N (kBn) index contiguous.
+template <bool kFp16, bool kAm, bool kBn>
 __host__ __device__ constexpr uint32_t attn_idesc(int M, int N) {
-  return (1u << 4) | (kFp16 ? 0u : (1u << 7) | (1u << 10)) | (kBn ? 1u << 16 : 0u) |
+  return (1u << 4) | (kFp16 ? 0u : (1u << 7) | (1u << 10)) | (kAm ? 1u << 15 : 0u) | (kBn ? 1u << 16 : 0u) |
          (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
 
-// Descriptor of a V tile as the B operand: [D / 64][128 keys][64 elements], 128-byte
-// swizzle, N (the elements) contiguous: 64-element blocks `block` bytes apart, groups
+// Descriptor of a V tile as an operand whose K index is the key: [D / 64][128 keys][64
+// elements], 128-byte swizzle, the other index (the element) contiguous: 64-element blocks `block` bytes apart, groups
 // of 8 keys 1024 bytes apart.
-__device__ __forceinline__ uint64_t sw128_n_desc(uint32_t saddr, uint32_t block) {
+__device__ __forceinline__ uint64_t sw128_v_desc(uint32_t saddr, uint32_t block) {
   uint64_t d = 0;
   d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
   d |= static_cast<uint64_t>(block >> 4) << 16;
@@ -203,7 +258,7 @@ __device__ __forceinline__ Request request(const PagedAttnParams& p, int s, bool
 
 // Unit m of a request: tokens [2 P m, 2 P m + n), keys [lo, hi), key tiles [t0, t0 + tiles).
 struct Unit {
-  int n, lo, hi, t0, tiles, weight;
+  int n, lo, hi, t0, tiles, kind;
 };
 __device__ __forceinline__ Unit unit_of(const PagedAttnParams& p, const Request& r, int m) {
   Unit u;
@@ -214,8 +269,11 @@ __device__ __forceinline__ Unit unit_of(const PagedAttnParams& p, const Request&
   u.lo = p.window > 0 ? max(0, pos0 - p.window + 1) : 0;
   u.t0 = u.lo >> 7;
   u.tiles = max(1, ((u.hi + 127) >> 7) - u.t0);
-  u.weight = u.n > p.P ? 2 : 1;
+  u.kind = u.n > p.P ? kFull : u.n * p.G > kFewRows ? kPaired : kFew;
   return u;
+}
+__device__ __forceinline__ long long cost_of(const Unit& u) {
+  return static_cast<long long>(tile_cost(u.kind)) * u.tiles + unit_cost(u.kind);
 }
 __device__ __forceinline__ int units_of(const PagedAttnParams& p, int q) { return (q + 2 * p.P - 1) / (2 * p.P); }
 
@@ -225,7 +283,7 @@ __device__ __forceinline__ long long head_cost(const PagedAttnParams& p, const R
   const int M = units_of(p, r.q);
   for (int m = 0; m < M; ++m) {
     const Unit u = unit_of(p, r, m);
-    c += static_cast<long long>(u.weight) * u.tiles + kUnitCost;
+    c += cost_of(u);
   }
   return c;
 }
@@ -327,16 +385,16 @@ __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, const Shar
     int h = static_cast<int>((sh.x0 - a) / hc), m = 0;
     a += h * hc;
     Unit u = unit_of(p, r, m);
-    auto cost = [&] { return static_cast<long long>(u.weight) * u.tiles + kUnitCost; };
-    while (a + cost() <= sh.x0) {
-      a += cost();
+    while (a + cost_of(u) <= sh.x0) {
+      a += cost_of(u);
       u = unit_of(p, r, ++m);
     }
     while (a < sh.x1) {
-      // boundary x cuts a unit before tile ceil((x - a) / weight)
+      // boundary x cuts a unit before tile ceil((x - a) / cost of a tile)
+      const int w = tile_cost(u.kind);
       auto cut = [&](long long x) {
         const long long o = x - a;
-        return o <= 0 ? 0 : static_cast<int>(min(static_cast<long long>(u.tiles), (o + u.weight - 1) / u.weight));
+        return o <= 0 ? 0 : static_cast<int>(min(static_cast<long long>(u.tiles), (o + w - 1) / w));
       };
       const int c0 = cut(sh.x0), c1 = cut(sh.x1);
       if (c0 < c1) {
@@ -350,12 +408,12 @@ __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, const Shar
         en.t1 = u.t0 + c1;
         en.klo = u.lo;
         en.khi = u.hi;
-        en.paired = u.weight == 1;
+        en.kind = u.kind;
         en.first = static_cast<int>(a / sh.share);
-        en.pieces = static_cast<int>((a + static_cast<long long>(u.weight) * (u.tiles - 1)) / sh.share) - en.first + 1;
+        en.pieces = static_cast<int>((a + static_cast<long long>(w) * (u.tiles - 1)) / sh.share) - en.first + 1;
         if (!put(en)) return;
       }
-      a += cost();
+      a += cost_of(u);
       if (a >= sh.x1) break;
       if (2 * p.P * ++m >= r.q) {
         m = 0;
@@ -385,22 +443,21 @@ __device__ __forceinline__ Entry take(const PagedAttnParams& p, S& sm, uint32_t 
 }
 
 // ---- warp 0: loads -------------------------------------------------------------------
-// Order of an entry's tiles in the ring: A K tiles ahead of V (A = 2 for a paired unit,
-// whose sides work on two tiles at once; 1 for a full one).
+// Order of an entry's tiles in the ring: A K tiles ahead of V (A = 1 for a full unit;
+// 2 for the others, whose sides work on two tiles at once).
 template <int D>
 __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>& sm) {
   using S = AttnSmem<D>;
   const int lane = threadIdx.x & 31;
   const int box_shift = min(p.page_shift, 7);           // rows of a page box
   const int boxes = kRows >> box_shift;                 // page boxes of a tile
-  const int pi = lane / (D / 64), kc = lane % (D / 64); // the lane's page box and 64-element column
   uint32_t st = 0, ph = 0, qs = 0, qn = 0, issued = 0;
   bool ok = true;
   for (uint32_t e = 0; ok; ++e) {
     const Entry en = take(p, sm, e);
     if (en.rows == 0) break;
     // ---- Q tiles ----
-    const int sides = en.paired ? 1 : 2;
+    const int sides = en.kind == kFull ? 2 : 1;
     for (int x = 0; ok && x < sides; ++x) {
       if (!attn_wait_warp(sm, &sm.qempty[qs], ((qn >> 1) & 1) ^ 1, p.status)) { ok = false; break; }
       const bool one = en.rows == p.G;
@@ -417,11 +474,11 @@ __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>&
       qs ^= 1;
     }
     // ---- pages ----
-    // the page of the lane's box in tile t (its number; num_pages = zeros)
+    // the page of box `lane` of tile t (its number; num_pages = zeros)
     const int* row = p.table + static_cast<long long>(en.s) * p.max_pages;
     auto page_of = [&](int t) {
-      const int k = t * kRows + (pi << box_shift);
-      if (t >= en.t1 || pi >= boxes || k >= en.khi || k + (1 << box_shift) <= en.klo) return p.num_pages;
+      const int k = t * kRows + (lane << box_shift);
+      if (t >= en.t1 || lane >= boxes || k >= en.khi || k + (1 << box_shift) <= en.klo) return p.num_pages;
       const int id = __ldg(row + (k >> p.page_shift));
       if (static_cast<unsigned>(id) < static_cast<unsigned>(p.num_pages)) return id;
       atomicOr(p.status, kStatusDevice);
@@ -431,13 +488,19 @@ __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>&
       if (!attn_wait_warp(sm, &sm.empty[st], ph ^ 1, p.status)) { ok = false; return; }
       if (lane == 0) mbar_expect_tx(&sm.full[st], S::kTileBytes);
       __syncwarp();
-      const int y = (t * kRows + (pi << box_shift)) & ((1 << p.page_shift) - 1);
-      if (pi < boxes)
-        tma_load_4d(sm.kv[st] + kc * (kRows * 128) + (pi << (box_shift + 7)), map, kc * 64, y, en.h, page, &sm.full[st]);
+      const int y = (t * kRows) & ((1 << p.page_shift) - 1);  // a page is whole boxes, or a box whole pages
+      const uint32_t dst = smem_u32(sm.kv[st]), bar = smem_u32(&sm.full[st]);
+#pragma unroll 2
+      for (int i = 0; i < boxes; ++i) {
+        const int pg = __shfl_sync(0xffffffffu, page, i);
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c)
+          tma_load_4d_elect(dst + c * (kRows * 128) + (i << (box_shift + 7)), map, c * 64, y, en.h, pg, bar);
+      }
       ++issued;
       if (++st == S::kStages) { st = 0; ph ^= 1; }
     };
-    const int A = en.paired ? 2 : 1;
+    const int A = en.kind == kFull ? 1 : 2;
     int p0 = page_of(en.t0), p1 = page_of(en.t0 + 1), p2 = page_of(en.t0 + 2);  // of tiles t, t + 1, t + 2
     for (int a = 0; ok && a < A && en.t0 + a < en.t1; ++a) load(&p.kmap, en.t0 + a, a == 0 ? p0 : p1);
     for (int t = en.t0; ok && t < en.t1; ++t) {
@@ -461,114 +524,143 @@ __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>&
 
 // ---- warp 1: MMAs --------------------------------------------------------------------
 
+// The weights of a side's few rows, [2][16 rows][64 keys] with the 128-byte swizzle, lie in
+// the rows' Q tile from its row 32 on.
+__device__ __forceinline__ uint32_t few_p_offset(int side) { return 4096 + side * 4096; }
+
 template <int D>
 __device__ __forceinline__ uint32_t s_col(int side) { return side * 128; }
 template <int D>
 __device__ __forceinline__ uint32_t o_col(int side) { return 256 + side * 128; }
 
-// Zeroes the rows of a V tile that hold no key of the unit, [128 t, lo) and [hi, 128 t + 128):
-// what lies there is any value, and 0 weight times NaN is NaN.  Only rows of a box that
-// also holds keys need it: the others were loaded as zeros.
-template <int D>
-__device__ __forceinline__ void mend_v(uint8_t* v, int t, int lo, int hi, int box) {
-  const int lane = threadIdx.x & 31;
-  const int k0 = t * kRows;
-  const int a = max(lo - k0, 0), b = min(hi - k0, kRows);
-  if (a == 0 && b == kRows) return;
-  auto zero = [&](int r0, int r1) {
-    for (int i = r0 * (D / 8) + lane; i < r1 * (D / 8); i += 32) {
-      const int r = i / (D / 8), c = i % (D / 8);
-      *reinterpret_cast<uint4*>(v + (c >> 3) * (kRows * 128) + r * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
-    }
-  };
-  zero(a & ~(box - 1), a);
-  if (b > 0) zero(b, min(kRows, (b + box - 1) & ~(box - 1)));
-  fence_proxy_async();
-  __syncwarp();
-}
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 
+// One warp issues every MMA: the sides' products run in turn, whole (issued by a thread
+// for each side they interleave, and either side waits twice as long for its own).  What
+// steers it is broadcast from lane 0, so that the compiler sees one path for the warp and
+// keeps the MMAs' operands in uniform registers.
 template <int D, bool kFp16>
 __device__ __forceinline__ void mma_warp(const PagedAttnParams& p, AttnSmem<D>& sm, uint32_t tmem) {
   using S = AttnSmem<D>;
   constexpr uint32_t kBlock = kRows * 128;  // bytes of a 64-element column block
-  constexpr uint32_t kIdescQK = attn_idesc<kFp16, false>(128, 128), kIdescPV = attn_idesc<kFp16, true>(128, D);
-  const int box = 1 << min(p.page_shift, 7);
-  uint32_t st = 0, ph = 0, qn = 0;
-  uint32_t pph[2] = {0, 0};
+  constexpr uint32_t kIdescQK = attn_idesc<kFp16, false, false>(128, 128);
+  constexpr uint32_t kIdescPV = attn_idesc<kFp16, false, true>(128, D);
+  constexpr uint32_t kIdescKQ = attn_idesc<kFp16, false, false>(128, kFewRows);
+  constexpr uint32_t kIdescVP = attn_idesc<kFp16, true, false>(128, kFewRows);
+  uint32_t st = 0, ph = 0, qn = 0, pph[2] = {0, 0};
   bool ok = true;
   auto advance = [&] { if (++st == S::kStages) { st = 0; ph ^= 1; } };
-  auto qk = [&](int x, uint32_t qslot, uint32_t stage) {
-    const uint64_t a = sw128_desc(smem_u32(sm.q[qslot])), b = sw128_desc(smem_u32(sm.kv[stage]));
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
-      const uint32_t off = (k >> 2) * (kBlock / 16) + (k & 3) * 2;
-      umma_bf16_elect(tmem + s_col<D>(x), a + off, b + off, kIdescQK, k > 0);
-    }
-    umma_commit_elect(&sm.sfull[x]);
-  };
-  auto pv = [&](int x, uint32_t stage, bool first) {
-    const uint64_t b = sw128_n_desc(smem_u32(sm.kv[stage]), kBlock);
-#pragma unroll
-    for (int k = 0; k < kRows / 16; ++k)
-      umma_ts_elect(tmem + o_col<D>(x), tmem + s_col<D>(x) + k * 8, b + k * (16 * 128 / 16), kIdescPV, !first || k > 0);
+  auto tile = [&] {  // the next tile of the ring has landed
+    ok = ok && attn_wait_warp(sm, &sm.full[st], ph, p.status);
   };
   for (uint32_t e = 0; ok; ++e) {
     const Entry en = take(p, sm, e);
-    if (en.rows == 0) break;
-    const int sides = en.paired ? 1 : 2, A = en.paired ? 2 : 1;
+    if (uniform(en.rows) == 0) break;
+    const int n = uniform(en.t1 - en.t0), kind = uniform(en.kind);
     const uint32_t q0 = qn & 1;
-    for (int x = 0; ok && x < sides; ++x, ++qn) ok = attn_wait_warp(sm, &sm.qfull[qn & 1], (qn >> 1) & 1, p.status);
-    if (!ok) break;
-    const int n = en.t1 - en.t0;
-    uint32_t kstage = 0;
-    // the K tile is done with, and after the last one the rows' Q tiles
-    auto k_done = [&](int j) {
-      umma_commit_elect(&sm.empty[kstage]);
-      if (j == n - 1)
-        for (int x = 0; x < sides; ++x) umma_commit_elect(&sm.qempty[q0 ^ x]);
-    };
-    auto next_tile = [&]() {
-      ok = ok && attn_wait_warp(sm, &sm.full[st], ph, p.status);
-      tc_fence_after();
-      const uint32_t s = st;
-      advance();
-      return s;
-    };
-    if (en.paired) {
-      for (int j = 0; ok && j < 2 && j < n; ++j) {
-        kstage = next_tile();
-        if (!ok) break;
-        qk(j, q0, kstage);
-        k_done(j);
-      }
-    } else {
-      kstage = next_tile();
-      if (ok) {
-        qk(0, q0, kstage);
-        qk(1, q0 ^ 1, kstage);
-        k_done(0);
-      }
-    }
-    for (int j = 0; ok && j < n; ++j) {
-      const uint32_t vs = next_tile();
-      if (!ok) break;
-      mend_v<D>(sm.kv[vs], en.t0 + j, en.klo, en.khi, box);
-      const bool more = j + A < n;
-      for (int i = 0; ok && i < sides; ++i) {
-        const int x = en.paired ? (j & 1) : i;
-        ok = attn_wait_warp(sm, &sm.pfull[x], pph[x], p.status);
+    if (kind == kFew) {
+      // transposed products: S^T = K Q^T (lanes are keys), O^T += V^T P^T (lanes are elements)
+      ok = attn_wait_warp(sm, &sm.qfull[q0], (qn >> 1) & 1, p.status);
+      ++qn;
+      const uint64_t qdesc = sw128_desc(smem_u32(sm.q[q0]));
+      auto kq = [&](int x) {
+        tile();
+        if (!ok) return;
+        tc_fence_after();
+        const uint64_t kdesc = sw128_desc(smem_u32(sm.kv[st]));
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t off = (k >> 2) * (kBlock / 16) + (k & 3) * 2;
+          umma_ss(tmem + s_col<D>(x), kdesc + off, qdesc + off, kIdescKQ, k > 0);
+        }
+        umma_commit_elect(&sm.sfull[x]);
+        umma_commit_elect(&sm.empty[st]);
+        advance();
+      };
+      for (int j = 0; j < 2 && j < n; ++j) kq(j);
+      for (int j = 0; ok && j < n; ++j) {
+        const int x = j & 1;
+        tile();
+        ok = ok && attn_wait_warp(sm, &sm.pfull[x][kParts - 1], pph[x], p.status);
         if (!ok) break;
         pph[x] ^= 1;
         tc_fence_after();
-        pv(x, vs, en.paired ? j < 2 : j == 0);
-        if (i == sides - 1) umma_commit_elect(&sm.empty[vs]);
+        const uint64_t vdesc = sw128_v_desc(smem_u32(sm.kv[st]), kBlock);
+        const uint64_t pdesc = sw128_desc(smem_u32(sm.q[q0]) + few_p_offset(x));
+#pragma unroll
+        for (int k = 0; k < kRows / 16; ++k)
+          umma_ss(tmem + o_col<D>(x), vdesc + k * (16 * 128 / 16), pdesc + (k >> 2) * (kFewRows * 128 / 16) + (k & 3) * 2,
+                  kIdescVP, j >= 2 || k > 0);
+        umma_commit_elect(&sm.empty[st]);
+        if (j + 2 >= n) umma_commit_elect(&sm.ofull[x]);
+        advance();
+        if (j + 2 < n) kq(x);
+      }
+      umma_commit_elect(&sm.qempty[q0]);  // (the weights lie in the Q tile)
+    } else {
+      const bool full = kind == kFull;
+      const int sides = full ? 2 : 1, A = full ? 1 : 2;
+      for (int i = 0; ok && i < sides; ++i, ++qn) ok = attn_wait_warp(sm, &sm.qfull[qn & 1], (qn >> 1) & 1, p.status);
+      auto qk = [&](int x, uint32_t q, uint32_t stage) {
+        const uint64_t qdesc = sw128_desc(smem_u32(sm.q[q])), kdesc = sw128_desc(smem_u32(sm.kv[stage]));
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t off = (k >> 2) * (kBlock / 16) + (k & 3) * 2;
+          umma_ss(tmem + s_col<D>(x), qdesc + off, kdesc + off, kIdescQK, k > 0);
+        }
+        umma_commit_elect(&sm.sfull[x]);
+      };
+      // the K tile is done with, and after the last one the rows' Q tiles
+      auto k_done = [&](int j, uint32_t stage) {
+        umma_commit_elect(&sm.empty[stage]);
+        if (j == n - 1)
+          for (int i = 0; i < sides; ++i) umma_commit_elect(&sm.qempty[q0 ^ i]);
+      };
+      for (int j = 0; ok && j < A && j < n; ++j) {
+        tile();
+        if (!ok) break;
+        tc_fence_after();
+        qk(j, q0, st);
+        if (full) qk(1, q0 ^ 1, st);
+        k_done(j, st);
+        advance();
+      }
+      for (int j = 0; ok && j < n; ++j) {
+        // both tiles of the round are there before the first weights are waited for
+        const uint32_t vs = st;
+        tile();
+        advance();
+        const bool more = j + A < n;
+        const uint32_t ks = st;
         if (more) {
-          if (i == 0) kstage = next_tile();
+          tile();
+          advance();
+        }
+        for (int i = 0; ok && i < sides; ++i) {
+          const int x = full ? i : j & 1;
+          const uint64_t vdesc = sw128_v_desc(smem_u32(sm.kv[vs]), kBlock);
+          const bool first = j < A;
+#pragma unroll
+          for (int part = 0; part < kParts; ++part) {
+            ok = ok && attn_wait_warp(sm, &sm.pfull[x][part], pph[x], p.status);
+            tc_fence_after();
+            if (ok) {
+#pragma unroll
+              for (int k = part * 8 / kParts; k < (part + 1) * 8 / kParts; ++k)
+                umma_ts(tmem + o_col<D>(x), tmem + s_col<D>(x) + k * 8, vdesc + k * (16 * 128 / 16), kIdescPV, !first || k > 0);
+            }
+          }
           if (!ok) break;
-          qk(x, en.paired ? q0 : q0 ^ i, kstage);
-          if (i == sides - 1) k_done(j + A);
-        } else {
-          umma_commit_elect(&sm.ofull[x]);
+          pph[x] ^= 1;
+          if (more) {
+            qk(x, full ? q0 ^ i : q0, ks);
+          } else {
+            umma_commit_elect(&sm.ofull[x]);
+          }
+          if (i == sides - 1) {
+            umma_commit_elect(&sm.empty[vs]);
+            if (more) k_done(j + A, ks);
+          }
         }
       }
     }
@@ -578,279 +670,562 @@ __device__ __forceinline__ void mma_warp(const PagedAttnParams& p, AttnSmem<D>& 
 }
 
 // ---- softmax warpgroups ------------------------------------------------------------------
+// A group's four warps run in step: they agree on every entry, and a wait that ran out
+// (ok = false) lets them run on with whatever is there, so that each reaches the same
+// barriers; the waits of an aborted CTA return at once.
 
 template <int D>
 __device__ __forceinline__ size_t part_bytes() { return kRows * D * 4 + kRows * sizeof(float2); }
 
+__device__ __forceinline__ void group_sync(int x) { named_bar_sync(1 + x, 128); }
+__device__ __forceinline__ bool group_any(int x, bool v) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred a, b;\n\t"
+      "setp.ne.u32 a, %1, 0;\n\t"
+      "barrier.cta.red.or.pred b, %2, 128, a;\n\t"
+      "selp.u32 %0, 1, 0, b;\n\t}"
+      : "=r"(r)
+      : "r"(static_cast<uint32_t>(v)), "r"(1 + x)
+      : "memory");
+  return r != 0;
+}
+
+// What a softmax warp keeps from entry to entry.
+struct SideState {
+  uint32_t sph = 0, oph = 0, xph = 0, qn = 0;  // phases of its barriers, Q tiles before this entry
+  uint32_t tiles = 0;                          // K and V tiles before this entry
+  bool ok = true;
+};
+
+// Before a side's weights of tile j (the a-th of the entry) are handed over: zeroes the
+// rows of the V tile that hold no key of the unit, of which anything may be in the pool
+// (0 weight times NaN is NaN).  Only the rows of a page box that also holds keys need it,
+// the others were loaded as zeros.  In a full unit both sides write the same zeros.
+template <int D>
+__device__ __forceinline__ void mend_v(const PagedAttnParams& p, AttnSmem<D>& sm, const Entry& en, int j, SideState& st) {
+  const int k0 = j * kRows, a = max(en.klo - k0, 0), b = min(en.khi - k0, kRows);
+  if (a == 0 && b == kRows) return;
+  const int n = en.t1 - en.t0, i = j - en.t0;
+  // the V tile's place in the ring's order (K tiles run 1 or 2 ahead)
+  const uint32_t at = st.tiles + (en.kind == kFull ? 2 * i + 1 : min(2 * i + 2, 2 * n - 1));
+  const uint32_t stage = at % AttnSmem<D>::kStages;
+  st.ok = st.ok && attn_wait_warp(sm, &sm.full[stage], (at / AttnSmem<D>::kStages) & 1, p.status);
+  const int box = 1 << min(p.page_shift, 7);
+  auto zero = [&](int r0, int r1) {
+    for (int q = r0 * (D / 8) + static_cast<int>(threadIdx.x & 127); q < r1 * (D / 8); q += 128) {
+      const int r = q / (D / 8), c = q % (D / 8);
+      *reinterpret_cast<uint4*>(sm.kv[stage] + (c >> 3) * (kRows * 128) + r * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+    }
+  };
+  zero(a & ~(box - 1), a);
+  if (b > 0) zero(b, min(kRows, (b + box - 1) & ~(box - 1)));
+  fence_proxy_async();
+}
+
+template <int D>
+struct Records {  // of a cut unit's piece, side x: the rows' unnormalised output, then their (m, l)
+  uint8_t* at;
+  __device__ float2* ml() const { return reinterpret_cast<float2*>(at + kRows * D * 4); }
+};
+template <int D>
+__device__ __forceinline__ Records<D> records(const PagedAttnParams& p, long long cta, bool first, int x) {
+  return {p.parts + ((2 * cta + (first ? 1 : 0)) * 2 + x) * part_bytes<D>()};
+}
+
+// After the group's records of a piece are written: whether it is the last of the unit's pieces.
+template <int D>
+__device__ __forceinline__ bool arrived_last(const PagedAttnParams& p, AttnSmem<D>& sm, const Entry& en, int x, bool ok) {
+  __threadfence();
+  group_sync(x);
+  if ((threadIdx.x & 127) == 0) {
+    int last = 0;
+    if (ok) {
+      int* cnt = p.sync + 2 * en.first + x;
+      last = atomicAdd(cnt, 1) == en.pieces - 1;
+      if (last) atomicExch(cnt, 0);
+      __threadfence();
+    }
+    sm.last[x] = last;
+  }
+  group_sync(x);
+  return sm.last[x] != 0;
+}
+
+__device__ __forceinline__ float lse_of(float m, float l) {  // natural log; m and l of weights 2^up larger
+  return l > 0.f ? (m + lg2_approx(l)) * 0.6931471805599453f : (l == 0.f ? -INFINITY : l);
+}
+__device__ __forceinline__ float finite_or_0(float m) { return m == -INFINITY ? 0.f : m; }
+
+// ---- up to 16 rows: a thread per key ----
+// S^T has the tile's keys on the lanes and the rows in the columns, so a thread forms
+// its key's weights of R rows; they go to shared memory as the B operand of
+// O^T += V^T P^T.  All threads hold the rows' maxima; each sums its own keys' weights.
+template <int D, bool kFp16, int R>
+__device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D>& sm, uint32_t tmem, int x, const Entry& en,
+                                         SideState& st) {
+  const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, key = warp * 32 + lane;
+  const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
+  const uint32_t ts = tmem + lanes + s_col<D>(x);
+  const float c = p.scale_log2;
+  constexpr float kUp = kFp16 ? 7.f : 0.f;
+  // this key's 2 bytes of row r: r * 128 + ((chunk ^ r) & 7) * 16 + ... in the 64-key half
+  uint8_t* const pw = sm.q[st.qn & 1] + few_p_offset(x) + (key >> 6) * (kFewRows * 128) + (key & 7) * 2;
+  const int chunk = (key & 63) >> 3;
+  const int tokn = (en.rows - 1) / p.G;
+  const int f1 = en.rows < R ? 0 : (en.pos0 + 1) >> 7;  // [f0, f1): every row sees every key
+  const int f0 = p.window > 0 ? (max(0, en.pos0 + tokn - p.window + 1) + 127) >> 7 : 0;
+  float m[R], l[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) { m[r] = -INFINITY; l[r] = 0.f; }
+  const int first = en.t0 + x;
+  for (int j = first; j < en.t1; j += 2) {
+    st.ok = st.ok && attn_wait_warp(sm, &sm.sfull[x], st.sph, p.status);
+    st.sph ^= 1;
+    tc_fence_after();
+    uint32_t u[R];
+    tmem_ld_cols<R>(ts, u);
+    float y[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) y[r] = __uint_as_float(u[r]) * c;
+    if (j < f0 || j >= f1) {
+      const int k = j * kRows + key;
+      int t = en.pos0, g = 0;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (r >= en.rows || k > t || (p.window > 0 && k <= t - p.window)) y[r] = -INFINITY;
+        if (++g == p.G) { g = 0; ++t; }
+      }
+    }
+    bool up = false;
+#pragma unroll
+    for (int r = 0; r < R; ++r) up |= y[r] > m[r] + kRaise;
+    if (group_any(x, up)) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float v = y[r];
+#pragma unroll
+        for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+        if (lane == 0) sm.red[x][warp][r] = v;
+      }
+      group_sync(x);
+      float f[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const float top = fmaxf(fmaxf(sm.red[x][0][r], sm.red[x][1][r]), fmaxf(sm.red[x][2][r], sm.red[x][3][r]));
+        const float mn = fmaxf(m[r], top);
+        f[r] = ex2_approx(m[r] - finite_or_0(mn));
+        m[r] = mn;
+        l[r] *= f[r];
+      }
+      if (j != first) {
+        // S of this tile is complete, so is O of the side's tile before it, and the next waits for us
+        uint32_t o[R];
+        tmem_ld_cols<R>(tmem + lanes + o_col<D>(x), o);
+#pragma unroll
+        for (int r = 0; r < R; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * f[r]);
+        tmem_st_cols<R>(tmem + lanes + o_col<D>(x), o);
+        tmem_wait_st();
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const float w = ex2_approx(y[r] - (finite_or_0(m[r]) - kUp));
+      l[r] += w;
+      *reinterpret_cast<uint16_t*>(pw + r * 128 + ((chunk ^ r) & 7) * 16) = static_cast<uint16_t>(pack2<kFp16>(w, 0.f));
+    }
+    mend_v<D>(p, sm, en, j, st);
+    fence_proxy_async();
+    tc_fence_before();
+    __syncwarp();
+#pragma unroll
+    for (int part = 0; part < kParts; ++part) mbar_arrive_elect(&sm.pfull[x][part]);
+  }
+  // ---- the rows' output: sums over the keys, then both sides' accumulators ----
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    float v = l[r];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    l[r] = v;
+  }
+  group_sync(x);  // (the maxima's readers are done)
+  if (lane < R) {
+    float v = 0.f;
+#pragma unroll
+    for (int r = 0; r < R; ++r) v = r == lane ? l[r] : v;
+    sm.red[x][warp][lane] = v;
+  }
+  group_sync(x);
+  if (warp == 0 && lane < R) {
+    float v = 0.f;
+#pragma unroll
+    for (int r = 0; r < R; ++r) v = r == lane ? m[r] : v;
+    sm.ml[x][lane] = make_float2(v, (sm.red[x][0][lane] + sm.red[x][1][lane]) + (sm.red[x][2][lane] + sm.red[x][3][lane]));
+  }
+  if (first < en.t1) {  // (side 1 of a single tile has no accumulator)
+    st.ok = st.ok && attn_wait_warp(sm, &sm.ofull[x], st.oph, p.status);
+    st.oph ^= 1;
+  }
+  tc_fence_before();
+  __syncwarp();
+  mbar_arrive_elect(&sm.xfull);
+  st.ok = st.ok && attn_wait_warp(sm, &sm.xfull, st.xph, p.status);
+  tc_fence_after();
+  const bool both = en.t0 + 1 < en.t1, whole = en.pieces == 1;
+  float v[R];
+  {
+    uint32_t o[R];
+    tmem_ld_cols<R>(tmem + lanes + o_col<D>(0), o);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const float2 a = sm.ml[0][r], b = both ? sm.ml[1][r] : make_float2(-INFINITY, 0.f);
+      m[r] = fmaxf(a.x, b.x);
+      const float f = ex2_approx(a.x - finite_or_0(m[r]));
+      l[r] = fmaf(a.y, f, b.y * ex2_approx(b.x - finite_or_0(m[r])));
+      v[r] = l[r] == 0.f ? 0.f : __uint_as_float(o[r]) * f;
+    }
+    if (both) {
+      tmem_ld_cols<R>(tmem + lanes + o_col<D>(1), o);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (l[r] != 0.f) v[r] = fmaf(__uint_as_float(o[r]), ex2_approx(sm.ml[1][r].x - finite_or_0(m[r])), v[r]);
+    }
+  }
+  tc_fence_before();
+  __syncwarp();
+  mbar_arrive_elect(&sm.xfree);
+  // side x writes the rows r with r mod 2 = x; the thread's element is d = key
+  auto emit = [&](int r, float o, float mm, float ll) {
+    const int i = r / p.G, head = en.h * p.G + r - i * p.G;
+    if (key < D)
+      *reinterpret_cast<uint16_t*>(p.out + static_cast<long long>(en.tok0 + i) * p.out_token +
+                                   static_cast<long long>(head) * p.out_head + key * 2) = static_cast<uint16_t>(pack2<kFp16>(o, 0.f));
+    if (p.lse && key == r) p.lse[static_cast<long long>(en.tok0 + i) * p.H_q + head] = lse_of(mm - kUp, ll);
+  };
+  if (whole) {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if ((r & 1) == x && r < en.rows) emit(r, v[r] * (l[r] == 0.f ? 0.f : 1.f / l[r]), m[r], l[r]);
+  } else {
+    const Records<D> mine = records<D>(p, blockIdx.x, en.first == static_cast<int>(blockIdx.x), x);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if ((r & 1) == x && r < en.rows) {
+        if (key < D) __stcg(reinterpret_cast<float*>(mine.at) + r * D + key, v[r]);
+        if (key == r) __stcg(mine.ml() + r, make_float2(m[r], l[r]));
+      }
+    if (arrived_last(p, sm, en, x, st.ok)) {
+#pragma unroll 1
+      for (int r = x; r < en.rows; r += 2) {
+        float mm = -INFINITY, ll = 0.f, oo = 0.f;
+        constexpr int kU = 8;
+        for (int q0 = 0; q0 < en.pieces; q0 += kU) {
+          float2 z[kU];
+          float o[kU];
+#pragma unroll
+          for (int q = 0; q < kU; ++q) {
+            z[q] = make_float2(-INFINITY, 0.f);
+            o[q] = 0.f;
+            if (q0 + q < en.pieces) {
+              const Records<D> rec = records<D>(p, en.first + q0 + q, q0 + q == 0, x);
+              z[q] = __ldcg(rec.ml() + r);
+              if (key < D) o[q] = __ldcg(reinterpret_cast<const float*>(rec.at) + r * D + key);
+            }
+          }
+          float mn = mm;
+#pragma unroll
+          for (int q = 0; q < kU; ++q) mn = fmaxf(mn, z[q].x);
+          const float bs = finite_or_0(mn), f0 = ex2_approx(mm - bs);
+          ll *= f0;
+          oo *= f0;
+#pragma unroll
+          for (int q = 0; q < kU; ++q) {
+            const float f = ex2_approx(z[q].x - bs);
+            ll = fmaf(z[q].y, f, ll);
+            oo = fmaf(o[q], f, oo);
+          }
+          mm = mn;
+        }
+        emit(r, ll == 0.f ? 0.f : oo * (1.f / ll), mm, ll);
+      }
+    }
+  }
+  // both sides have read both accumulators and (m, l) before either goes on
+  st.ok = st.ok && attn_wait_warp(sm, &sm.xfree, st.xph, p.status);
+  st.xph ^= 1;
+  tc_fence_after();
+  ++st.qn;
+}
+
+// ---- whole tiles of rows: a thread per row ----
+__device__ __forceinline__ float max32u(const uint32_t (&u)[32]) {
+  float v[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    v[q] = fmax3(__uint_as_float(u[8 * q]), __uint_as_float(u[8 * q + 1]), __uint_as_float(u[8 * q + 2]));
+    v[q] = fmax3(v[q], __uint_as_float(u[8 * q + 3]), __uint_as_float(u[8 * q + 4]));
+    v[q] = fmax3(v[q], __uint_as_float(u[8 * q + 5]), __uint_as_float(u[8 * q + 6]));
+    v[q] = fmaxf(v[q], __uint_as_float(u[8 * q + 7]));
+  }
+  return fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+}
+
 template <int D, bool kFp16>
-__device__ __forceinline__ void softmax_group(const PagedAttnParams& p, AttnSmem<D>& sm, uint32_t tmem, int x) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int r = (warp & 3) * 32 + lane;  // row of the side = TMEM lane
-  const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+__device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>& sm, uint32_t tmem, int x, const Entry& en,
+                                          SideState& st) {
+  const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
+  const int r = warp * 32 + lane;  // row of the side = TMEM lane
+  const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
   const uint32_t ts = tmem + lanes + s_col<D>(x);
   const float c = p.scale_log2;
   // half precision: the weights are kept 2^7 larger, clear of its subnormals (a lagging maximum adds 2^kRaise)
   constexpr float kUp = kFp16 ? 7.f : 0.f;
-  uint32_t sph = 0, oph = 0, xph = 0, wph = 0;
-  bool ok = true;
-  for (uint32_t e = 0; ok; ++e) {
-    const Entry en = take(p, sm, e);
-    if (en.rows == 0) break;
-    const int base = en.paired ? 0 : x * p.P * p.G;  // first row of the side in the unit
-    const int rows = min(en.rows - base, p.P * p.G);
-    const bool valid = r < rows;
-    const bool work = (warp & 3) * 32 < rows;  // the warp has rows
-    const int i = (base + r) / p.G;            // token of the row
-    const int t = en.pos0 + i;
-    const int lo = p.window > 0 ? t - p.window + 1 : 0;
-    // tiles [f0, f1) need no mask: every row of the side sees all of their keys
-    const int tok0 = base / p.G, tokn = (base + rows - 1) / p.G;
-    const int f1 = (en.pos0 + tok0 + 1) >> 7;
-    const int f0 = p.window > 0 ? (max(0, en.pos0 + tokn - p.window + 1) + 127) >> 7 : 0;
-    float m = -INFINITY, l = 0.f;
-    const int step = en.paired ? 2 : 1;
-    const int first = en.t0 + (en.paired ? x : 0);
-    for (int j = first; j < en.t1; j += step) {
-      ok = attn_wait_warp(sm, &sm.sfull[x], sph, p.status);
-      if (!ok) break;
-      sph ^= 1;
-      tc_fence_after();
-      if (work) {
-        uint32_t u[4][32];
-        tmem_ld64_async(ts, u[0], u[1]);
-        tmem_ld64_async(ts + 64, u[2], u[3]);
-        tmem_wait64(u[0], u[1]);
-        tmem_wait64(u[2], u[3]);
-        if (j < f0 || j >= f1) {
-          const int a = lo - j * kRows, b = t - j * kRows;  // the row sees keys a..b of the tile
-#pragma unroll
-          for (int q = 0; q < 128; ++q)
-            if (q < a || q > b) u[q >> 5][q & 31] = 0xff800000u;
-        }
-        float mx[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          float v = fmax3(__uint_as_float(u[q][0]), __uint_as_float(u[q][1]), __uint_as_float(u[q][2]));
-#pragma unroll
-          for (int k = 3; k < 31; k += 2) v = fmax3(v, __uint_as_float(u[q][k]), __uint_as_float(u[q][k + 1]));
-          mx[q] = fmaxf(v, __uint_as_float(u[q][31]));
-        }
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
-        if (j == first) {
-          m = top;
-        } else {
-          const bool raise = valid && top > m + kRaise;
-          if (__any_sync(0xffffffffu, raise)) {
-            // S of this tile is complete, so is O += P V of the side's tile before it, and the next waits for us
-            const float f = raise ? ex2_approx(m - top) : 1.f;
-            if (raise) { m = top; l *= f; }
-#pragma unroll 1
-            for (int q = 0; q < D; q += 32) {
-              uint32_t o[32];
-              tmem_ld32_async(tmem + lanes + o_col<D>(x) + q, o);
-              tmem_wait32(o);
-#pragma unroll
-              for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-              tmem_st32(tmem + lanes + o_col<D>(x) + q, o);
-            }
-          }
-        }
-        const float nb = (m == -INFINITY ? 0.f : -m) + kUp;
-        const float2 cc = make_float2(c, c), bb = make_float2(nb, nb);
-        float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-          uint32_t w[32];
-#pragma unroll
-          for (int q = 0; q < 32; ++q) {
-            const int k = hh * 64 + 2 * q;
-            const float2 y = ffma2(make_float2(__uint_as_float(u[k >> 5][k & 31]), __uint_as_float(u[k >> 5][(k & 31) + 1])), cc, bb);
-            const float2 z = make_float2(ex2_approx(y.x), ex2_approx(y.y));
-            acc[q & 3] = fadd2(acc[q & 3], z);
-            w[q] = pack2<kFp16>(z.x, z.y);
-          }
-          tmem_st32(ts + hh * 32, w);
-        }
-        const float2 sum = fadd2(fadd2(acc[0], acc[1]), fadd2(acc[2], acc[3]));
-        l += sum.x + sum.y;
-        tmem_wait_st();
-      }
-      tc_fence_before();
-      __syncwarp();
-      mbar_arrive_elect(&sm.pfull[x]);
-    }
-    if (!ok) break;
-    // ---- the rows' output ----
-    const bool any = first < en.t1;  // the side had a tile (side 1 of a paired unit's single tile has none)
-    if (any) {
-      ok = attn_wait_warp(sm, &sm.ofull[x], oph, p.status);
-      if (!ok) break;
-      oph ^= 1;
-      tc_fence_after();
-    }
-    // factors of the two accumulators, and the columns that this side writes
-    float f0x = 1.f, f1x = 0.f;
-    int col0 = 0, cols = D;
-    uint32_t o0 = o_col<D>(x), o1 = 0;
-    bool both = false;
-    if (en.paired) {
-      sm.ml[x][r] = make_float2(m, l);
-      tc_fence_before();
-      __syncwarp();
-      mbar_arrive_elect(&sm.xfull);
-      ok = attn_wait_warp(sm, &sm.xfull, xph, p.status);
-      if (!ok) break;
-      tc_fence_after();
-      const float2 a = sm.ml[0][r], b = sm.ml[1][r];
-      both = en.t0 + 1 < en.t1;
-      m = both ? fmaxf(a.x, b.x) : a.x;
-      const float bs = m == -INFINITY ? 0.f : m;
-      f0x = ex2_approx(a.x - bs);
-      f1x = both ? ex2_approx(b.x - bs) : 0.f;
-      l = a.y * f0x + (both ? b.y * f1x : 0.f);
-      o0 = o_col<D>(0);
-      o1 = o_col<D>(1);
-      cols = D / 2;
-      col0 = x * cols;
-    }
-    const bool whole = en.pieces == 1;
-    const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
-    f0x *= inv;
-    f1x *= inv;
-    const long long piece = 2 * blockIdx.x + (en.first == static_cast<int>(blockIdx.x) ? 1 : 0);
-    uint8_t* part = p.parts + (piece * 2 + x) * part_bytes<D>();
-    uint8_t* orow = p.out + static_cast<long long>(en.tok0 + i) * p.out_token +
-                    static_cast<long long>(en.h * p.G + (base + r) - i * p.G) * p.out_head;
+  const bool paired = en.kind == kPaired;
+  const int base = paired ? 0 : x * p.P * p.G;  // first row of the side in the unit
+  const int rows = min(en.rows - base, p.P * p.G);
+  const bool valid = r < rows;
+  const bool work = warp * 32 < rows;  // the warp has rows
+  const int i = (base + r) / p.G;      // token of the row
+  const int t = en.pos0 + i;
+  const int lo = p.window > 0 ? t - p.window + 1 : 0;
+  // tiles [f0, f1) need no mask: every row of the side sees all of their keys
+  const int tok0 = base / p.G, tokn = (base + rows - 1) / p.G;
+  const int f1 = (en.pos0 + tok0 + 1) >> 7;
+  const int f0 = p.window > 0 ? (max(0, en.pos0 + tokn - p.window + 1) + 127) >> 7 : 0;
+  float m = -INFINITY, l = 0.f;
+  const int step = paired ? 2 : 1;
+  const int first = en.t0 + (paired ? x : 0);
+  for (int j = first; j < en.t1; j += step) {
+    st.ok = st.ok && attn_wait_warp(sm, &sm.sfull[x], st.sph, p.status);
+    st.sph ^= 1;
+    tc_fence_after();
     if (work) {
+      uint32_t u[4][32];
+      tmem_ld64_async(ts, u[0], u[1]);
+      tmem_wait64(u[0], u[1]);
+      tmem_ld64_async(ts + 64, u[2], u[3]);
+      float mx[4];
+      if (j >= f0 && j < f1) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) mx[q] = max32u(u[q]);
+      }
+      tmem_wait64(u[2], u[3]);
+      if (j < f0 || j >= f1) {
+        const int a = lo - j * kRows, b = t - j * kRows;  // the row sees keys a..b of the tile
+#pragma unroll
+        for (int q = 0; q < 128; ++q)
+          if (q < a || q > b) u[q >> 5][q & 31] = 0xff800000u;
+      }
+      if (j < f0 || j >= f1) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) mx[q] = max32u(u[q]);
+      }
+#pragma unroll
+      for (int q = 2; q < 4; ++q) mx[q] = max32u(u[q]);
+      const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+      if (j == first) {
+        m = top;
+      } else {
+        const bool raise = valid && top > m + kRaise;
+        if (__any_sync(0xffffffffu, raise)) {
+          // S of this tile is complete, so is O += P V of the side's tile before it, and the next waits for us
+          const float f = raise ? ex2_approx(m - top) : 1.f;
+          if (raise) { m = top; l *= f; }
 #pragma unroll 1
-      for (int q = col0; q < col0 + cols; q += 32) {
-        uint32_t o[32];
-        float v[32];
-        tmem_ld32_async(tmem + lanes + o0 + q, o);
+          for (int q = 0; q < D; q += 32) {
+            uint32_t o[32];
+            tmem_ld32_async(tmem + lanes + o_col<D>(x) + q, o);
+            tmem_wait32(o);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+            tmem_st32(tmem + lanes + o_col<D>(x) + q, o);
+          }
+        }
+      }
+      const float nb = kUp - finite_or_0(m);
+      const float2 cc = make_float2(c, c), bb = make_float2(nb, nb);
+      float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+      mend_v<D>(p, sm, en, j, st);
+#pragma unroll
+      for (int hh = 0; hh < 4; ++hh) {
+        uint32_t w[16];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          const int k = 2 * q;
+          const float2 y = ffma2(make_float2(__uint_as_float(u[hh][k]), __uint_as_float(u[hh][k + 1])), cc, bb);
+          const float2 z = make_float2(ex2_approx(y.x), ex2_approx(y.y));
+          acc[q & 3] = fadd2(acc[q & 3], z);
+          w[q] = pack2<kFp16>(z.x, z.y);
+        }
+        tmem_st_cols<16>(ts + hh * 16, w);
+        if ((hh + 1) % (4 / kParts) == 0) {
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          mbar_arrive_elect(&sm.pfull[x][(hh + 1) / (4 / kParts) - 1]);
+        }
+      }
+      const float2 sum = fadd2(fadd2(acc[0], acc[1]), fadd2(acc[2], acc[3]));
+      l += sum.x + sum.y;
+    } else {
+      mend_v<D>(p, sm, en, j, st);
+      tc_fence_before();
+      __syncwarp();
+#pragma unroll
+      for (int part = 0; part < kParts; ++part) mbar_arrive_elect(&sm.pfull[x][part]);
+    }
+  }
+  // ---- the rows' output ----
+  if (first < en.t1) {  // (side 1 of a paired unit's single tile has no accumulator)
+    st.ok = st.ok && attn_wait_warp(sm, &sm.ofull[x], st.oph, p.status);
+    st.oph ^= 1;
+    tc_fence_after();
+  }
+  // factors of the accumulators, and the columns that this side writes
+  float fa = 1.f, fb = 0.f;
+  int col0 = 0, cols = D;
+  uint32_t oa = o_col<D>(x);
+  bool both = false;
+  if (paired) {
+    sm.ml[x][r] = make_float2(m, l);
+    tc_fence_before();
+    __syncwarp();
+    mbar_arrive_elect(&sm.xfull);
+    st.ok = st.ok && attn_wait_warp(sm, &sm.xfull, st.xph, p.status);
+    tc_fence_after();
+    both = en.t0 + 1 < en.t1;
+    const float2 a = sm.ml[0][r], b = both ? sm.ml[1][r] : make_float2(-INFINITY, 0.f);
+    m = fmaxf(a.x, b.x);
+    fa = ex2_approx(a.x - finite_or_0(m));
+    fb = ex2_approx(b.x - finite_or_0(m));
+    l = fmaf(a.y, fa, b.y * fb);
+    oa = o_col<D>(0);
+    cols = D / 2;
+    col0 = x * cols;
+  }
+  const bool whole = en.pieces == 1;
+  const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
+  fa *= inv;
+  fb *= inv;
+  const Records<D> mine = records<D>(p, blockIdx.x, en.first == static_cast<int>(blockIdx.x), x);
+  const int head = en.h * p.G + base + r - i * p.G;
+  uint8_t* orow = p.out + static_cast<long long>(en.tok0 + i) * p.out_token + static_cast<long long>(head) * p.out_head;
+  if (work) {
+#pragma unroll 1
+    for (int q = col0; q < col0 + cols; q += 32) {
+      uint32_t o[32];
+      float v[32];
+      tmem_ld32_async(tmem + lanes + oa + q, o);
+      tmem_wait32(o);
+#pragma unroll
+      for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(o[k]) * fa;
+      if (both) {
+        tmem_ld32_async(tmem + lanes + o_col<D>(1) + q, o);
         tmem_wait32(o);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(o[k]) * f0x;
-        if (both) {
-          tmem_ld32_async(tmem + lanes + o1 + q, o);
-          tmem_wait32(o);
+        for (int k = 0; k < 32; ++k) v[k] = fmaf(__uint_as_float(o[k]), fb, v[k]);
+      }
+      if (l == 0.f) {  // no key (or none with a weight): nothing to weigh
 #pragma unroll
-          for (int k = 0; k < 32; ++k) v[k] = fmaf(__uint_as_float(o[k]), f1x, v[k]);
-        }
-        if (l == 0.f) {  // no key (or none above the type's range): nothing to weigh
+        for (int k = 0; k < 32; ++k) v[k] = 0.f;
+      }
+      if (valid) {
+        if (whole) {
 #pragma unroll
-          for (int k = 0; k < 32; ++k) v[k] = 0.f;
-        }
-        if (valid) {
-          if (whole) {
-#pragma unroll
-            for (int k = 0; k < 32; k += 8) {
-              uint4 w;
-              w.x = pack2<kFp16>(v[k], v[k + 1]);
-              w.y = pack2<kFp16>(v[k + 2], v[k + 3]);
-              w.z = pack2<kFp16>(v[k + 4], v[k + 5]);
-              w.w = pack2<kFp16>(v[k + 6], v[k + 7]);
-              *reinterpret_cast<uint4*>(orow + (q + k) * 2) = w;
-            }
-          } else {
-#pragma unroll
-            for (int k = 0; k < 32; k += 4)
-              __stcg(reinterpret_cast<float4*>(part) + ((q - col0 + k) / 4) * kRows + r, make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]));
+          for (int k = 0; k < 32; k += 8) {
+            uint4 w;
+            w.x = pack2<kFp16>(v[k], v[k + 1]);
+            w.y = pack2<kFp16>(v[k + 2], v[k + 3]);
+            w.z = pack2<kFp16>(v[k + 4], v[k + 5]);
+            w.w = pack2<kFp16>(v[k + 6], v[k + 7]);
+            *reinterpret_cast<uint4*>(orow + (q + k) * 2) = w;
           }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 32; k += 4)
+            __stcg(reinterpret_cast<float4*>(mine.at) + ((q - col0 + k) / 4) * kRows + r, make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]));
         }
       }
     }
-    if (en.paired) {  // both sides have read both accumulators before either is written again
-      tc_fence_before();
-      __syncwarp();
-      mbar_arrive_elect(&sm.xfree);
-    }
-    constexpr float kLn2 = 0.6931471805599453f;
-    if (whole) {
-      if (p.lse && valid && (!en.paired || x == 0))
-        p.lse[static_cast<long long>(en.tok0 + i) * p.H_q + en.h * p.G + (base + r) - i * p.G] =
-            l > 0.f ? (m - kUp + lg2_approx(l)) * kLn2 : (l == 0.f ? -INFINITY : l);
-    } else {
-      float2* mlp = reinterpret_cast<float2*>(part + kRows * D * 4);
-      if (valid) __stcg(mlp + r, make_float2(m, l));
-      __threadfence();
-      __syncwarp();
-      mbar_arrive_elect(&sm.wrote[x]);
-      ok = attn_wait_warp(sm, &sm.wrote[x], wph, p.status);
-      if (!ok) break;
-      if ((warp & 3) == 0 && lane == 0) {
-        __threadfence();
-        int* cnt = p.sync + 2 * en.first + x;
-        const int n = atomicAdd(cnt, 1);
-        sm.last[x] = n == en.pieces - 1;
-        if (n == en.pieces - 1) atomicExch(cnt, 0);
-        __threadfence();
-        mbar_arrive(&sm.told[x]);
-      }
-      __syncwarp();
-      ok = attn_wait_warp(sm, &sm.told[x], wph, p.status);
-      wph ^= 1;
-      if (!ok) break;
-      if (sm.last[x] && rows > 0) {
-        // merge: record i of the unit is CTA first + i's; a row's factors first, then (row, 4 columns) per thread
-        auto rec = [&](int q) {
-          const long long cta = en.first + q;
-          return p.parts + ((2 * cta + (q == 0 ? 1 : 0)) * 2 + x) * part_bytes<D>();
-        };
-        const int tid = (warp & 3) * 32 + lane;
-        const int items = rows * (cols / 4);
-        for (int it = tid; it < items; it += 128) {
-          const int c4 = it / rows, rr = it - c4 * rows;
-          float mm = -INFINITY, ll = 0.f;
-          float4 acc4 = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int q0 = 0; q0 < en.pieces; q0 += 4) {
-            float2 z[4];
-            float4 v[4];
+  }
+  if (paired) {
+    tc_fence_before();
+    __syncwarp();
+    mbar_arrive_elect(&sm.xfree);
+  }
+  if (whole) {
+    if (p.lse && valid && (!paired || x == 0)) p.lse[static_cast<long long>(en.tok0 + i) * p.H_q + head] = lse_of(m - kUp, l);
+  } else {
+    if (valid) __stcg(mine.ml() + r, make_float2(m, l));
+    if (arrived_last(p, sm, en, x, st.ok)) {
+      // merge the unit's records in order, four columns of a row per thread
+      const int items = rows * (cols / 4);
+      for (int it = r; it < items; it += 128) {
+        const int c4 = it / rows, rr = it - c4 * rows;
+        float mm = -INFINITY, ll = 0.f;
+        float4 oo = make_float4(0.f, 0.f, 0.f, 0.f);
+        constexpr int kU = 4;
+        for (int q0 = 0; q0 < en.pieces; q0 += kU) {
+          float2 z[kU];
+          float4 v[kU];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              if (q0 + q < en.pieces) {
-                const uint8_t* rc = rec(q0 + q);
-                z[q] = __ldcg(reinterpret_cast<const float2*>(rc + kRows * D * 4) + rr);
-                v[q] = __ldcg(reinterpret_cast<const float4*>(rc) + c4 * kRows + rr);
-              } else {
-                z[q] = make_float2(-INFINITY, 0.f);
-                v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
-              }
+          for (int q = 0; q < kU; ++q) {
+            z[q] = make_float2(-INFINITY, 0.f);
+            v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (q0 + q < en.pieces) {
+              const Records<D> rec = records<D>(p, en.first + q0 + q, q0 + q == 0, x);
+              z[q] = __ldcg(rec.ml() + rr);
+              v[q] = __ldcg(reinterpret_cast<const float4*>(rec.at) + c4 * kRows + rr);
             }
-            const float mn = fmaxf(fmaxf(fmaxf(z[0].x, z[1].x), fmaxf(z[2].x, z[3].x)), mm);
-            const float bs = mn == -INFINITY ? 0.f : mn;
-            float f = ex2_approx(mm - bs);
-            ll *= f;
-            acc4.x *= f; acc4.y *= f; acc4.z *= f; acc4.w *= f;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              f = ex2_approx(z[q].x - bs);
-              ll = fmaf(z[q].y, f, ll);
-              acc4.x = fmaf(v[q].x, f, acc4.x);
-              acc4.y = fmaf(v[q].y, f, acc4.y);
-              acc4.z = fmaf(v[q].z, f, acc4.z);
-              acc4.w = fmaf(v[q].w, f, acc4.w);
-            }
-            mm = mn;
           }
-          const float iv = ll > 0.f ? 1.f / ll : (ll == 0.f ? 0.f : ll);
-          const int ii = (base + rr) / p.G;
-          const int head = en.h * p.G + base + rr - ii * p.G;
-          uint2 w;
-          w.x = pack2<kFp16>(acc4.x * iv, acc4.y * iv);
-          w.y = pack2<kFp16>(acc4.z * iv, acc4.w * iv);
-          *reinterpret_cast<uint2*>(p.out + static_cast<long long>(en.tok0 + ii) * p.out_token +
-                                    static_cast<long long>(head) * p.out_head + (col0 + c4 * 4) * 2) = w;
-          if (p.lse && c4 == 0 && (!en.paired || x == 0))
-            p.lse[static_cast<long long>(en.tok0 + ii) * p.H_q + head] =
-                ll > 0.f ? (mm - kUp + lg2_approx(ll)) * kLn2 : (ll == 0.f ? -INFINITY : ll);
+          float mn = mm;
+#pragma unroll
+          for (int q = 0; q < kU; ++q) mn = fmaxf(mn, z[q].x);
+          const float bs = finite_or_0(mn);
+          float f = ex2_approx(mm - bs);
+          ll *= f;
+          oo.x *= f; oo.y *= f; oo.z *= f; oo.w *= f;
+#pragma unroll
+          for (int q = 0; q < kU; ++q) {
+            f = ex2_approx(z[q].x - bs);
+            ll = fmaf(z[q].y, f, ll);
+            oo.x = fmaf(v[q].x, f, oo.x);
+            oo.y = fmaf(v[q].y, f, oo.y);
+            oo.z = fmaf(v[q].z, f, oo.z);
+            oo.w = fmaf(v[q].w, f, oo.w);
+          }
+          mm = mn;
         }
+        const float iv = ll == 0.f ? 0.f : 1.f / ll;
+        const int ii = (base + rr) / p.G, hd = en.h * p.G + base + rr - ii * p.G;
+        const uint2 w = make_uint2(pack2<kFp16>(oo.x * iv, oo.y * iv), pack2<kFp16>(oo.z * iv, oo.w * iv));
+        *reinterpret_cast<uint2*>(p.out + static_cast<long long>(en.tok0 + ii) * p.out_token +
+                                  static_cast<long long>(hd) * p.out_head + (col0 + c4 * 4) * 2) = w;
+        if (p.lse && c4 == 0 && (!paired || x == 0))
+          p.lse[static_cast<long long>(en.tok0 + ii) * p.H_q + hd] = lse_of(mm - kUp, ll);
       }
     }
-    if (en.paired) {
-      ok = attn_wait_warp(sm, &sm.xfree, xph, p.status);
-      xph ^= 1;
-      tc_fence_after();
-    }
+  }
+  if (paired) {  // both sides have read both accumulators and (m, l) before either goes on
+    st.ok = st.ok && attn_wait_warp(sm, &sm.xfree, st.xph, p.status);
+    st.xph ^= 1;
+    tc_fence_after();
+  }
+  st.qn += paired ? 1 : 2;
+}
+
+template <int D, bool kFp16>
+__device__ __forceinline__ void softmax_group(const PagedAttnParams& p, AttnSmem<D>& sm, uint32_t tmem, int x) {
+  SideState st;
+  for (uint32_t e = 0;; ++e) {
+    const Entry en = take(p, sm, e);
+    if (group_any(x, en.rows == 0)) break;  // no more, or a warp's wait for the entry ran out
+    if (en.kind != kFew) row_tiles<D, kFp16>(p, sm, tmem, x, en, st);
+    else if (en.rows <= 4) few_rows<D, kFp16, 4>(p, sm, tmem, x, en, st);
+    else if (en.rows <= 8) few_rows<D, kFp16, 8>(p, sm, tmem, x, en, st);
+    else few_rows<D, kFp16, 16>(p, sm, tmem, x, en, st);
+    st.tiles += 2 * (en.t1 - en.t0);
   }
 }
 
@@ -863,16 +1238,14 @@ __global__ void __launch_bounds__(kAttnThreads, 1) paged_attn_kernel(const __gri
     return;
   }
   S& sm = *reinterpret_cast<S*>(smem_raw);
-  const int warp = threadIdx.x >> 5;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sm.qfull[i], 1);
       mbar_init(&sm.qempty[i], 1);
       mbar_init(&sm.sfull[i], 1);
-      mbar_init(&sm.pfull[i], 4);
+      for (int j = 0; j < kParts; ++j) mbar_init(&sm.pfull[i][j], 4);
       mbar_init(&sm.ofull[i], 1);
-      mbar_init(&sm.wrote[i], 4);
-      mbar_init(&sm.told[i], 1);
     }
     for (int i = 0; i < S::kStages; ++i) {
       mbar_init(&sm.full[i], 1);
@@ -905,6 +1278,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) paged_attn_kernel(const __gri
     if (warp == 0) load_warp<D>(p, sm);
     if (warp == 1) mma_warp<D, kFp16>(p, sm, tmem);
     if (warp == 2) deal(p, sm, sh);
+    __syncwarp();
   } else {
     regs_alloc<kRegsAttnSoftmax>();
     softmax_group<D, kFp16>(p, sm, tmem, (warp - 4) >> 2);
