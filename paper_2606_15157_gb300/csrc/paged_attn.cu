@@ -134,6 +134,22 @@ __device__ __forceinline__ void attn_drain(uint64_t* bar, uint32_t parity) {
 // ---- PTX ------------------------------------------------------------------------
 
 // From a whole converged warp; the operands are the same in every lane.
+__device__ __forceinline__ void mbar_expect_elect(uint64_t* bar, uint32_t bytes) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(smem_u32(bar)), "r"(bytes)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_elect(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "@e cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];\n\t}" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
 __device__ __forceinline__ void tma_load_4d_elect(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w,
                                                   uint32_t bar) {
   asm volatile(
@@ -442,6 +458,10 @@ __device__ __forceinline__ Entry take(const PagedAttnParams& p, S& sm, uint32_t 
   return en;
 }
 
+// A value that is the same in every lane, broadcast, so that the compiler knows it to be: what
+// depends on it is one path for the warp, with operands in uniform registers.
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+
 // ---- warp 0: loads -------------------------------------------------------------------
 // Order of an entry's tiles in the ring: A K tiles ahead of V (A = 1 for a full unit;
 // 2 for the others, whose sides work on two tiles at once).
@@ -449,67 +469,77 @@ template <int D>
 __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>& sm) {
   using S = AttnSmem<D>;
   const int lane = threadIdx.x & 31;
-  const int box_shift = min(p.page_shift, 7);           // rows of a page box
-  const int boxes = kRows >> box_shift;                 // page boxes of a tile
-  uint32_t st = 0, ph = 0, qs = 0, qn = 0, issued = 0;
+  const int box_shift = min(p.page_shift, 7);  // rows of a page box
+  const int boxes = kRows >> box_shift;        // page boxes of a tile
+  uint32_t st = 0, ph = 0, qn = 0, issued = 0;
   bool ok = true;
   for (uint32_t e = 0; ok; ++e) {
     const Entry en = take(p, sm, e);
-    if (en.rows == 0) break;
+    if (uniform(en.rows) == 0) break;
+    const int kind = uniform(en.kind), h = uniform(en.h), t0 = uniform(en.t0), t1 = uniform(en.t1);
+    const int tok0 = uniform(en.tok0), klo = uniform(en.klo), khi = uniform(en.khi);
+    const bool one = uniform(en.rows) == p.G;
     // ---- Q tiles ----
-    const int sides = en.kind == kFull ? 2 : 1;
+    const int sides = kind == kFull ? 2 : 1;
     for (int x = 0; ok && x < sides; ++x) {
-      if (!attn_wait_warp(sm, &sm.qempty[qs], ((qn >> 1) & 1) ^ 1, p.status)) { ok = false; break; }
-      const bool one = en.rows == p.G;
-      const uint32_t bytes = static_cast<uint32_t>(p.G) * (one ? 1 : p.P) * D * 2;
-      if (lane == 0) {
-        mbar_expect_tx(&sm.qfull[qs], bytes);
+      const uint32_t qs = qn & 1;
+      ok = attn_wait_warp(sm, &sm.qempty[qs], ((qn >> 1) & 1) ^ 1, p.status);
+      if (!ok) break;
+      mbar_expect_elect(&sm.qfull[qs], static_cast<uint32_t>(p.G) * (one ? 1 : p.P) * D * 2);
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c)
-          tma_load_3d(sm.q[qs] + c * (kRows * 128), one ? &p.qmap1 : &p.qmap, c * 64, en.h * p.G, en.tok0 + x * p.P,
-                      &sm.qfull[qs]);
-      }
-      __syncwarp();
+      for (int c = 0; c < D / 64; ++c)
+        tma_load_3d_elect(smem_u32(sm.q[qs]) + c * (kRows * 128), one ? &p.qmap1 : &p.qmap, c * 64, h * p.G, tok0 + x * p.P,
+                          smem_u32(&sm.qfull[qs]));
       ++qn;
-      qs ^= 1;
     }
     // ---- pages ----
-    // the page of box `lane` of tile t (its number; num_pages = zeros)
-    const int* row = p.table + static_cast<long long>(en.s) * p.max_pages;
+    // lane i holds the page of the tile's box i: its entry of the table, read three tiles ahead and checked when used
+    const int* row = p.table + static_cast<long long>(uniform(en.s)) * p.max_pages;
     auto page_of = [&](int t) {
       const int k = t * kRows + (lane << box_shift);
-      if (t >= en.t1 || lane >= boxes || k >= en.khi || k + (1 << box_shift) <= en.klo) return p.num_pages;
-      const int id = __ldg(row + (k >> p.page_shift));
+      return t < t1 && lane < boxes && k < khi && k + (1 << box_shift) > klo ? __ldg(row + (k >> p.page_shift)) : INT_MAX;
+    };
+    auto checked = [&](int id) {  // num_pages (loads zeros) for no page or one outside the pool
       if (static_cast<unsigned>(id) < static_cast<unsigned>(p.num_pages)) return id;
-      atomicOr(p.status, kStatusDevice);
+      if (id != INT_MAX) atomicOr(p.status, kStatusDevice);
       return p.num_pages;
     };
     auto load = [&](const CUtensorMap* map, int t, int page) {
-      if (!attn_wait_warp(sm, &sm.empty[st], ph ^ 1, p.status)) { ok = false; return; }
-      if (lane == 0) mbar_expect_tx(&sm.full[st], S::kTileBytes);
-      __syncwarp();
-      const int y = (t * kRows) & ((1 << p.page_shift) - 1);  // a page is whole boxes, or a box whole pages
+      ok = ok && attn_wait_warp(sm, &sm.empty[st], ph ^ 1, p.status);
+      if (!ok) return;
       const uint32_t dst = smem_u32(sm.kv[st]), bar = smem_u32(&sm.full[st]);
-#pragma unroll 2
-      for (int i = 0; i < boxes; ++i) {
-        const int pg = __shfl_sync(0xffffffffu, page, i);
+      mbar_expect_elect(&sm.full[st], S::kTileBytes);
+      const int y = (t * kRows) & ((1 << p.page_shift) - 1);  // a page is whole boxes, or a box whole pages
+      if (boxes == 1) {
 #pragma unroll
         for (int c = 0; c < D / 64; ++c)
-          tma_load_4d_elect(dst + c * (kRows * 128) + (i << (box_shift + 7)), map, c * 64, y, en.h, pg, bar);
+          tma_load_4d_elect(dst + c * (kRows * 128), map, c * 64, y, h, uniform(page), bar);
+      } else {
+        for (int i = 0; i < boxes; i += 2) {  // an even number of them
+          const int pa = __shfl_sync(0xffffffffu, page, i), pb = __shfl_sync(0xffffffffu, page, i + 1);
+#pragma unroll
+          for (int c = 0; c < D / 64; ++c) {
+            const uint32_t at = dst + c * (kRows * 128) + (i << (box_shift + 7));
+            tma_load_4d_elect(at, map, c * 64, y, h, pa, bar);
+            tma_load_4d_elect(at + (1 << (box_shift + 7)), map, c * 64, y, h, pb, bar);
+          }
+        }
       }
       ++issued;
       if (++st == S::kStages) { st = 0; ph ^= 1; }
     };
-    const int A = en.kind == kFull ? 1 : 2;
-    int p0 = page_of(en.t0), p1 = page_of(en.t0 + 1), p2 = page_of(en.t0 + 2);  // of tiles t, t + 1, t + 2
-    for (int a = 0; ok && a < A && en.t0 + a < en.t1; ++a) load(&p.kmap, en.t0 + a, a == 0 ? p0 : p1);
-    for (int t = en.t0; ok && t < en.t1; ++t) {
-      const int next = page_of(t + 3);
+    const int A = kind == kFull ? 1 : 2;
+    int r0 = page_of(t0), r1 = page_of(t0 + 1), r2 = page_of(t0 + 2);
+    int p0 = checked(r0), p1 = checked(r1);  // pages of tiles t, t + 1
+    for (int a = 0; a < A && t0 + a < t1; ++a) load(&p.kmap, t0 + a, a == 0 ? p0 : p1);
+    for (int t = t0; ok && t < t1; ++t) {
+      const int r3 = page_of(t + 3);
+      const int p2 = checked(r2);
       load(&p.vmap, t, p0);
-      if (ok && t + A < en.t1) load(&p.kmap, t + A, A == 1 ? p1 : p2);
+      if (t + A < t1) load(&p.kmap, t + A, A == 1 ? p1 : p2);
       p0 = p1;
       p1 = p2;
-      p2 = next;
+      r2 = r3;
     }
   }
   // After an abort, wait (bounded) for the copies still landing before the CTA retires.
@@ -532,8 +562,6 @@ template <int D>
 __device__ __forceinline__ uint32_t s_col(int side) { return side * 128; }
 template <int D>
 __device__ __forceinline__ uint32_t o_col(int side) { return 256 + side * 128; }
-
-__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 
 // One warp issues every MMA: the sides' products run in turn, whole (issued by a thread
 // for each side they interleave, and either side waits twice as long for its own).  What
