@@ -49,7 +49,7 @@ __host__ __device__ constexpr int tile_cost(int kind) { return kind == kFull ? 2
 __host__ __device__ constexpr int unit_cost(int kind) { return kind == kFull ? 1 : 1; }
 constexpr int kMinShare = 2;        // least cost of a share, a tile's or more: no piece of a cut unit is empty
 constexpr int kRows = 128;          // rows of a side
-constexpr int kParts = 2;           // parts of a tile's weights that the second product takes as they come
+constexpr int kParts = 2;           // halves of a tile's weights, which the second product takes as they come
 constexpr float kRaise = 8.f;       // a row's maximum is raised when a tile's is this much (log2) above it
 constexpr uint64_t kAttnWaitNs = 2000000000ull;
 
@@ -987,6 +987,48 @@ __device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D>& 
 }
 
 // ---- whole tiles of rows: a thread per row ----
+
+// Keys [a, b] of 32 stay, the others' logits become -inf.
+__device__ __forceinline__ void mask_keys(uint32_t (&u)[32], int a, int b) {
+  const uint32_t from = a <= 0 ? ~0u : a > 31 ? 0u : ~0u << a;
+  const uint32_t to = b < 0 ? 0u : b >= 31 ? ~0u : (2u << b) - 1;
+  const uint32_t keep = from & to;
+#pragma unroll
+  for (int q = 0; q < 32; ++q)
+    if (!(keep & (1u << q))) u[q] = 0xff800000u;
+}
+
+// Four lanes' four values each, transposed: lane q gets the q-th value of lane k as w[k].
+__device__ __forceinline__ void transpose4(uint4 (&w)[4], int q) {
+  auto swap = [&](uint4& a, uint4& b, bool up, int d) {  // lanes with `up` give a and take it back as theirs, the others b
+    uint4 s = up ? a : b;
+    s.x = __shfl_xor_sync(0xffffffffu, s.x, d);
+    s.y = __shfl_xor_sync(0xffffffffu, s.y, d);
+    s.z = __shfl_xor_sync(0xffffffffu, s.z, d);
+    s.w = __shfl_xor_sync(0xffffffffu, s.w, d);
+    (up ? a : b) = s;
+  };
+  swap(w[0], w[1], q & 1, 1);
+  swap(w[2], w[3], q & 1, 1);
+  swap(w[0], w[2], q & 2, 2);
+  swap(w[1], w[3], q & 2, 2);
+}
+
+// Weights exp2(c u + nb) of 64 keys as 16-bit pairs, and their sums before rounding.
+template <bool kFp16>
+__device__ __forceinline__ void weights(const uint32_t (&u0)[32], const uint32_t (&u1)[32], float c, float nb, uint32_t (&w)[32],
+                                        float2 (&acc)[4]) {
+  const float2 cc = make_float2(c, c), bb = make_float2(nb, nb);
+#pragma unroll
+  for (int q = 0; q < 32; ++q) {
+    const uint32_t a = q < 16 ? u0[2 * q] : u1[2 * q - 32], b = q < 16 ? u0[2 * q + 1] : u1[2 * q - 31];
+    const float2 y = ffma2(make_float2(__uint_as_float(a), __uint_as_float(b)), cc, bb);
+    const float2 z = make_float2(ex2_approx(y.x), ex2_approx(y.y));
+    acc[q & 3] = fadd2(acc[q & 3], z);
+    w[q] = pack2<kFp16>(z.x, z.y);
+  }
+}
+
 __device__ __forceinline__ float max32u(const uint32_t (&u)[32]) {
   float v[4];
 #pragma unroll
@@ -1033,69 +1075,55 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
       tmem_ld64_async(ts, u[0], u[1]);
       tmem_wait64(u[0], u[1]);
       tmem_ld64_async(ts + 64, u[2], u[3]);
-      float mx[4];
-      if (j >= f0 && j < f1) {
+      const bool edge = j < f0 || j >= f1;
+      if (edge) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q) mx[q] = max32u(u[q]);
+        for (int q = 0; q < 2; ++q) mask_keys(u[q], lo - j * kRows - 32 * q, t - j * kRows - 32 * q);
       }
+      float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+      // the first half's weights by the maximum so far, while the tile's is being formed
+      uint32_t w[32];
+      weights<kFp16>(u[0], u[1], c, kUp - finite_or_0(m), w, acc);
+      float top = fmaxf(max32u(u[0]), max32u(u[1]));
       tmem_wait64(u[2], u[3]);
-      if (j < f0 || j >= f1) {
-        const int a = lo - j * kRows, b = t - j * kRows;  // the row sees keys a..b of the tile
+      if (edge) {
 #pragma unroll
-        for (int q = 0; q < 128; ++q)
-          if (q < a || q > b) u[q >> 5][q & 31] = 0xff800000u;
+        for (int q = 2; q < 4; ++q) mask_keys(u[q], lo - j * kRows - 32 * q, t - j * kRows - 32 * q);
       }
-      if (j < f0 || j >= f1) {
-#pragma unroll
-        for (int q = 0; q < 2; ++q) mx[q] = max32u(u[q]);
-      }
-#pragma unroll
-      for (int q = 2; q < 4; ++q) mx[q] = max32u(u[q]);
-      const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
-      if (j == first) {
-        m = top;
-      } else {
-        const bool raise = valid && top > m + kRaise;
-        if (__any_sync(0xffffffffu, raise)) {
+      top = fmaxf(top, fmaxf(max32u(u[2]), max32u(u[3]))) * c;
+      const bool raise = valid && (j == first || top > m + kRaise);
+      if (__any_sync(0xffffffffu, raise)) {
+        const float f = raise ? ex2_approx(m - finite_or_0(top)) : 1.f;
+        if (raise) { m = top; l *= f; }
+        if (j != first) {
           // S of this tile is complete, so is O += P V of the side's tile before it, and the next waits for us
-          const float f = raise ? ex2_approx(m - top) : 1.f;
-          if (raise) { m = top; l *= f; }
 #pragma unroll 1
-          for (int q = 0; q < D; q += 32) {
-            uint32_t o[32];
-            tmem_ld32_async(tmem + lanes + o_col<D>(x) + q, o);
-            tmem_wait32(o);
+          for (int q = 0; q < D; q += 16) {
+            uint32_t o[16];
+            tmem_ld_cols<16>(tmem + lanes + o_col<D>(x) + q, o);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-            tmem_st32(tmem + lanes + o_col<D>(x) + q, o);
+            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+            tmem_st_cols<16>(tmem + lanes + o_col<D>(x) + q, o);
           }
         }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[q] = make_float2(0.f, 0.f);
+        weights<kFp16>(u[0], u[1], c, kUp - finite_or_0(m), w, acc);
       }
-      const float nb = kUp - finite_or_0(m);
-      const float2 cc = make_float2(c, c), bb = make_float2(nb, nb);
-      float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
       mend_v<D>(p, sm, en, j, st);
-#pragma unroll
-      for (int hh = 0; hh < 4; ++hh) {
-        uint32_t w[16];
-#pragma unroll
-        for (int q = 0; q < 16; ++q) {
-          const int k = 2 * q;
-          const float2 y = ffma2(make_float2(__uint_as_float(u[hh][k]), __uint_as_float(u[hh][k + 1])), cc, bb);
-          const float2 z = make_float2(ex2_approx(y.x), ex2_approx(y.y));
-          acc[q & 3] = fadd2(acc[q & 3], z);
-          w[q] = pack2<kFp16>(z.x, z.y);
-        }
-        tmem_st_cols<16>(ts + hh * 16, w);
-        if ((hh + 1) % (4 / kParts) == 0) {
-          tmem_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          mbar_arrive_elect(&sm.pfull[x][(hh + 1) / (4 / kParts) - 1]);
-        }
-      }
+      tmem_st32(ts, w);
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      mbar_arrive_elect(&sm.pfull[x][0]);
+      weights<kFp16>(u[2], u[3], c, kUp - finite_or_0(m), w, acc);
+      tmem_st32(ts + 32, w);
       const float2 sum = fadd2(fadd2(acc[0], acc[1]), fadd2(acc[2], acc[3]));
       l += sum.x + sum.y;
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      mbar_arrive_elect(&sm.pfull[x][1]);
     } else {
       mend_v<D>(p, sm, en, j, st);
       tc_fence_before();
@@ -1138,8 +1166,16 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
   fb *= inv;
   const Records<D> mine = records<D>(p, blockIdx.x, en.first == static_cast<int>(blockIdx.x), x);
   const int head = en.h * p.G + base + r - i * p.G;
-  uint8_t* orow = p.out + static_cast<long long>(en.tok0 + i) * p.out_token + static_cast<long long>(head) * p.out_head;
   if (work) {
+    // a warp's stores go row by row in groups of four lanes: lane q of a group writes the q-th 16 bytes of
+    // 64 of each of its four rows in turn
+    const int q4 = lane & 3;
+    long long at[4];  // of the group's rows; -1: no row
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const long long mine4 = valid ? static_cast<long long>(en.tok0 + i) * p.out_token + static_cast<long long>(head) * p.out_head : -1;
+      at[k] = __shfl_sync(0xffffffffu, mine4, (lane & 28) + k);
+    }
 #pragma unroll 1
     for (int q = col0; q < col0 + cols; q += 32) {
       uint32_t o[32];
@@ -1158,22 +1194,23 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
 #pragma unroll
         for (int k = 0; k < 32; ++k) v[k] = 0.f;
       }
-      if (valid) {
-        if (whole) {
+      if (whole) {
+        uint4 w[4];
 #pragma unroll
-          for (int k = 0; k < 32; k += 8) {
-            uint4 w;
-            w.x = pack2<kFp16>(v[k], v[k + 1]);
-            w.y = pack2<kFp16>(v[k + 2], v[k + 3]);
-            w.z = pack2<kFp16>(v[k + 4], v[k + 5]);
-            w.w = pack2<kFp16>(v[k + 6], v[k + 7]);
-            *reinterpret_cast<uint4*>(orow + (q + k) * 2) = w;
-          }
-        } else {
-#pragma unroll
-          for (int k = 0; k < 32; k += 4)
-            __stcg(reinterpret_cast<float4*>(mine.at) + ((q - col0 + k) / 4) * kRows + r, make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]));
+        for (int k = 0; k < 4; ++k) {
+          w[k].x = pack2<kFp16>(v[8 * k], v[8 * k + 1]);
+          w[k].y = pack2<kFp16>(v[8 * k + 2], v[8 * k + 3]);
+          w[k].z = pack2<kFp16>(v[8 * k + 4], v[8 * k + 5]);
+          w[k].w = pack2<kFp16>(v[8 * k + 6], v[8 * k + 7]);
         }
+        transpose4(w, q4);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (at[k] >= 0) *reinterpret_cast<uint4*>(p.out + at[k] + (q + 8 * q4) * 2) = w[k];
+      } else if (valid) {
+#pragma unroll
+        for (int k = 0; k < 32; k += 4)
+          __stcg(reinterpret_cast<float4*>(mine.at) + ((q - col0 + k) / 4) * kRows + r, make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]));
       }
     }
   }
@@ -1187,51 +1224,48 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
   } else {
     if (valid) __stcg(mine.ml() + r, make_float2(m, l));
     if (arrived_last(p, sm, en, x, st.ok)) {
-      // merge the unit's records in order, four columns of a row per thread
-      const int items = rows * (cols / 4);
-      for (int it = r; it < items; it += 128) {
-        const int c4 = it / rows, rr = it - c4 * rows;
+      // merge the unit's records in order: the row's maximum and sum, then 32 columns at a time
+      if (valid) {
         float mm = -INFINITY, ll = 0.f;
-        float4 oo = make_float4(0.f, 0.f, 0.f, 0.f);
-        constexpr int kU = 4;
-        for (int q0 = 0; q0 < en.pieces; q0 += kU) {
-          float2 z[kU];
-          float4 v[kU];
-#pragma unroll
-          for (int q = 0; q < kU; ++q) {
-            z[q] = make_float2(-INFINITY, 0.f);
-            v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (q0 + q < en.pieces) {
-              const Records<D> rec = records<D>(p, en.first + q0 + q, q0 + q == 0, x);
-              z[q] = __ldcg(rec.ml() + rr);
-              v[q] = __ldcg(reinterpret_cast<const float4*>(rec.at) + c4 * kRows + rr);
-            }
-          }
-          float mn = mm;
-#pragma unroll
-          for (int q = 0; q < kU; ++q) mn = fmaxf(mn, z[q].x);
-          const float bs = finite_or_0(mn);
-          float f = ex2_approx(mm - bs);
-          ll *= f;
-          oo.x *= f; oo.y *= f; oo.z *= f; oo.w *= f;
-#pragma unroll
-          for (int q = 0; q < kU; ++q) {
-            f = ex2_approx(z[q].x - bs);
-            ll = fmaf(z[q].y, f, ll);
-            oo.x = fmaf(v[q].x, f, oo.x);
-            oo.y = fmaf(v[q].y, f, oo.y);
-            oo.z = fmaf(v[q].z, f, oo.z);
-            oo.w = fmaf(v[q].w, f, oo.w);
-          }
-          mm = mn;
+        for (int q = 0; q < en.pieces; ++q) mm = fmaxf(mm, __ldcg(records<D>(p, en.first + q, q == 0, x).ml() + r).x);
+        const float bs = finite_or_0(mm);
+        for (int q = 0; q < en.pieces; ++q) {
+          const float2 z = __ldcg(records<D>(p, en.first + q, q == 0, x).ml() + r);
+          ll = fmaf(z.y, ex2_approx(z.x - bs), ll);
         }
         const float iv = ll == 0.f ? 0.f : 1.f / ll;
-        const int ii = (base + rr) / p.G, hd = en.h * p.G + base + rr - ii * p.G;
-        const uint2 w = make_uint2(pack2<kFp16>(oo.x * iv, oo.y * iv), pack2<kFp16>(oo.z * iv, oo.w * iv));
-        *reinterpret_cast<uint2*>(p.out + static_cast<long long>(en.tok0 + ii) * p.out_token +
-                                  static_cast<long long>(hd) * p.out_head + (col0 + c4 * 4) * 2) = w;
-        if (p.lse && c4 == 0 && (!paired || x == 0))
-          p.lse[static_cast<long long>(en.tok0 + ii) * p.H_q + hd] = lse_of(mm - kUp, ll);
+        uint8_t* const orow = p.out + static_cast<long long>(en.tok0 + i) * p.out_token + static_cast<long long>(head) * p.out_head;
+#pragma unroll 1
+        for (int c4 = 0; c4 < cols / 4; c4 += 8) {
+          float4 oo[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) oo[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+          for (int q = 0; q < en.pieces; ++q) {
+            const Records<D> rec = records<D>(p, en.first + q, q == 0, x);
+            const float f = ex2_approx(__ldcg(rec.ml() + r).x - bs);
+            float4 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = __ldcg(reinterpret_cast<const float4*>(rec.at) + (c4 + k) * kRows + r);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              oo[k].x = fmaf(v[k].x, f, oo[k].x);
+              oo[k].y = fmaf(v[k].y, f, oo[k].y);
+              oo[k].z = fmaf(v[k].z, f, oo[k].z);
+              oo[k].w = fmaf(v[k].w, f, oo[k].w);
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 8; k += 2) {
+            uint4 w;
+            w.x = pack2<kFp16>(oo[k].x * iv, oo[k].y * iv);
+            w.y = pack2<kFp16>(oo[k].z * iv, oo[k].w * iv);
+            w.z = pack2<kFp16>(oo[k + 1].x * iv, oo[k + 1].y * iv);
+            w.w = pack2<kFp16>(oo[k + 1].z * iv, oo[k + 1].w * iv);
+            *reinterpret_cast<uint4*>(orow + (col0 + (c4 + k) * 4) * 2) = w;
+          }
+        }
+        if (p.lse && (!paired || x == 0)) p.lse[static_cast<long long>(en.tok0 + i) * p.H_q + head] = lse_of(mm - kUp, ll);
       }
     }
   }
