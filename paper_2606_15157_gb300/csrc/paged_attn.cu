@@ -28,9 +28,9 @@
 // (pieces of units) to the others through a ring, warps 4-7 and 8-11 are the sides' softmax warpgroups, a
 // thread per row.  S = Q K^T is read from tensor memory into registers, and the
 // weights go back into the same columns as the A operand of O += P V.
+#include <atomic>
 #include <climits>
 #include <cmath>
-#include <mutex>
 
 #include "paged.cuh"
 
@@ -45,9 +45,9 @@ constexpr int kEntries = 4;         // ring of dealt entries
 // Kinds of unit, and the cost of a key tile and of a unit's start and end in each.
 enum Kind : int { kFew = 0, kPaired = 1, kFull = 2 };
 constexpr int kFewRows = 16;
-__host__ __device__ constexpr int tile_cost(int kind) { return kind == kFull ? 2 : 1; }
-__host__ __device__ constexpr int unit_cost(int kind) { return kind == kFull ? 1 : 1; }
-constexpr int kMinShare = 2;        // least cost of a share, a tile's or more: no piece of a cut unit is empty
+__host__ __device__ constexpr int tile_cost(int kind) { return kind == kFull ? 4 : 3; }
+__host__ __device__ constexpr int unit_cost(int kind) { return kind == kFull ? 12 : 6; }
+constexpr int kMinShare = 4;        // least cost of a share, a tile's or more: no piece of a cut unit is empty
 constexpr int kRows = 128;          // rows of a side
 constexpr int kParts = 2;           // halves of a tile's weights, which the second product takes as they come
 constexpr float kRaise = 8.f;       // a row's maximum is raised when a tile's is this much (log2) above it
@@ -1362,17 +1362,29 @@ AttnFn attn_fn(int d, bool fp16) {
 }
 size_t attn_smem(int d) { return d == 64 ? sizeof(AttnSmem<64>) : sizeof(AttnSmem<128>); }
 
-// Whether the compiled kernel's registers cover the warpgroups' split (an increase that
-// the launch's registers cannot cover would never complete).
-bool attn_regs_ok(int d, bool fp16) {
-  static std::once_flag once[4];
-  static bool ok[4] = {};
-  const int i = (d == 64 ? 0 : 2) + (fp16 ? 1 : 0);
-  std::call_once(once[i], [&] {
-    cudaFuncAttributes a = {};
-    ok[i] = cudaFuncGetAttributes(&a, attn_fn(d, fp16)) == cudaSuccess && a.numRegs * kAttnThreads >= kRegsAttnNeeded;
-  });
-  return ok[i];
+// Readies a kernel for the current device, once: its registers have to cover the
+// warpgroups' split (an increase that the launch's registers cannot cover would never
+// complete), its shared memory limit is raised.  grid: CTAs to launch.
+int attn_ready(int d, bool fp16, int* grid) {
+  constexpr int kDevices = 64;
+  static std::atomic<int> ctas[4][kDevices];  // 0: not yet
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev >= kDevices) return KVEV_ECUDA;
+  std::atomic<int>& ready = ctas[(d == 64 ? 0 : 2) + (fp16 ? 1 : 0)][dev];
+  *grid = ready.load(std::memory_order_relaxed);
+  if (*grid > 0) return KVEV_OK;
+  int sms = 0;
+  cudaFuncAttributes a = {};
+  const AttnFn fn = attn_fn(d, fp16);
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+      cudaFuncGetAttributes(&a, fn) != cudaSuccess)
+    return KVEV_ECUDA;
+  if (a.numRegs * kAttnThreads < kRegsAttnNeeded) return KVEV_ENOTSUP;
+  if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(attn_smem(d))) != cudaSuccess)
+    return KVEV_ECUDA;
+  *grid = sms < kMaxCtas ? sms : kMaxCtas;
+  ready.store(*grid, std::memory_order_relaxed);  // (two threads at once: the same values)
+  return KVEV_OK;
 }
 
 bool encode16(CUtensorMap* m, bool fp16, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
@@ -1425,13 +1437,11 @@ extern "C" int kvev_paged_attention(const kvev_paged_cache* cache, const void* q
       (reinterpret_cast<uintptr_t>(lse) & 3u))
     return KVEV_EINVAL;
 
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return KVEV_ECUDA;
   const int d = cache->d;
   const bool fp16 = cache->dtype == KVEV_FP16;
-  if (!attn_regs_ok(d, fp16)) return KVEV_ENOTSUP;
+  int grid = 0;
+  rc = attn_ready(d, fp16, &grid);
+  if (rc != KVEV_OK) return rc;
   PagedAttnParams p = {};
   p.G = H_q / cache->H_kv;
   p.P = kRows / p.G;
@@ -1472,11 +1482,7 @@ extern "C" int kvev_paged_attention(const kvev_paged_cache* cache, const void* q
   p.status = device_status;
   p.sync = static_cast<int*>(workspace);
   p.parts = static_cast<uint8_t*>(workspace) + KVEV_PAGED_SYNC_BYTES;
-  const AttnFn fn = attn_fn(d, fp16);
-  const size_t smem = attn_smem(d);
-  if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
-    return KVEV_ECUDA;
-  const int grid = sms < kMaxCtas ? sms : kMaxCtas;
-  return launch_overlapped(fn, p, grid, kAttnThreads, smem, static_cast<cudaStream_t>(stream)) == cudaSuccess ? KVEV_OK
-                                                                                                           : KVEV_ECUDA;
+  return launch_overlapped(attn_fn(d, fp16), p, grid, kAttnThreads, attn_smem(d), static_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? KVEV_OK
+             : KVEV_ECUDA;
 }

@@ -5,6 +5,9 @@ are a scheduler step.  :class:`PagedCache` is one layer's pages under such a tab
 tokens' rows, ``attention`` over them, ``gather`` whole prompts for ``Plan.evict_prefill``.  Lengths,
 tables and slots stay on the device throughout.  Argument checks raise ``ValueError`` (shapes, types)
 or ``KvevError`` (what the library refuses).
+
+These are calls of a few microseconds on the device, made for every layer of every token: the checks
+here are a handful of attribute reads, the stream is read as a number.
 """
 from __future__ import annotations
 
@@ -15,6 +18,7 @@ import torch
 from . import kvev
 
 _DTYPES = {torch.bfloat16: kvev.BF16, torch.float16: kvev.FP16}
+_I32 = torch.int32
 
 
 def _need(ok: bool, what: str):
@@ -22,29 +26,33 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
-def _int32(t, n: int | None, what: str):
-    """Device pointer of a contiguous int32 CUDA tensor of n elements (any number: None)."""
-    if t.dtype is not torch.int32 or not t.is_cuda or not t.is_contiguous() or (n is not None and t.numel() != n):
-        raise ValueError(f"{what}: a contiguous int32 CUDA tensor" + (f" of {n} elements" if n is not None else ""))
+def _int32(t, n: int, what: str) -> int:
+    """Device pointer of a contiguous int32 tensor of n elements."""
+    if t.dtype is not _I32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous int32 tensor of {n} elements")
     return t.data_ptr()
 
 
-def _stride(t, i: int) -> int:
-    """Element stride of dimension i (that of a dimension of one element means nothing: the row size)."""
-    return t.stride(i) if t.shape[i] != 1 else t.shape[-1] * (t.shape[-2] if i < t.dim() - 2 else 1)
+# The current stream of a device as a number; torch.cuda.current_stream() makes an object first (2.8 us).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _same_layout(a, b) -> bool:
-    return a.shape == b.shape and all(_stride(a, i) == _stride(b, i) for i in range(a.dim() - 1))
+def _table(block_table) -> int:
+    _need(block_table.dim() == 2 and block_table.is_cuda, "block_table: int32 [requests][pages] on a GPU")
+    return _int32(block_table, block_table.numel(), "block_table")
 
 
-def _stream(stream) -> int:
-    return torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream
-
-
-def _table(block_table):
-    _need(block_table.dim() == 2, "block_table: [requests][pages]")
-    return _int32(block_table, None, "block_table")
+def _strides(t) -> tuple:
+    """Element strides; that of a dimension of one element, which means nothing, as if it were contiguous."""
+    shape, st = t.shape, t.stride()
+    if 1 in shape:
+        st, full = list(st), 1
+        for i in range(len(shape) - 1, -1, -1):
+            if shape[i] == 1:
+                st[i] = full
+            full = shape[i] * st[i]
+    return st
 
 
 class PagePool:
@@ -56,46 +64,61 @@ class PagePool:
     def __init__(self, num_pages: int, page_size: int, block_table, free=None, free_count=None):
         dev = block_table.device
         if free is None:
-            free = torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=dev)
-            free_count = torch.full((1,), num_pages, dtype=torch.int32, device=dev) if free_count is None else free_count
+            free = torch.arange(num_pages - 1, -1, -1, dtype=_I32, device=dev)
+            free_count = torch.full((1,), num_pages, dtype=_I32, device=dev) if free_count is None else free_count
         self.num_pages, self.page_size = num_pages, page_size
         self.block_table, self._table = block_table, _table(block_table)
+        self.max_requests, self.max_pages = block_table.shape
         self.free, self._free = free, _int32(free, num_pages, "free")
-        self.free_count = torch.zeros(1, dtype=torch.int32, device=dev) if free_count is None else free_count
-        self.device_status = torch.zeros(1, dtype=torch.int32, device=dev)
+        state = torch.zeros(2, dtype=_I32, device=dev)
+        self.free_count = state[:1] if free_count is None else free_count
+        self.device_status = state[1:]
+        self._status, self._device = self.device_status.data_ptr(), dev.index or 0
 
     def tables(self, lens, new_lens, T: int, *, kv_lens=None, cu=None, slots=None, positions=None, granted=None,
                free_count=None, free_count_out=None, stream=None):
         """Pages for the new tokens, and where each goes: (kv_lens, cu, slots, positions, granted).
         T: rows of the new tokens' tensors.  By default the pool's count is updated in place and the
         outputs are new tensors; ``kv_lens=lens`` updates the lengths in place."""
-        B, dev = lens.numel(), lens.device
-        _need(B <= self.block_table.shape[0], "more requests than the block table has rows")
-        e = lambda t, n: torch.empty(n, dtype=torch.int32, device=dev) if t is None else t
-        kv_lens, cu, slots, positions, granted = e(kv_lens, B), e(cu, B + 1), e(slots, T), e(positions, T), e(granted, B)
-        free_count = self.free_count if free_count is None else free_count
-        free_count_out = free_count if free_count_out is None else free_count_out
-        kvev._check(kvev.kvev_paged_tables(
+        B = lens.numel()
+        if B > self.max_requests:
+            raise ValueError("more requests than the block table has rows")
+        if kv_lens is None or cu is None or slots is None or positions is None or granted is None:
+            e = lambda t, n: torch.empty(n, dtype=_I32, device=lens.device) if t is None else t
+            kv_lens, cu, slots, positions, granted = e(kv_lens, B), e(cu, B + 1), e(slots, T), e(positions, T), e(granted, B)
+        if free_count is None:
+            free_count = self.free_count
+        if free_count_out is None:
+            free_count_out = free_count
+        rc = kvev.load().kvev_paged_tables(
             _int32(lens, B, "lens"), _int32(new_lens, B, "new_lens"), B, self.page_size, self.num_pages, self._free,
-            _int32(free_count, 1, "free_count"), self._table, self.block_table.shape[1], T, _int32(kv_lens, B, "kv_lens"),
+            _int32(free_count, 1, "free_count"), self._table, self.max_pages, T, _int32(kv_lens, B, "kv_lens"),
             _int32(cu, B + 1, "cu"), _int32(slots, T, "slots"), _int32(positions, T, "positions"),
-            _int32(granted, B, "granted"), _int32(free_count_out, 1, "free_count_out"), self.device_status.data_ptr(),
-            _stream(stream)), "kvev_paged_tables")
+            _int32(granted, B, "granted"), _int32(free_count_out, 1, "free_count_out"), self._status,
+            _raw_stream(self._device) if stream is None else stream.cuda_stream)
+        if rc:
+            raise kvev.KvevError(rc, "kvev_paged_tables")
         return kv_lens, cu, slots, positions, granted
 
     def release(self, lens, done, *, lens_out=None, free_count=None, free_count_out=None, stream=None):
         """The pages of requests with done != 0 go back; returns the lengths, 0 for those (by default
         ``lens`` itself and the pool's count are updated in place)."""
         B = lens.numel()
-        _need(B <= self.block_table.shape[0], "more requests than the block table has rows")
-        lens_out = lens if lens_out is None else lens_out
-        free_count = self.free_count if free_count is None else free_count
-        free_count_out = free_count if free_count_out is None else free_count_out
-        kvev._check(kvev.kvev_paged_release(
-            _int32(lens, B, "lens"), _int32(done, B, "done"), B, self.page_size, self.num_pages, self._table,
-            self.block_table.shape[1], self._free, _int32(free_count, 1, "free_count"), _int32(lens_out, B, "lens_out"),
-            _int32(free_count_out, 1, "free_count_out"), self.device_status.data_ptr(), _stream(stream)),
-            "kvev_paged_release")
+        if B > self.max_requests:
+            raise ValueError("more requests than the block table has rows")
+        if lens_out is None:
+            lens_out = lens
+        if free_count is None:
+            free_count = self.free_count
+        if free_count_out is None:
+            free_count_out = free_count
+        rc = kvev.load().kvev_paged_release(
+            _int32(lens, B, "lens"), _int32(done, B, "done"), B, self.page_size, self.num_pages, self._table, self.max_pages,
+            self._free, _int32(free_count, 1, "free_count"), _int32(lens_out, B, "lens_out"),
+            _int32(free_count_out, 1, "free_count_out"), self._status,
+            _raw_stream(self._device) if stream is None else stream.cuda_stream)
+        if rc:
+            raise kvev.KvevError(rc, "kvev_paged_release")
         return lens_out
 
 
@@ -104,16 +127,18 @@ class PagedCache:
     contiguous; a transposed view of [num_pages][H_kv][page_size][d] will do), under a block table."""
 
     def __init__(self, K, V, block_table):
-        _need(K.dim() == 4 and V.dim() == 4 and _same_layout(K, V) and K.stride(3) == V.stride(3) == 1,
+        _need(K.dim() == 4 and K.shape == V.shape and _strides(K) == _strides(V) and K.stride(3) == V.stride(3) == 1,
               "K, V: [num_pages][page_size][H_kv][d] of equal strides, d contiguous")
-        _need(K.dtype in _DTYPES and K.dtype == V.dtype, "K, V: bfloat16 or float16")
+        _need(K.dtype in _DTYPES and K.dtype is V.dtype, "K, V: bfloat16 or float16")
         _need(K.is_cuda and V.is_cuda, "K, V: CUDA tensors")
         self.K, self.V, self.block_table, self._table = K, V, block_table, _table(block_table)
+        self.max_requests, self.max_pages = block_table.shape
         pages, page, self.H_kv, self.d = K.shape
-        self.desc = kvev.PagedCacheDesc(K.data_ptr(), V.data_ptr(), _stride(K, 0), _stride(K, 1), _stride(K, 2), pages, page,
-                                        self.H_kv, self.d, _DTYPES[K.dtype])
-        self._desc = C.addressof(self.desc)
-        self.device_status = torch.zeros(1, dtype=torch.int32, device=K.device)
+        self.dtype = K.dtype
+        self.desc = kvev.PagedCacheDesc(K.data_ptr(), V.data_ptr(), *_strides(K)[:3], pages, page, self.H_kv, self.d,
+                                        _DTYPES[K.dtype])
+        self._desc, self._device = C.addressof(self.desc), K.device.index or 0
+        self.device_status = torch.zeros(1, dtype=_I32, device=K.device)
         self._status = self.device_status.data_ptr()
         self._workspaces = {}
 
@@ -125,56 +150,83 @@ class PagedCache:
         K, V = x.transpose(2, 3) if heads_first else x
         return cls(K, V, block_table)
 
-    def _rows(self, t, H, what):
-        _need(t.dim() == 3 and t.shape[1] == H and t.shape[2] == self.d and t.dtype is self.K.dtype and t.stride(2) == 1,
-              f"{what}: [tokens][{H}][{self.d}] of the cache's type, d contiguous")
-        return t.data_ptr()
+    def _rows(self, t, shape, what) -> tuple:
+        """(token stride, head stride) of [T][H][d] rows of the cache's type."""
+        if len(shape) != 3 or t.dtype is not self.dtype or shape[2] != self.d:
+            raise ValueError(f"{what}: [tokens][heads][{self.d}] of the cache's type")
+        st = _strides(t)
+        if st[2] != 1:
+            raise ValueError(f"{what}: the last dimension is contiguous")
+        return st
 
     def write(self, k, v, slots, stream=None):
         """k, v [T][H_kv][d] of equal strides into the slots (int32 [T], negative: left out)."""
-        T = k.shape[0]
-        _need(k.dim() == 3 and _same_layout(k, v), "k, v: equal shapes and strides")
-        kvev._check(kvev.kvev_paged_write(self._desc, self._rows(k, self.H_kv, "k"), self._rows(v, self.H_kv, "v"),
-                                          _stride(k, 0), _stride(k, 1), _int32(slots, T, "slots"), T, self._status,
-                                          _stream(stream)), "kvev_paged_write")
+        shape = k.shape
+        st = self._rows(k, shape, "k")
+        if shape[1] != self.H_kv or v.shape != shape or self._rows(v, shape, "v") != st:
+            raise ValueError(f"k, v: [tokens][{self.H_kv}][{self.d}] of equal strides")
+        rc = kvev.load().kvev_paged_write(
+            self._desc, k.data_ptr(), v.data_ptr(), st[0], st[1], _int32(slots, shape[0], "slots"), shape[0], self._status,
+            _raw_stream(self._device) if stream is None else stream.cuda_stream)
+        if rc:
+            raise kvev.KvevError(rc, "kvev_paged_write")
 
     def workspace(self, H_q, stream=None):
         """The scratch of attention calls on a stream (one per stream: overlapping calls may not share it)."""
-        at = _stream(stream)
-        ws = self._workspaces.get((H_q, at))
+        return self._workspace(H_q, _raw_stream(self._device) if stream is None else stream.cuda_stream)[2]
+
+    def _workspace(self, H_q, stream: int):
+        ws = self._workspaces.get((H_q, stream))
         if ws is None:
             n = kvev.kvev_paged_attention_workspace(H_q, self.H_kv, self.d)
-            ws = self._workspaces[H_q, at] = torch.zeros(n, dtype=torch.uint8, device=self.K.device)
+            t = torch.empty(n, dtype=torch.uint8, device=self.K.device)
+            t[:kvev.PAGED_SYNC_BYTES].zero_()
+            ws = self._workspaces[H_q, stream] = (t.data_ptr(), n, t)
         return ws
 
     def attention(self, q, cu, kv_lens, *, scale=0.0, window=0, out=None, lse=None, workspace=None, stream=None):
         """Causal attention of the new tokens' queries q [T][H_q][d] (request s: rows cu[s]..cu[s+1], the last of
         its kv_lens[s] positions).  lse: fp32 [T][H_q] for the rows' log-sum-exp.  Returns out."""
-        T, H_q = q.shape[0], q.shape[1]
+        shape = q.shape
+        sq = self._rows(q, shape, "q")
+        T, H_q, _ = shape
         B = kv_lens.numel()
-        _need(B <= self.block_table.shape[0], "more requests than the block table has rows")
-        out = torch.empty((T, H_q, self.d), dtype=q.dtype, device=q.device) if out is None else out
-        _need(out.shape == q.shape, "out: q's shape")
-        _need(lse is None or (lse.dtype is torch.float32 and lse.is_contiguous() and lse.shape == (T, H_q)),
-              "lse: contiguous float32 [T][H_q]")
-        ws = self.workspace(H_q, stream) if workspace is None else workspace
-        kvev._check(kvev.kvev_paged_attention(
-            self._desc, self._rows(q, H_q, "q"), _stride(q, 0), _stride(q, 1), _int32(cu, B + 1, "cu"),
-            _int32(kv_lens, B, "kv_lens"), self._table, self.block_table.shape[1], B, T, H_q, scale, window,
-            self._rows(out, H_q, "out"), _stride(out, 0), _stride(out, 1), None if lse is None else lse.data_ptr(),
-            ws.data_ptr(), ws.numel(), self._status, _stream(stream)), "kvev_paged_attention")
+        if B > self.max_requests:
+            raise ValueError("more requests than the block table has rows")
+        if out is None:
+            out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        elif out.shape != shape:
+            raise ValueError("out: q's shape")
+        so = self._rows(out, shape, "out")
+        if lse is None:
+            lse_ptr = None
+        else:
+            if lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.shape != shape[:2]:
+                raise ValueError("lse: contiguous float32 [T][H_q]")
+            lse_ptr = lse.data_ptr()
+        at = _raw_stream(self._device) if stream is None else stream.cuda_stream
+        ws = self._workspace(H_q, at) if workspace is None else (workspace.data_ptr(), workspace.numel())
+        rc = kvev.load().kvev_paged_attention(
+            self._desc, q.data_ptr(), sq[0], sq[1], _int32(cu, B + 1, "cu"), _int32(kv_lens, B, "kv_lens"), self._table,
+            self.max_pages, B, T, H_q, scale, window, out.data_ptr(), so[0], so[1], lse_ptr, ws[0], ws[1], self._status, at)
+        if rc:
+            raise kvev.KvevError(rc, "kvev_paged_attention")
         return out
 
     def gather(self, lens, out_K, out_V, stream=None):
         """The first lens[s] tokens of every request into out_K, out_V [B][H_kv][S_cap][d] (contiguous)."""
-        B, S_cap = lens.numel(), out_K.shape[2]
-        for t in (out_K, out_V):
-            _need(t.shape == (B, self.H_kv, S_cap, self.d) and t.is_contiguous() and t.dtype is self.K.dtype,
-                  f"out_K, out_V: contiguous [{B}][{self.H_kv}][S_cap][{self.d}] of the cache's type")
-        _need(B <= self.block_table.shape[0], "more requests than the block table has rows")
-        kvev._check(kvev.kvev_paged_gather(self._desc, self._table, self.block_table.shape[1], _int32(lens, B, "lens"), B,
-                                           S_cap, out_K.data_ptr(), out_V.data_ptr(), self._status, _stream(stream)),
-                    "kvev_paged_gather")
+        B, shape = lens.numel(), out_K.shape
+        if (len(shape) != 4 or shape[0] != B or shape[1] != self.H_kv or shape[3] != self.d or out_V.shape != shape
+                or out_K.dtype is not self.dtype or out_V.dtype is not self.dtype
+                or not out_K.is_contiguous() or not out_V.is_contiguous()):
+            raise ValueError(f"out_K, out_V: contiguous [{B}][{self.H_kv}][S_cap][{self.d}] of the cache's type")
+        if B > self.max_requests:
+            raise ValueError("more requests than the block table has rows")
+        rc = kvev.load().kvev_paged_gather(
+            self._desc, self._table, self.max_pages, _int32(lens, B, "lens"), B, shape[2], out_K.data_ptr(), out_V.data_ptr(),
+            self._status, _raw_stream(self._device) if stream is None else stream.cuda_stream)
+        if rc:
+            raise kvev.KvevError(rc, "kvev_paged_gather")
 
     def status(self) -> int:
         """Synchronises, reads and clears the device status word (0: every call so far was in order)."""
