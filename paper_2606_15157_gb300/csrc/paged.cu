@@ -1,7 +1,6 @@
 // paged.cu -- the paged cache in front of the eviction: block tables and slots
 // built on the GPU, rows written to their slots, and whole prompts gathered
 // into the contiguous caches that the prefill eviction reads.
-#include <algorithm>
 #include <climits>
 
 #include "paged.cuh"
@@ -11,12 +10,15 @@ namespace {
 
 // ---------------------------------------------------------------------------
 // Block tables.  Everything a step needs follows from two prefix sums over the
-// requests, of new tokens and of new pages, which one CTA forms in shared memory;
-// then tokens and pages are dealt over its threads, each finding its request by
+// requests, of new tokens and of new pages, which every CTA forms in its own shared
+// memory; then tokens and pages are dealt over all threads, each finding its request by
 // bisection.  Whatever is written may be an input's own memory (lengths, the
-// count): it is written after all of it has been read.
+// count): nothing is written before every CTA has read all of it, so the CTAs are one
+// cluster, of eight when there are tokens for them.  Bound by its round trips to L2
+// (lengths; table or stack), 2 us, and the launch.
 // ---------------------------------------------------------------------------
 constexpr int kTableThreads = 1024;
+constexpr int kTableCluster = 8;  // most CTAs of a cluster that every device takes
 
 struct TableParams {
   const int *lens, *new_lens, *free_pages, *free_count;
@@ -61,12 +63,22 @@ __device__ __forceinline__ int pages_of(int n, int shift) {
   return static_cast<int>((static_cast<long long>(n) + (1 << shift) - 1) >> shift);
 }
 
+// Every CTA of the cluster is here, and what their threads read before has been read.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+__device__ __forceinline__ int cluster_size() {
+  int n;
+  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n));
+  return n;
+}
+
 __global__ void __launch_bounds__(kTableThreads) tables_kernel(const __grid_constant__ TableParams p) {
   extern __shared__ int sm[];
-  int* const cu = sm;             // [B] first token
-  int* const first = sm + p.B;    // [B] new pages of the requests before
-  int* const len = sm + 2 * p.B;  // [B] tokens held
-  int* const need = sm + 3 * p.B; // [B] new pages, -1 = refused
+  int* const cu = sm;                     // [B + 1] first token
+  int* const first = sm + p.B + 1;        // [B] new pages of the requests before
+  int* const len = sm + 2 * p.B + 1;      // [B] tokens held
+  int* const granted = sm + 3 * p.B + 1;  // [B]
   __shared__ longlong2 ws[32];
   __shared__ long long carry[2];
   __shared__ int given;
@@ -74,8 +86,8 @@ __global__ void __launch_bounds__(kTableThreads) tables_kernel(const __grid_cons
   pdl_trigger();
   const int tid = threadIdx.x;
   if (tid == 0) { carry[0] = carry[1] = 0; given = 0; }
-  const int count = min(max(*p.free_count, 0), p.num_pages);
-  bool bad = *p.free_count != count;
+  const int top = *p.free_count, count = min(max(top, 0), p.num_pages);
+  bool bad = top != count;
   __syncthreads();
   for (int s0 = 0; s0 < p.B; s0 += kTableThreads) {
     const int s = s0 + tid;
@@ -101,31 +113,37 @@ __global__ void __launch_bounds__(kTableThreads) tables_kernel(const __grid_cons
       cu[s] = static_cast<int>(min(c0 + upto.x - q, static_cast<long long>(INT_MAX)));
       first[s] = static_cast<int>(min(c1 + upto.y - k, static_cast<long long>(INT_MAX)));
       len[s] = n;
-      need[s] = ok ? k : -1;
+      granted[s] = ok;
       if (ok && k > 0) atomicMax(&given, static_cast<int>(c1 + upto.y));
-      p.cu[s] = cu[s];
-      p.granted[s] = ok;
-      p.kv_lens[s] = ok ? n + q : n;
     }
     __syncthreads();
   }
-  const int total = static_cast<int>(min(carry[0], static_cast<long long>(INT_MAX)));
-  if (tid == 0) {
-    p.cu[p.B] = total;
+  if (tid == 0) cu[p.B] = static_cast<int>(min(carry[0], static_cast<long long>(INT_MAX)));
+  cluster_sync();
+  const int total = cu[p.B];
+  const int t0 = blockIdx.x * kTableThreads + tid, step = cluster_size() * kTableThreads;
+  if (t0 == 0) {
     *p.count_out = count - given;
     bad |= total > p.T;
   }
+  for (int s = t0; s <= p.B; s += step) {
+    p.cu[s] = cu[s];
+    if (s < p.B) {
+      p.granted[s] = granted[s];
+      p.kv_lens[s] = granted[s] ? len[s] + (cu[s + 1] - cu[s]) : len[s];
+    }
+  }
   // pages given out, the k-th of them to the request whose range holds k
-  for (int k = tid; k < given; k += kTableThreads) {
+  for (int k = t0; k < given; k += step) {
     const int s = find_request(first, p.B, k);
     p.table[static_cast<long long>(s) * p.max_pages + pages_of(len[s], p.page_shift) + k - first[s]] =
         p.free_pages[count - 1 - k];
   }
-  for (int t = tid; t < p.T; t += kTableThreads) {
+  for (int t = t0; t < p.T; t += step) {
     int slot = -1, pos = -1;
     if (t < total) {
       const int s = find_request(cu, p.B, t);
-      if (need[s] >= 0) {
+      if (granted[s]) {
         pos = len[s] + t - cu[s];
         const int j = pos >> p.page_shift, held = pages_of(len[s], p.page_shift);
         const int page = j < held ? p.table[static_cast<long long>(s) * p.max_pages + j]
@@ -151,8 +169,8 @@ __global__ void __launch_bounds__(kTableThreads) release_kernel(const __grid_con
   pdl_trigger();
   const int tid = threadIdx.x;
   if (tid == 0) carry = 0;
-  const int count = min(max(*p.free_count, 0), p.num_pages);
-  bool bad = *p.free_count != count;
+  const int top = *p.free_count, count = min(max(top, 0), p.num_pages);
+  bool bad = top != count;
   __syncthreads();
   for (int s0 = 0; s0 < p.B; s0 += kTableThreads) {
     const int s = s0 + tid;
@@ -186,78 +204,116 @@ __global__ void __launch_bounds__(kTableThreads) release_kernel(const __grid_con
 }
 
 // ---------------------------------------------------------------------------
-// Rows.
+// Rows.  A CTA moves the rows of 2^row_shift tokens, of every head, K and V: its
+// vectors of 16 bytes are numbered head by head, token by token, and a thread has the
+// loads of kBatch of them in flight, K's and V's, before the first store.
 // ---------------------------------------------------------------------------
 struct WriteParams {
   PagedView c;
   const uint4 *k, *v;
   long long token_stride, head_stride;  // in vectors
   const int* slots;
-  int T;
+  int T, row_shift, dv_shift;
   int* status;
 };
 
 constexpr int kRowThreads = 256;
+constexpr int kBatch = 4;
+constexpr int kMaxRowShift = 4;
 
-// A thread carries vectors of 16 bytes, K's and V's of the same place together.
 __global__ void __launch_bounds__(kRowThreads) write_kernel(const __grid_constant__ WriteParams p) {
+  __shared__ long long to[1 << kMaxRowShift];  // a token's row in the pool, -1: none
   pdl_wait();
   pdl_trigger();
-  const int nv = p.c.H_kv * p.c.dv;
-  const long long n = static_cast<long long>(p.T) * nv;
-  for (long long i = static_cast<long long>(blockIdx.x) * kRowThreads + threadIdx.x; i < n;
-       i += static_cast<long long>(gridDim.x) * kRowThreads) {
-    const int t = static_cast<int>(i / nv), r = static_cast<int>(i - static_cast<long long>(t) * nv);
-    const int h = r / p.c.dv, x = r - h * p.c.dv;
-    const int slot = p.slots[t];
-    if (slot < 0) continue;
-    const int page = slot >> p.c.page_shift;
-    if (page >= p.c.num_pages) {
-      atomicOr(p.status, kStatusDevice);
-      continue;
+  const int t0 = blockIdx.x << p.row_shift;
+  if (threadIdx.x < (1 << p.row_shift)) {
+    const int t = t0 + threadIdx.x;
+    const int slot = t < p.T ? p.slots[t] : -1, page = slot >> p.c.page_shift;
+    long long at = -1;
+    if (slot >= 0) {
+      if (page < p.c.num_pages) at = page * p.c.page_stride + (slot & ((1 << p.c.page_shift) - 1)) * p.c.token_stride;
+      else atomicOr(p.status, kStatusDevice);
     }
-    const long long src = t * p.token_stride + h * p.head_stride + x;
-    const long long dst = page * p.c.page_stride + (slot & ((1 << p.c.page_shift) - 1)) * p.c.token_stride +
-                          h * p.c.head_stride + x;
-    const_cast<uint4*>(p.c.K)[dst] = p.k[src];
-    const_cast<uint4*>(p.c.V)[dst] = p.v[src];
+    to[threadIdx.x] = at;
+  }
+  __syncthreads();
+  const int n = p.c.H_kv << (p.row_shift + p.dv_shift);
+  for (int i0 = threadIdx.x; i0 < n; i0 += kBatch * kRowThreads) {
+    uint4 a[kBatch], b[kBatch];
+    long long at[kBatch];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      const int i = i0 + q * kRowThreads;
+      const int x = i & ((1 << p.dv_shift) - 1), k = (i >> p.dv_shift) & ((1 << p.row_shift) - 1), h = i >> (p.dv_shift + p.row_shift);
+      at[q] = i < n ? to[k] : -1;
+      if (at[q] < 0) continue;
+      at[q] += h * p.c.head_stride + x;
+      const long long from = (t0 + k) * p.token_stride + h * p.head_stride + x;
+      a[q] = __ldg(p.k + from);
+      b[q] = __ldg(p.v + from);
+    }
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q)
+      if (at[q] >= 0) {
+        const_cast<uint4*>(p.c.K)[at[q]] = a[q];
+        const_cast<uint4*>(p.c.V)[at[q]] = b[q];
+      }
   }
 }
 
 struct PageGatherParams {
   PagedView c;
   const int *table, *lens;
-  int B, max_pages, S_cap;
+  int B, max_pages, S_cap, dv_shift;
   uint4 *out_K, *out_V;
   int* status;
 };
 
-constexpr int kGatherRows = 32;  // positions of a CTA
+constexpr int kGatherShift = 4;  // 16 positions of a CTA
 
 __global__ void __launch_bounds__(kRowThreads) page_gather_kernel(const __grid_constant__ PageGatherParams p) {
+  __shared__ long long from[1 << kGatherShift];  // a position's row in the pool, -1: none
   pdl_wait();
   pdl_trigger();
-  const int s = blockIdx.y;
-  const int k0 = blockIdx.x * kGatherRows;
-  const int len = p.lens[s];
-  const int n = min(max(len, 0), min(p.S_cap, p.max_pages << p.c.page_shift));
+  const int s = blockIdx.y, k0 = blockIdx.x << kGatherShift;
+  const int len = p.lens[s], n = min(max(len, 0), min(p.S_cap, p.max_pages << p.c.page_shift));
   if (n != len && threadIdx.x == 0 && blockIdx.x == 0) atomicOr(p.status, kStatusDevice);
-  const int rows = min(kGatherRows, n - k0);
-  if (rows <= 0) return;
-  const int nv = p.c.H_kv * p.c.dv;
-  for (int i = threadIdx.x; i < rows * nv; i += kRowThreads) {
-    const int k = k0 + i / nv, r = i % nv;
-    const int h = r / p.c.dv, x = r - h * p.c.dv;
-    const int page = p.table[static_cast<long long>(s) * p.max_pages + (k >> p.c.page_shift)];
-    if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.c.num_pages)) {
-      atomicOr(p.status, kStatusDevice);
-      continue;
+  if (k0 >= n) return;
+  if (threadIdx.x < (1 << kGatherShift)) {
+    const int k = k0 + threadIdx.x;
+    long long at = -1;
+    if (k < n) {
+      const int page = p.table[static_cast<long long>(s) * p.max_pages + (k >> p.c.page_shift)];
+      if (static_cast<unsigned>(page) < static_cast<unsigned>(p.c.num_pages))
+        at = page * p.c.page_stride + (k & ((1 << p.c.page_shift) - 1)) * p.c.token_stride;
+      else
+        atomicOr(p.status, kStatusDevice);
     }
-    const long long src = page * p.c.page_stride + (k & ((1 << p.c.page_shift) - 1)) * p.c.token_stride +
-                          h * p.c.head_stride + x;
-    const long long dst = ((static_cast<long long>(s) * p.c.H_kv + h) * p.S_cap + k) * p.c.dv + x;
-    p.out_K[dst] = p.c.K[src];
-    p.out_V[dst] = p.c.V[src];
+    from[threadIdx.x] = at;
+  }
+  __syncthreads();
+  const int total = p.c.H_kv << (kGatherShift + p.dv_shift);
+  const long long out0 = static_cast<long long>(s) * p.c.H_kv * p.S_cap + k0;
+  for (int i0 = threadIdx.x; i0 < total; i0 += kBatch * kRowThreads) {
+    uint4 a[kBatch], b[kBatch];
+    long long at[kBatch];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      const int i = i0 + q * kRowThreads;
+      const int x = i & ((1 << p.dv_shift) - 1), k = (i >> p.dv_shift) & ((1 << kGatherShift) - 1), h = i >> (p.dv_shift + kGatherShift);
+      const long long row = i < total ? from[k] : -1;
+      at[q] = -1;
+      if (row < 0) continue;
+      at[q] = ((out0 + static_cast<long long>(h) * p.S_cap + k) << p.dv_shift) + x;
+      a[q] = __ldg(p.c.K + row + h * p.c.head_stride + x);
+      b[q] = __ldg(p.c.V + row + h * p.c.head_stride + x);
+    }
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q)
+      if (at[q] >= 0) {
+        p.out_K[at[q]] = a[q];
+        p.out_V[at[q]] = b[q];
+      }
   }
 }
 
@@ -310,14 +366,15 @@ extern "C" int kvev_paged_tables(const int32_t* lens, const int32_t* new_lens, i
     return KVEV_EINVAL;
   if (B > KVEV_PAGED_MAX_REQUESTS) return KVEV_ENOTSUP;
   constexpr int kPerRequest = 4 * sizeof(int);
-  if (B * kPerRequest > 48 * 1024 &&
+  if (B * kPerRequest > 47 * 1024 &&
       cudaFuncSetAttribute(tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           KVEV_PAGED_MAX_REQUESTS * kPerRequest) != cudaSuccess)
+                           KVEV_PAGED_MAX_REQUESTS * kPerRequest + sizeof(int)) != cudaSuccess)
     return KVEV_ECUDA;
   TableParams p = {lens, new_lens, free_pages, free_count, block_table, kv_lens, cu_new, slots, positions, granted,
                    free_count_out, device_status, B, log2_of(page_size), num_pages, max_pages, T};
-  return launched(launch_overlapped(tables_kernel, p, 1, kTableThreads, kPerRequest * B,
-                                    static_cast<cudaStream_t>(stream)));
+  const int ctas = T > kTableThreads ? kTableCluster : 1;
+  return launched(launch_overlapped(tables_kernel, p, ctas, kTableThreads, kPerRequest * B + sizeof(int),
+                                    static_cast<cudaStream_t>(stream), ctas));
 }
 
 extern "C" int kvev_paged_release(const int32_t* lens, const int32_t* done, int B, int page_size, int num_pages,
@@ -351,8 +408,10 @@ extern "C" int kvev_paged_write(const kvev_paged_cache* cache, const void* k, co
   p.slots = slots;
   p.T = T;
   p.status = device_status;
-  const int64_t n = static_cast<int64_t>(T) * p.c.H_kv * p.c.dv;
-  const int grid = static_cast<int>(std::min<int64_t>((n + kRowThreads - 1) / kRowThreads, 152 * 8));
+  p.dv_shift = log2_of(p.c.dv);
+  // few tokens: a CTA each; many: as many as keep a batch of every thread full
+  p.row_shift = T < 2048 ? 0 : kMaxRowShift;
+  const int grid = static_cast<int>((static_cast<int64_t>(T) + (1 << p.row_shift) - 1) >> p.row_shift);
   return launched(launch_overlapped(write_kernel, p, grid, kRowThreads, 0, static_cast<cudaStream_t>(stream)));
 }
 
@@ -375,7 +434,8 @@ extern "C" int kvev_paged_gather(const kvev_paged_cache* cache, const int32_t* b
   p.out_K = static_cast<uint4*>(out_K);
   p.out_V = static_cast<uint4*>(out_V);
   p.status = device_status;
-  page_gather_kernel<<<dim3((S_cap + kGatherRows - 1) / kGatherRows, B), kRowThreads, 0,
+  p.dv_shift = log2_of(p.c.dv);
+  page_gather_kernel<<<dim3((S_cap + (1 << kGatherShift) - 1) >> kGatherShift, B), kRowThreads, 0,
                        static_cast<cudaStream_t>(stream)>>>(p);
   return launched(cudaGetLastError());
 }
