@@ -14,7 +14,7 @@ namespace {
 // memory; then tokens and pages are dealt over all threads, each finding its request by
 // bisection.  Whatever is written may be an input's own memory (lengths, the
 // count): nothing is written before every CTA has read all of it, so the CTAs are one
-// cluster, of eight when there are tokens for them.  Bound by its round trips to L2
+// cluster, of eight when there may be more than a thread's worth.  Bound by its round trips to L2
 // (lengths; table or stack), 2 us, and the launch.
 // ---------------------------------------------------------------------------
 constexpr int kTableThreads = 1024;
@@ -162,7 +162,8 @@ __global__ void __launch_bounds__(kTableThreads) tables_kernel(const __grid_cons
 
 __global__ void __launch_bounds__(kTableThreads) release_kernel(const __grid_constant__ ReleaseParams p) {
   extern __shared__ int sm[];
-  int* const first = sm;  // [B] pages released by the requests before
+  int* const first = sm;        // [B] pages released by the requests before
+  int* const len = sm + p.B;    // [B] what is left of the lengths
   __shared__ longlong2 ws[32];
   __shared__ long long carry;
   pdl_wait();
@@ -182,7 +183,7 @@ __global__ void __launch_bounds__(kTableThreads) release_kernel(const __grid_con
       k = done ? pages_of(max(n, 0), p.page_shift) : 0;
       bad |= k > p.max_pages;
       k = min(k, p.max_pages);
-      p.lens_out[s] = done ? 0 : n;
+      len[s] = done ? 0 : n;
     }
     const longlong2 upto = block_scan(k, 0, ws);
     const long long c = carry;
@@ -191,14 +192,27 @@ __global__ void __launch_bounds__(kTableThreads) release_kernel(const __grid_con
     if (s < p.B) first[s] = static_cast<int>(min(c + upto.x - k, static_cast<long long>(INT_MAX)));
     __syncthreads();
   }
+  cluster_sync();
   bad |= carry > p.num_pages - count;
   const int total = static_cast<int>(min(carry, static_cast<long long>(p.num_pages - count)));
-  if (tid == 0) *p.count_out = count + total;
-  for (int k = tid; k < total; k += kTableThreads) {
-    const int s = find_request(first, p.B, k);
-    const int page = p.table[static_cast<long long>(s) * p.max_pages + k - first[s]];
-    bad |= static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages);
-    p.free_pages[count + k] = page;
+  const int t0 = blockIdx.x * kTableThreads + tid, step = cluster_size() * kTableThreads;
+  if (t0 == 0) *p.count_out = count + total;
+  for (int s = t0; s < p.B; s += step) p.lens_out[s] = len[s];
+  for (int k0 = t0; k0 < total; k0 += 4 * step) {  // four entries in flight per thread
+    int page[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int k = k0 + q * step;
+      if (k >= total) continue;
+      const int s = find_request(first, p.B, k);
+      page[q] = p.table[static_cast<long long>(s) * p.max_pages + k - first[s]];
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (k0 + q * step < total) {
+        bad |= static_cast<unsigned>(page[q]) >= static_cast<unsigned>(p.num_pages);
+        p.free_pages[count + k0 + q * step] = page[q];
+      }
   }
   if (bad) atomicOr(p.status, kStatusDevice);
 }
@@ -387,8 +401,15 @@ extern "C" int kvev_paged_release(const int32_t* lens, const int32_t* done, int 
   if (B > KVEV_PAGED_MAX_REQUESTS) return KVEV_ENOTSUP;
   ReleaseParams p = {lens, done, block_table, free_count, free_pages, lens_out, free_count_out, device_status,
                      B, log2_of(page_size), num_pages, max_pages};
-  return launched(launch_overlapped(release_kernel, p, 1, kTableThreads, sizeof(int) * B,
-                                    static_cast<cudaStream_t>(stream)));
+  constexpr int kPerRequest = 2 * sizeof(int);
+  if (B * kPerRequest > 47 * 1024 &&
+      cudaFuncSetAttribute(release_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           KVEV_PAGED_MAX_REQUESTS * kPerRequest) != cudaSuccess)
+    return KVEV_ECUDA;
+  // how many pages come back only the device knows: more than a CTA's threads, as far as the table's size tells
+  const int ctas = static_cast<int64_t>(B) * max_pages > kTableThreads ? kTableCluster : 1;
+  return launched(launch_overlapped(release_kernel, p, ctas, kTableThreads, kPerRequest * B,
+                                    static_cast<cudaStream_t>(stream), ctas));
 }
 
 extern "C" int kvev_paged_write(const kvev_paged_cache* cache, const void* k, const void* v, int64_t token_stride,
