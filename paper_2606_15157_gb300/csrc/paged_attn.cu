@@ -71,7 +71,7 @@ struct PagedAttnParams {
 
 // One piece of a unit.
 struct Entry {
-  int tok0, rows, pos0, h;         // first token, rows (0: no more entries), the first token's position, KV head
+  int tok0, n, pos0, h;            // first token, tokens (0: no more entries), the first token's position, KV head
   int s, t0, t1, klo;              // request, key tiles [t0, t1), first key any row sees
   int khi, kind, pieces, first;    // end of the keys, kind of unit, pieces of the unit and the first one's CTA
 };
@@ -446,7 +446,7 @@ __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, const Shar
       if (c0 < c1) {
         Entry en;
         en.tok0 = r.c0 + 2 * p.P * m;
-        en.rows = u.n * p.G;
+        en.n = u.n;
         en.pos0 = r.kv - r.q + 2 * p.P * m;
         en.h = h;
         en.s = s;
@@ -476,7 +476,7 @@ __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, const Shar
   put(end);
 }
 
-// The next entry; every warp that takes entries calls it in order.  rows = 0: no more.
+// The next entry; every warp that takes entries calls it in order.  n = 0: no more.
 template <class S>
 __device__ __forceinline__ Entry take(const PagedAttnParams& p, S& sm, uint32_t e) {
   Entry en = {};
@@ -505,10 +505,10 @@ __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>&
   bool ok = true;
   for (uint32_t e = 0; ok; ++e) {
     const Entry en = take(p, sm, e);
-    if (uniform(en.rows) == 0) break;
+    if (uniform(en.n) == 0) break;
     const int kind = uniform(en.kind), h = uniform(en.h), t0 = uniform(en.t0), t1 = uniform(en.t1);
     const int tok0 = uniform(en.tok0), klo = uniform(en.klo), khi = uniform(en.khi);
-    const bool one = uniform(en.rows) == p.G;
+    const bool one = uniform(en.n) == 1;
     // ---- Q tiles ----
     const int sides = kind == kFull ? 2 : 1;
     for (int x = 0; ok && x < sides; ++x) {
@@ -613,7 +613,7 @@ __device__ __forceinline__ void mma_warp(const PagedAttnParams& p, AttnSmem<D>& 
   };
   for (uint32_t e = 0; ok; ++e) {
     const Entry en = take(p, sm, e);
-    if (uniform(en.rows) == 0) break;
+    if (uniform(en.n) == 0) break;
     const int n = uniform(en.t1 - en.t0), kind = uniform(en.kind);
     const uint32_t q0 = qn & 1;
     if (kind == kFew) {
@@ -830,9 +830,9 @@ __device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D>& 
   // this key's 2 bytes of row r: r * 128 + ((chunk ^ r) & 7) * 16 + ... in the 64-key half
   uint8_t* const pw = sm.q[st.qn & 1] + few_p_offset(x) + (key >> 6) * (kFewRows * 128) + (key & 7) * 2;
   const int chunk = (key & 63) >> 3;
-  const int tokn = (en.rows - 1) / p.G;
-  const int f1 = en.rows < R ? 0 : (en.pos0 + 1) >> 7;  // [f0, f1): every row sees every key
-  const int f0 = p.window > 0 ? (max(0, en.pos0 + tokn - p.window + 1) + 127) >> 7 : 0;
+  const int rows = en.n * p.G;
+  const int f1 = rows < R ? 0 : (en.pos0 + 1) >> 7;  // [f0, f1): every row sees every key
+  const int f0 = p.window > 0 ? (max(0, en.pos0 + en.n - p.window) + 127) >> 7 : 0;
   float m[R], l[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) { m[r] = -INFINITY; l[r] = 0.f; }
@@ -851,7 +851,7 @@ __device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D>& 
       int t = en.pos0, g = 0;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        if (r >= en.rows || k > t || (p.window > 0 && k <= t - p.window)) y[r] = -INFINITY;
+        if (r >= rows || k > t || (p.window > 0 && k <= t - p.window)) y[r] = -INFINITY;
         if (++g == p.G) { g = 0; ++t; }
       }
     }
@@ -964,12 +964,12 @@ __device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D>& 
   if (whole) {
 #pragma unroll
     for (int r = 0; r < R; ++r)
-      if ((r & 1) == x && r < en.rows) emit(r, v[r] * (l[r] == 0.f ? 0.f : 1.f / l[r]), m[r], l[r]);
+      if ((r & 1) == x && r < rows) emit(r, v[r] * (l[r] == 0.f ? 0.f : 1.f / l[r]), m[r], l[r]);
   } else {
     const Records<D> mine = records<D>(p, blockIdx.x, en.first == static_cast<int>(blockIdx.x), x);
 #pragma unroll
     for (int r = 0; r < R; ++r)
-      if ((r & 1) == x && r < en.rows) {
+      if ((r & 1) == x && r < rows) {
         if (key < D) __stcg(reinterpret_cast<float*>(mine.at) + r * D + key, v[r]);
         if (key == r) __stcg(mine.ml() + r, make_float2(m[r], l[r]));
       }
@@ -989,7 +989,7 @@ __device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D>& 
           for (int r = 0; r < kR; ++r) {
             z[r][q] = make_float2(-INFINITY, 0.f);
             o[r][q] = 0.f;
-            if (q0 + q < en.pieces && 2 * r + x < en.rows) {
+            if (q0 + q < en.pieces && 2 * r + x < rows) {
               z[r][q] = __ldcg(rec.ml() + 2 * r + x);
               if (key < D) o[r][q] = __ldcg(reinterpret_cast<const float*>(rec.at) + (2 * r + x) * D + key);
             }
@@ -1014,7 +1014,7 @@ __device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D>& 
       }
 #pragma unroll
       for (int r = 0; r < kR; ++r)
-        if (2 * r + x < en.rows) emit(2 * r + x, ll[r] == 0.f ? 0.f : oo[r] * (1.f / ll[r]), mm[r], ll[r]);
+        if (2 * r + x < rows) emit(2 * r + x, ll[r] == 0.f ? 0.f : oo[r] * (1.f / ll[r]), mm[r], ll[r]);
     }
   }
   // both sides have read both accumulators and (m, l) before either goes on
@@ -1052,18 +1052,16 @@ __device__ __forceinline__ void transpose4(uint4 (&w)[4], int q) {
   swap(w[1], w[3], q & 2, 2);
 }
 
-// Weights exp2(c u + nb) of 64 keys as 16-bit pairs, and their sums before rounding.
-template <bool kFp16>
-__device__ __forceinline__ void weights(const uint32_t (&u0)[32], const uint32_t (&u1)[32], float c, float nb, uint32_t (&w)[32],
-                                        float2 (&acc)[4]) {
+// Weights exp2(c u + nb) of 32 keys as 16-bit pairs, and their sums before rounding.
+template <bool kFp16, int N>
+__device__ __forceinline__ void weights(const uint32_t (&u)[32], float c, float nb, uint32_t (&w)[N], int o, float2 (&acc)[4]) {
   const float2 cc = make_float2(c, c), bb = make_float2(nb, nb);
 #pragma unroll
-  for (int q = 0; q < 32; ++q) {
-    const uint32_t a = q < 16 ? u0[2 * q] : u1[2 * q - 32], b = q < 16 ? u0[2 * q + 1] : u1[2 * q - 31];
-    const float2 y = ffma2(make_float2(__uint_as_float(a), __uint_as_float(b)), cc, bb);
+  for (int q = 0; q < 16; ++q) {
+    const float2 y = ffma2(make_float2(__uint_as_float(u[2 * q]), __uint_as_float(u[2 * q + 1])), cc, bb);
     const float2 z = make_float2(ex2_approx(y.x), ex2_approx(y.y));
     acc[q & 3] = fadd2(acc[q & 3], z);
-    w[q] = pack2<kFp16>(z.x, z.y);
+    w[o + q] = pack2<kFp16>(z.x, z.y);
   }
 }
 
@@ -1081,7 +1079,7 @@ __device__ __forceinline__ float max32u(const uint32_t (&u)[32]) {
 
 template <int D, bool kFp16>
 __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>& sm, uint32_t tmem, int x, const Entry& en,
-                                          SideState& st) {
+                                          SideState& st, int i0) {
   const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
   const int r = warp * 32 + lane;  // row of the side = TMEM lane
   const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
@@ -1091,16 +1089,17 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
   constexpr float kUp = kFp16 ? 7.f : 0.f;
   const bool paired = en.kind == kPaired;
   const int base = paired ? 0 : x * p.P * p.G;  // first row of the side in the unit
-  const int rows = min(en.rows - base, p.P * p.G);
+  const int rows = min(en.n * p.G - base, p.P * p.G);
   const bool valid = r < rows;
   const bool work = warp * 32 < rows;  // the warp has rows
-  const int i = (base + r) / p.G;      // token of the row
+  const int side0 = paired ? 0 : x * p.P;  // the side's first token, and its last
+  const int side1 = side0 + min(en.n - side0, p.P) - 1;
+  const int i = side0 + i0;  // token of the row
   const int t = en.pos0 + i;
   const int lo = p.window > 0 ? t - p.window + 1 : 0;
   // tiles [f0, f1) need no mask: every row of the side sees all of their keys
-  const int tok0 = base / p.G, tokn = (base + rows - 1) / p.G;
-  const int f1 = (en.pos0 + tok0 + 1) >> 7;
-  const int f0 = p.window > 0 ? (max(0, en.pos0 + tokn - p.window + 1) + 127) >> 7 : 0;
+  const int f1 = (en.pos0 + side0 + 1) >> 7;
+  const int f0 = p.window > 0 ? (max(0, en.pos0 + side1 - p.window + 1) + 127) >> 7 : 0;
   float m = -INFINITY, l = 0.f;
   const int step = paired ? 2 : 1;
   const int first = en.t0 + (paired ? x : 0);
@@ -1108,66 +1107,89 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
     st.ok = st.ok && attn_wait_warp(sm, &sm.sfull[x], st.sph, p.status);
     st.sph ^= 1;
     tc_fence_after();
+    // weights stored: half h of the tile's is complete
+    auto hand_over = [&](int h) {
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      mbar_arrive_elect(&sm.pfull[x][h]);
+    };
     if (work) {
-      uint32_t u[4][32];
-      tmem_ld64_async(ts, u[0], u[1]);
-      tmem_wait64(u[0], u[1]);
-      tmem_ld64_async(ts + 64, u[2], u[3]);
       const bool edge = j < f0 || j >= f1;
-      if (edge) {
-#pragma unroll
-        for (int q = 0; q < 2; ++q) mask_keys(u[q], lo - j * kRows - 32 * q, t - j * kRows - 32 * q);
+      bool slow = edge || j == first;
+      if (!slow) {
+        // the first half's weights by the maximum so far, while the tile's own is being formed
+        uint32_t u[2][32], w[32];
+        float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        tmem_ld64_async(ts, u[0], u[1]);
+        tmem_wait64(u[0], u[1]);
+        const float nb = kUp - finite_or_0(m);
+        weights<kFp16>(u[0], c, nb, w, 0, acc);
+        weights<kFp16>(u[1], c, nb, w, 16, acc);
+        float top = fmaxf(max32u(u[0]), max32u(u[1]));
+        tmem_ld64_async(ts + 64, u[0], u[1]);
+        tmem_wait64(u[0], u[1]);
+        top = fmaxf(top, fmaxf(max32u(u[0]), max32u(u[1]))) * c;
+        slow = __any_sync(0xffffffffu, valid && top > m + kRaise);
+        if (!slow) {
+          tmem_st32(ts, w);
+          hand_over(0);
+          weights<kFp16>(u[0], c, nb, w, 0, acc);
+          weights<kFp16>(u[1], c, nb, w, 16, acc);
+          tmem_st32(ts + 32, w);
+          const float2 sum = fadd2(fadd2(acc[0], acc[1]), fadd2(acc[2], acc[3]));
+          l += sum.x + sum.y;
+          hand_over(1);
+        }
       }
-      float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-      // the first half's weights by the maximum so far, while the tile's is being formed
-      uint32_t w[32];
-      if (j != first) weights<kFp16>(u[0], u[1], c, kUp - finite_or_0(m), w, acc);
-      float top = fmaxf(max32u(u[0]), max32u(u[1]));
-      tmem_wait64(u[2], u[3]);
-      if (edge) {
-#pragma unroll
-        for (int q = 2; q < 4; ++q) mask_keys(u[q], lo - j * kRows - 32 * q, t - j * kRows - 32 * q);
-      }
-      top = fmaxf(top, fmaxf(max32u(u[2]), max32u(u[3]))) * c;
-      const bool raise = valid && (j == first || top > m + kRaise);
-      if (__any_sync(0xffffffffu, raise)) {
-        const float f = raise ? ex2_approx(m - finite_or_0(top)) : 1.f;
-        if (raise) { m = top; l *= f; }
-        if (j != first) {
-          // S of this tile is complete, so is O += P V of the side's tile before it, and the next waits for us
+      if (slow) {
+        // an edge of the rows' keys, the first tile, or a maximum to raise: in 32-key pieces
+        // and two passes, which keep the code short (the instruction cache is the limit of short units)
+        float top = -INFINITY;
 #pragma unroll 1
-          for (int q = 0; q < D; q += 16) {
-            uint32_t o[16];
-            tmem_ld_cols<16>(tmem + lanes + o_col<D>(x) + q, o);
+        for (int q = 0; q < 4; ++q) {
+          uint32_t u[32];
+          tmem_ld32_async(ts + 32 * q, u);
+          tmem_wait32(u);
+          if (edge) mask_keys(u, lo - j * kRows - 32 * q, t - j * kRows - 32 * q);
+          top = fmaxf(top, max32u(u));
+        }
+        top *= c;
+        const bool raise = valid && (j == first || top > m + kRaise);
+        if (__any_sync(0xffffffffu, raise)) {
+          const float f = raise ? ex2_approx(m - finite_or_0(top)) : 1.f;
+          if (raise) { m = top; l *= f; }
+          if (j != first) {
+            // S of this tile is complete, so is O += P V of the side's tile before it, and the next waits for us
+#pragma unroll 1
+            for (int q = 0; q < D; q += 16) {
+              uint32_t o[16];
+              tmem_ld_cols<16>(tmem + lanes + o_col<D>(x) + q, o);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-            tmem_st_cols<16>(tmem + lanes + o_col<D>(x) + q, o);
+              for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+              tmem_st_cols<16>(tmem + lanes + o_col<D>(x) + q, o);
+            }
           }
         }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) acc[q] = make_float2(0.f, 0.f);
-        weights<kFp16>(u[0], u[1], c, kUp - finite_or_0(m), w, acc);
+        mend_v<D>(p, sm, en, j, st);
+        float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll 1
+        for (int q = 0; q < 4; ++q) {
+          uint32_t u[32], w[16];
+          tmem_ld32_async(ts + 32 * q, u);
+          tmem_wait32(u);
+          if (edge) mask_keys(u, lo - j * kRows - 32 * q, t - j * kRows - 32 * q);
+          weights<kFp16>(u, c, kUp - finite_or_0(m), w, 0, acc);
+          tmem_st_cols<16>(ts + 16 * q, w);
+          if (q & 1) hand_over(q >> 1);
+        }
+        const float2 sum = fadd2(fadd2(acc[0], acc[1]), fadd2(acc[2], acc[3]));
+        l += sum.x + sum.y;
       }
-      mend_v<D>(p, sm, en, j, st);
-      tmem_st32(ts, w);
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      mbar_arrive_elect(&sm.pfull[x][0]);
-      weights<kFp16>(u[2], u[3], c, kUp - finite_or_0(m), w, acc);
-      tmem_st32(ts + 32, w);
-      const float2 sum = fadd2(fadd2(acc[0], acc[1]), fadd2(acc[2], acc[3]));
-      l += sum.x + sum.y;
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      mbar_arrive_elect(&sm.pfull[x][1]);
     } else {
       mend_v<D>(p, sm, en, j, st);
-      tc_fence_before();
-      __syncwarp();
-#pragma unroll
-      for (int part = 0; part < kParts; ++part) mbar_arrive_elect(&sm.pfull[x][part]);
+      hand_over(0);
+      hand_over(1);
     }
   }
   // ---- the rows' output ----
@@ -1228,9 +1250,9 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
 #pragma unroll
         for (int k = 0; k < 32; ++k) v[k] = fmaf(__uint_as_float(o[k]), fb, v[k]);
       }
-      if (l == 0.f) {  // no key (or none with a weight): nothing to weigh
+      if (__any_sync(0xffffffffu, l == 0.f)) {  // no key (or none with a weight): nothing to weigh
 #pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] = 0.f;
+        for (int k = 0; k < 32; ++k) v[k] = l == 0.f ? 0.f : v[k];
       }
       if (whole) {
         uint4 w[4];
@@ -1318,12 +1340,13 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
 template <int D, bool kFp16>
 __device__ __forceinline__ void softmax_group(const PagedAttnParams& p, AttnSmem<D>& sm, uint32_t tmem, int x) {
   SideState st;
+  const int i0 = static_cast<int>(threadIdx.x & 127) / p.G;  // the thread's row: its token in the side
   for (uint32_t e = 0;; ++e) {
     const Entry en = take(p, sm, e);
-    if (group_any(x, en.rows == 0)) break;  // no more, or a warp's wait for the entry ran out
-    if (en.kind != kFew) row_tiles<D, kFp16>(p, sm, tmem, x, en, st);
-    else if (en.rows <= 4) few_rows<D, kFp16, 4>(p, sm, tmem, x, en, st);
-    else if (en.rows <= 8) few_rows<D, kFp16, 8>(p, sm, tmem, x, en, st);
+    if (group_any(x, en.n == 0)) break;  // no more, or a warp's wait for the entry ran out
+    if (en.kind != kFew) row_tiles<D, kFp16>(p, sm, tmem, x, en, st, i0);
+    else if (en.n * p.G <= 4) few_rows<D, kFp16, 4>(p, sm, tmem, x, en, st);
+    else if (en.n * p.G <= 8) few_rows<D, kFp16, 8>(p, sm, tmem, x, en, st);
     else few_rows<D, kFp16, 16>(p, sm, tmem, x, en, st);
     st.tiles += 2 * (en.t1 - en.t0);
   }
