@@ -38,16 +38,16 @@ namespace kvev {
 namespace {
 
 constexpr int kAttnThreads = 384;
-constexpr int kRegsAttnControl = 72, kRegsAttnSoftmax = 216;
+constexpr int kRegsAttnControl = 40, kRegsAttnSoftmax = 232;
 constexpr int kRegsAttnNeeded = 128 * kRegsAttnControl + 256 * kRegsAttnSoftmax;
 constexpr int kMaxCtas = 152;
 constexpr int kEntries = 4;         // ring of dealt entries
 // Kinds of unit, and the cost of a key tile and of a unit's start and end in each.
 enum Kind : int { kFew = 0, kPaired = 1, kFull = 2 };
 constexpr int kFewRows = 16;
-__host__ __device__ constexpr int tile_cost(int kind) { return kind == kFull ? 4 : 3; }
-__host__ __device__ constexpr int unit_cost(int kind) { return kind == kFull ? 12 : 6; }
-constexpr int kMinShare = 4;        // least cost of a share, a tile's or more: no piece of a cut unit is empty
+__host__ __device__ constexpr int tile_cost(int kind) { return kind == kFull ? 5 : 3; }
+__host__ __device__ constexpr int unit_cost(int kind) { return kind == kFull ? 16 : 8; }
+constexpr int kMinShare = 5;        // least cost of a share, a tile's or more: no piece of a cut unit is empty
 constexpr int kRows = 128;          // rows of a side
 constexpr int kParts = 2;           // halves of a tile's weights, which the second product takes as they come
 constexpr float kRaise = 8.f;       // a row's maximum is raised when a tile's is this much (log2) above it
@@ -384,11 +384,15 @@ __device__ __forceinline__ Share share_of(const PagedAttnParams& p, S& sm) {
 }
 
 // The same by one warp for up to 32 requests, with no barrier for the block: a single
-// generation at a 4K context 13.1 -> 11.3 us.
-__device__ __forceinline__ Share share_of_warp(const PagedAttnParams& p) {
+// generation at a 4K context 13.1 -> 10.4 us.
+// Lane s keeps request s and its cost for one KV head.
+__device__ __forceinline__ Share share_of_warp(const PagedAttnParams& p, Request& held, long long& held_cost) {
   const int lane = threadIdx.x & 31;
   bool bad = false;
-  const long long mine = lane < p.B ? head_cost(p, request(p, lane, &bad)) * p.H_kv : 0;
+  held = {};
+  if (lane < p.B) held = request(p, lane, &bad);
+  held_cost = head_cost(p, held);
+  const long long mine = held_cost * p.H_kv;
   if (bad && blockIdx.x == 0) atomicOr(p.status, kStatusDevice);
   long long upto = mine;
 #pragma unroll
@@ -409,9 +413,19 @@ __device__ __forceinline__ Share share_of_warp(const PagedAttnParams& p) {
 
 // Warp 2: the CTA's entries in order.
 template <class S>
-__device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, const Share& sh) {
+__device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, Share sh) {
   uint32_t e = 0;
   const int lane = threadIdx.x & 31;
+  const bool short_batch = p.B <= 32;
+  Request held;
+  long long held_cost;
+  if (short_batch) sh = share_of_warp(p, held, held_cost);
+  auto get = [&](int s) {
+    if (short_batch)
+      return Request{__shfl_sync(0xffffffffu, held.c0, s), __shfl_sync(0xffffffffu, held.q, s), __shfl_sync(0xffffffffu, held.kv, s)};
+    bool bad = false;  // (said by the schedule's first pass)
+    return request(p, s, &bad);
+  };
   auto put = [&](const Entry& en) {
     if (!attn_wait_warp(sm, &sm.eempty[e % kEntries], ((e / kEntries) & 1) ^ 1, p.status)) return false;
     if (lane == 0) {
@@ -423,11 +437,10 @@ __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, const Shar
     return true;
   };
   if (sh.x0 < sh.x1) {
-    bool bad = false;
     int s = sh.s;
-    Request r = request(p, s, &bad);
+    Request r = get(s);
     long long a = sh.before;  // cost before the unit
-    const long long hc = head_cost(p, r);
+    const long long hc = short_batch ? __shfl_sync(0xffffffffu, held_cost, s) : head_cost(p, r);
     int h = static_cast<int>(divide(sh.x0 - a, hc)), m = 0;
     a += h * hc;
     Unit u = unit_of(p, r, m);
@@ -465,7 +478,7 @@ __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, const Shar
         m = 0;
         if (++h == p.H_kv) {
           h = 0;
-          do r = request(p, ++s, &bad);
+          do r = get(++s);
           while (r.q == 0);
         }
       }
@@ -509,6 +522,14 @@ __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>&
     const int kind = uniform(en.kind), h = uniform(en.h), t0 = uniform(en.t0), t1 = uniform(en.t1);
     const int tok0 = uniform(en.tok0), klo = uniform(en.klo), khi = uniform(en.khi);
     const bool one = uniform(en.n) == 1;
+    // ---- pages ----
+    // lane i holds the page of the tile's box i: its entry of the table, read three tiles ahead and checked when used
+    const int* row = p.table + static_cast<long long>(uniform(en.s)) * p.max_pages;
+    auto page_of = [&](int t) {
+      const int k = t * kRows + (lane << box_shift);
+      return t < t1 && lane < boxes && k < khi && k + (1 << box_shift) > klo ? __ldg(row + (k >> p.page_shift)) : INT_MAX;
+    };
+    int r0 = page_of(t0), r1 = page_of(t0 + 1), r2 = page_of(t0 + 2);
     // ---- Q tiles ----
     const int sides = kind == kFull ? 2 : 1;
     for (int x = 0; ok && x < sides; ++x) {
@@ -522,13 +543,6 @@ __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>&
                           smem_u32(&sm.qfull[qs]));
       ++qn;
     }
-    // ---- pages ----
-    // lane i holds the page of the tile's box i: its entry of the table, read three tiles ahead and checked when used
-    const int* row = p.table + static_cast<long long>(uniform(en.s)) * p.max_pages;
-    auto page_of = [&](int t) {
-      const int k = t * kRows + (lane << box_shift);
-      return t < t1 && lane < boxes && k < khi && k + (1 << box_shift) > klo ? __ldg(row + (k >> p.page_shift)) : INT_MAX;
-    };
     auto checked = [&](int id) {  // num_pages (loads zeros) for no page or one outside the pool
       if (static_cast<unsigned>(id) < static_cast<unsigned>(p.num_pages)) return id;
       if (id != INT_MAX) atomicOr(p.status, kStatusDevice);
@@ -559,7 +573,6 @@ __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>&
       if (++st == S::kStages) { st = 0; ph ^= 1; }
     };
     const int A = kind == kFull ? 1 : 2;
-    int r0 = page_of(t0), r1 = page_of(t0 + 1), r2 = page_of(t0 + 2);
     int p0 = checked(r0), p1 = checked(r1);  // pages of tiles t, t + 1
     for (int a = 0; a < A && t0 + a < t1; ++a) load(&p.kmap, t0 + a, a == 0 ? p0 : p1);
     for (int t = t0; ok && t < t1; ++t) {
@@ -794,11 +807,11 @@ __device__ __forceinline__ Records<D> records(const PagedAttnParams& p, long lon
 // After the group's records of a piece are written: whether it is the last of the unit's pieces.
 template <int D>
 __device__ __forceinline__ bool arrived_last(const PagedAttnParams& p, AttnSmem<D>& sm, const Entry& en, int x, bool ok) {
-  __threadfence();
   group_sync(x);
   if ((threadIdx.x & 127) == 0) {
     int last = 0;
     if (ok) {
+      __threadfence();  // (for the whole group's records: the barrier orders them before it)
       int* cnt = p.sync + 2 * en.first + x;
       last = atomicAdd(cnt, 1) == en.pieces - 1;
       if (last) atomicExch(cnt, 0);
@@ -974,8 +987,8 @@ __device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D>& 
         if (key == r) __stcg(mine.ml() + r, make_float2(m[r], l[r]));
       }
     if (arrived_last(p, sm, en, x, st.ok)) {
-      // the side's rows together, sixteen records in flight
-      constexpr int kR = R / 2, kU = 16 / kR;
+      // the side's rows together, 32 records in flight
+      constexpr int kR = R / 2, kU = 32 / kR;
       float mm[kR], ll[kR], oo[kR];
 #pragma unroll
       for (int r = 0; r < kR; ++r) { mm[r] = -INFINITY; ll[r] = oo[r] = 0.f; }
@@ -1385,6 +1398,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) paged_attn_kernel(const __gri
     fence_barrier_init();
     fence_proxy_async();
   }
+  if (threadIdx.x == 64) {
+    for (const CUtensorMap* m : {&p.qmap1, &p.kmap, &p.vmap, &p.qmap})
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
+  }
   if (warp == 1) {
     tmem_alloc(&sm.tmem_slot, 512);
     tmem_relinquish();
@@ -1401,7 +1418,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) paged_attn_kernel(const __gri
     regs_dealloc<kRegsAttnControl>();
     if (warp == 0) load_warp<D>(p, sm);
     if (warp == 1) mma_warp<D, kFp16>(p, sm, tmem);
-    if (warp == 2) deal(p, sm, p.B > 32 ? sh : share_of_warp(p));
+    if (warp == 2) deal(p, sm, sh);
     __syncwarp();
   } else {
     regs_alloc<kRegsAttnSoftmax>();
