@@ -38,7 +38,7 @@ namespace kvev {
 namespace {
 
 constexpr int kAttnThreads = 384;
-constexpr int kRegsAttnControl = 40, kRegsAttnSoftmax = 232;
+constexpr int kRegsAttnControl = 56, kRegsAttnSoftmax = 224;
 constexpr int kRegsAttnNeeded = 128 * kRegsAttnControl + 256 * kRegsAttnSoftmax;
 constexpr int kMaxCtas = 152;
 constexpr int kEntries = 4;         // ring of dealt entries
@@ -47,7 +47,9 @@ enum Kind : int { kFew = 0, kPaired = 1, kFull = 2 };
 constexpr int kFewRows = 16;
 __host__ __device__ constexpr int tile_cost(int kind) { return kind == kFull ? 5 : 3; }
 __host__ __device__ constexpr int unit_cost(int kind) { return kind == kFull ? 16 : 8; }
-constexpr int kMinShare = 5;        // least cost of a share, a tile's or more: no piece of a cut unit is empty
+// Least cost of a share (a tile's or more: no piece of a cut unit is empty).  Records of
+// more than a few rows are up to 64 KB a side and piece, and one CTA merges them.
+constexpr int kMinShare = 5, kMinShareRows = 20;
 constexpr int kRows = 128;          // rows of a side
 constexpr int kParts = 2;           // halves of a tile's weights, which the second product takes as they come
 constexpr float kRaise = 8.f;       // a row's maximum is raised when a tile's is this much (log2) above it
@@ -402,7 +404,8 @@ __device__ __forceinline__ Share share_of_warp(const PagedAttnParams& p, Request
   }
   const long long total = __shfl_sync(0xffffffffu, upto, 31);
   Share r;
-  r.share = max(static_cast<long long>(kMinShare), divide(total + gridDim.x - 1, gridDim.x));
+  const bool rows = __any_sync(0xffffffffu, held.q * p.G > kFewRows);
+  r.share = max(static_cast<long long>(rows ? kMinShareRows : kMinShare), divide(total + gridDim.x - 1, gridDim.x));
   r.x0 = min(total, r.share * blockIdx.x);
   r.x1 = min(total, r.x0 + r.share);
   const uint32_t here = __ballot_sync(0xffffffffu, mine > 0 && upto - mine <= r.x0 && r.x0 < upto);
@@ -1559,7 +1562,7 @@ extern "C" int kvev_paged_attention(const kvev_paged_cache* cache, const void* q
   p.page_shift = view.page_shift;
   p.num_pages = view.num_pages;
   p.max_pages = max_pages;
-  p.window = window;
+  p.window = window < static_cast<int64_t>(max_pages) * cache->page_size ? window : 0;  // (a window as long as any sequence is none)
   p.scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt(static_cast<float>(d))) * 1.4426950408889634f;
   p.status = device_status;
   p.sync = static_cast<int*>(workspace);

@@ -38,6 +38,22 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
+# Scratch of the attention calls on a stream, (device, stream) -> (pointer, bytes, tensor): calls on a stream
+# follow one another, whatever layer they are for, so they share it.
+_workspaces: dict = {}
+
+
+def _workspace(device: int, stream: int):
+    ws = _workspaces.get((device, stream))
+    if ws is None:
+        n = kvev.kvev_paged_attention_workspace(1, 1, 128)  # what the largest call needs
+        with torch.cuda.device(device), torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
+            t = torch.empty(n, dtype=torch.uint8, device="cuda")
+            t[:kvev.PAGED_SYNC_BYTES].zero_()
+        ws = _workspaces[device, stream] = (t.data_ptr(), n, t)
+    return ws
+
+
 def _table(block_table) -> int:
     _need(block_table.dim() == 2 and block_table.is_cuda, "block_table: int32 [requests][pages] on a GPU")
     return _int32(block_table, block_table.numel(), "block_table")
@@ -140,7 +156,6 @@ class PagedCache:
         self._desc, self._device = C.addressof(self.desc), K.device.index or 0
         self.device_status = torch.zeros(1, dtype=_I32, device=K.device)
         self._status = self.device_status.data_ptr()
-        self._workspaces = {}
 
     @classmethod
     def empty(cls, num_pages, page_size, H_kv, d, block_table, dtype=torch.bfloat16, heads_first=False):
@@ -171,18 +186,10 @@ class PagedCache:
         if rc:
             raise kvev.KvevError(rc, "kvev_paged_write")
 
-    def workspace(self, H_q, stream=None):
-        """The scratch of attention calls on a stream (one per stream: overlapping calls may not share it)."""
-        return self._workspace(H_q, _raw_stream(self._device) if stream is None else stream.cuda_stream)[2]
-
-    def _workspace(self, H_q, stream: int):
-        ws = self._workspaces.get((H_q, stream))
-        if ws is None:
-            n = kvev.kvev_paged_attention_workspace(H_q, self.H_kv, self.d)
-            t = torch.empty(n, dtype=torch.uint8, device=self.K.device)
-            t[:kvev.PAGED_SYNC_BYTES].zero_()
-            ws = self._workspaces[H_q, stream] = (t.data_ptr(), n, t)
-        return ws
+    def workspace(self, H_q: int | None = None, stream=None):
+        """The scratch that attention calls on a stream use, made at the first of them (before a capture of
+        the stream, let one call or this one make it): all layers' calls on a stream share one."""
+        return _workspace(self._device, _raw_stream(self._device) if stream is None else stream.cuda_stream)[2]
 
     def attention(self, q, cu, kv_lens, *, scale=0.0, window=0, out=None, lse=None, workspace=None, stream=None):
         """Causal attention of the new tokens' queries q [T][H_q][d] (request s: rows cu[s]..cu[s+1], the last of
@@ -205,7 +212,7 @@ class PagedCache:
                 raise ValueError("lse: contiguous float32 [T][H_q]")
             lse_ptr = lse.data_ptr()
         at = _raw_stream(self._device) if stream is None else stream.cuda_stream
-        ws = self._workspace(H_q, at) if workspace is None else (workspace.data_ptr(), workspace.numel())
+        ws = _workspace(self._device, at) if workspace is None else (workspace.data_ptr(), workspace.numel())
         rc = kvev.load().kvev_paged_attention(
             self._desc, q.data_ptr(), sq[0], sq[1], _int32(cu, B + 1, "cu"), _int32(kv_lens, B, "kv_lens"), self._table,
             self.max_pages, B, T, H_q, scale, window, out.data_ptr(), so[0], so[1], lse_ptr, ws[0], ws[1], self._status, at)
