@@ -2,7 +2,9 @@
 
 ``libkvev.so``        the eviction library (C ABI of ``include/kvev.h``);
 ``libkvev_synth.so``  the device-side synthetic input generator
-                      (C ABI of ``include/kvev_synth.h``).
+                      (C ABI of ``include/kvev_synth.h``);
+``kvev_paged_bind.so`` the extension module through which ``paged.py`` calls ``libkvev.so``
+                      with torch tensors (host code only).
 
 Translation units are compiled in parallel with nvcc, then linked; a unit is
 rebuilt only when it or a header it includes changed.
@@ -13,6 +15,7 @@ import concurrent.futures as cf
 import glob
 import os
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -29,6 +32,38 @@ LIBS = {
                    "paged.cu", "paged_attn.cu"],
     "libkvev_synth.so": ["synth.cu"],
 }
+
+
+BIND = "kvev_paged_bind.so"
+CXX = os.environ.get("CXX", "g++")
+
+
+def _bind_flags() -> tuple[list[str], list[str]]:
+    """(compiler, linker) flags of the extension module: Python's, torch's and CUDA's headers and libraries."""
+    import importlib.util
+    torch_dir = os.path.dirname(importlib.util.find_spec("torch").origin)  # (without importing it)
+    cuda = os.path.dirname(os.path.dirname(NVCC))
+    libs = os.path.join(torch_dir, "lib")
+    return (["-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I", os.path.join(torch_dir, "include"),
+             "-I", os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
+             "-I", sysconfig.get_paths()["include"], "-I", os.path.join(cuda, "include"), "-I", os.path.join(ROOT, "include")],
+            ["-L", libs, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", f"-Wl,-rpath,{libs}",
+             "-L", LIBDIR, "-l:libkvev.so", "-Wl,-rpath,$ORIGIN"])
+
+
+def _run(cmd: list[str], what: str):
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{what}:\n{r.stdout}\n{r.stderr}")
+
+
+def _compile_bind() -> str:
+    src, obj = os.path.join(CSRC, "paged_bind.cpp"), os.path.join(OBJDIR, "paged_bind.cpp.o")
+    if _stale(obj, [src] + _headers()):
+        tmp = obj + f".tmp{os.getpid()}"
+        _run([CXX, *_bind_flags()[0], "-c", src, "-o", tmp], f"{CXX} failed for {src}")
+        os.replace(tmp, obj)
+    return obj
 
 
 def _headers():
@@ -61,7 +96,9 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> dict[str, st
     out = {}
     srcs = sorted({s for v in LIBS.values() for s in v})
     with cf.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 4)) as ex:
+        bind = ex.submit(_compile_bind)
         objs = dict(zip(srcs, ex.map(lambda s: _compile(os.path.join(CSRC, s), extra), srcs)))
+        bind_obj = bind.result()
     for lib, units in LIBS.items():
         path = os.path.join(LIBDIR, lib)
         deps = [objs[u] for u in units]
@@ -75,6 +112,14 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> dict[str, st
         if verbose:
             print("built", path)
         out[lib] = path
+    path = os.path.join(LIBDIR, BIND)
+    if _stale(path, [bind_obj, out["libkvev.so"]]):
+        tmp = path + f".tmp{os.getpid()}"
+        _run([CXX, "-shared", "-o", tmp, bind_obj, *_bind_flags()[1]], f"link failed for {BIND}")
+        os.replace(tmp, path)
+    if verbose:
+        print("built", path)
+    out[BIND] = path
     return out
 
 

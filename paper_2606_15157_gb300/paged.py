@@ -7,11 +7,13 @@ tables and slots stay on the device throughout.  Argument checks raise ``ValueEr
 or ``KvevError`` (what the library refuses).
 
 These are calls of a few microseconds on the device, made for every layer of every token: the checks
-here are a handful of attribute reads, the stream is read as a number.
+and the calls themselves are in the extension module ``kvev_paged_bind`` (``csrc/paged_bind.cpp``).
 """
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
+import os
 
 import torch
 
@@ -19,23 +21,27 @@ from . import kvev
 
 _DTYPES = {torch.bfloat16: kvev.BF16, torch.float16: kvev.FP16}
 _I32 = torch.int32
+_bind_module = None
+
+
+def _bind():
+    """The extension module (loaded once).  Raises if it is missing."""
+    global _bind_module
+    if _bind_module is None:
+        kvev.load()
+        path = os.path.join(os.path.dirname(kvev.LIB_PATH), "kvev_paged_bind.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it with __graft_entry__.build()")
+        spec = importlib.util.spec_from_file_location("kvev_paged_bind", path)
+        m = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(m)
+        _bind_module = m
+    return _bind_module
 
 
 def _need(ok: bool, what: str):
     if not ok:
         raise ValueError(what)
-
-
-def _int32(t, n: int, what: str) -> int:
-    """Device pointer of a contiguous int32 tensor of n elements."""
-    if t.dtype is not _I32 or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous int32 tensor of {n} elements")
-    return t.data_ptr()
-
-
-# The current stream of a device as a number; torch.cuda.current_stream() makes an object first (2.8 us).
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
-    lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 # Scratch of the attention calls on a stream, (device, stream) -> (pointer, bytes, tensor): calls on a stream
@@ -55,8 +61,9 @@ def _workspace(device: int, stream: int):
 
 
 def _table(block_table) -> int:
-    _need(block_table.dim() == 2 and block_table.is_cuda, "block_table: int32 [requests][pages] on a GPU")
-    return _int32(block_table, block_table.numel(), "block_table")
+    _need(block_table.dim() == 2 and block_table.is_cuda and block_table.dtype is _I32 and block_table.is_contiguous(),
+          "block_table: contiguous int32 [requests][pages] on a GPU")
+    return block_table.data_ptr()
 
 
 def _strides(t) -> tuple:
@@ -85,33 +92,29 @@ class PagePool:
         self.num_pages, self.page_size = num_pages, page_size
         self.block_table, self._table = block_table, _table(block_table)
         self.max_requests, self.max_pages = block_table.shape
-        self.free, self._free = free, _int32(free, num_pages, "free")
+        _need(free.dtype is _I32 and free.is_contiguous() and free.numel() == num_pages and free.device == dev,
+              "free: contiguous int32 [num_pages] beside the block table")
+        self.free = free
         state = torch.zeros(2, dtype=_I32, device=dev)
         self.free_count = state[:1] if free_count is None else free_count
         self.device_status = state[1:]
-        self._status, self._device = self.device_status.data_ptr(), dev.index or 0
+        self._call = (page_size, num_pages, free.data_ptr(), self._table, self.max_requests, self.max_pages,
+                      self.device_status.data_ptr(), dev.index or 0)
+        self._lib = _bind()
 
     def tables(self, lens, new_lens, T: int, *, kv_lens=None, cu=None, slots=None, positions=None, granted=None,
                free_count=None, free_count_out=None, stream=None):
         """Pages for the new tokens, and where each goes: (kv_lens, cu, slots, positions, granted).
         T: rows of the new tokens' tensors.  By default the pool's count is updated in place and the
         outputs are new tensors; ``kv_lens=lens`` updates the lengths in place."""
-        B = lens.numel()
-        if B > self.max_requests:
-            raise ValueError("more requests than the block table has rows")
         if kv_lens is None or cu is None or slots is None or positions is None or granted is None:
+            B = lens.numel()
             e = lambda t, n: torch.empty(n, dtype=_I32, device=lens.device) if t is None else t
             kv_lens, cu, slots, positions, granted = e(kv_lens, B), e(cu, B + 1), e(slots, T), e(positions, T), e(granted, B)
         if free_count is None:
             free_count = self.free_count
-        if free_count_out is None:
-            free_count_out = free_count
-        rc = kvev.load().kvev_paged_tables(
-            _int32(lens, B, "lens"), _int32(new_lens, B, "new_lens"), B, self.page_size, self.num_pages, self._free,
-            _int32(free_count, 1, "free_count"), self._table, self.max_pages, T, _int32(kv_lens, B, "kv_lens"),
-            _int32(cu, B + 1, "cu"), _int32(slots, T, "slots"), _int32(positions, T, "positions"),
-            _int32(granted, B, "granted"), _int32(free_count_out, 1, "free_count_out"), self._status,
-            _raw_stream(self._device) if stream is None else stream.cuda_stream)
+        rc = self._lib.tables(*self._call, None if stream is None else stream.cuda_stream, lens, new_lens, T, kv_lens, cu, slots,
+                              positions, granted, free_count, free_count if free_count_out is None else free_count_out)
         if rc:
             raise kvev.KvevError(rc, "kvev_paged_tables")
         return kv_lens, cu, slots, positions, granted
@@ -119,20 +122,12 @@ class PagePool:
     def release(self, lens, done, *, lens_out=None, free_count=None, free_count_out=None, stream=None):
         """The pages of requests with done != 0 go back; returns the lengths, 0 for those (by default
         ``lens`` itself and the pool's count are updated in place)."""
-        B = lens.numel()
-        if B > self.max_requests:
-            raise ValueError("more requests than the block table has rows")
         if lens_out is None:
             lens_out = lens
         if free_count is None:
             free_count = self.free_count
-        if free_count_out is None:
-            free_count_out = free_count
-        rc = kvev.load().kvev_paged_release(
-            _int32(lens, B, "lens"), _int32(done, B, "done"), B, self.page_size, self.num_pages, self._table, self.max_pages,
-            self._free, _int32(free_count, 1, "free_count"), _int32(lens_out, B, "lens_out"),
-            _int32(free_count_out, 1, "free_count_out"), self._status,
-            _raw_stream(self._device) if stream is None else stream.cuda_stream)
+        rc = self._lib.release(*self._call, None if stream is None else stream.cuda_stream, lens, done, lens_out, free_count,
+                               free_count if free_count_out is None else free_count_out)
         if rc:
             raise kvev.KvevError(rc, "kvev_paged_release")
         return lens_out
@@ -153,9 +148,12 @@ class PagedCache:
         self.dtype = K.dtype
         self.desc = kvev.PagedCacheDesc(K.data_ptr(), V.data_ptr(), *_strides(K)[:3], pages, page, self.H_kv, self.d,
                                         _DTYPES[K.dtype])
-        self._desc, self._device = C.addressof(self.desc), K.device.index or 0
+        self._device = K.device.index or 0
+        _need(block_table.device == K.device == V.device, "K, V and block_table: one GPU")
         self.device_status = torch.zeros(1, dtype=_I32, device=K.device)
-        self._status = self.device_status.data_ptr()
+        self._call = (C.addressof(self.desc), self._table, self.max_requests, self.max_pages, self.device_status.data_ptr(),
+                      self._device)
+        self._lib = _bind()
 
     @classmethod
     def empty(cls, num_pages, page_size, H_kv, d, block_table, dtype=torch.bfloat16, heads_first=False):
@@ -165,73 +163,32 @@ class PagedCache:
         K, V = x.transpose(2, 3) if heads_first else x
         return cls(K, V, block_table)
 
-    def _rows(self, t, shape, what) -> tuple:
-        """(token stride, head stride) of [T][H][d] rows of the cache's type."""
-        if len(shape) != 3 or t.dtype is not self.dtype or shape[2] != self.d:
-            raise ValueError(f"{what}: [tokens][heads][{self.d}] of the cache's type")
-        st = _strides(t)
-        if st[2] != 1:
-            raise ValueError(f"{what}: the last dimension is contiguous")
-        return st
-
     def write(self, k, v, slots, stream=None):
         """k, v [T][H_kv][d] of equal strides into the slots (int32 [T], negative: left out)."""
-        shape = k.shape
-        st = self._rows(k, shape, "k")
-        if shape[1] != self.H_kv or v.shape != shape or self._rows(v, shape, "v") != st:
-            raise ValueError(f"k, v: [tokens][{self.H_kv}][{self.d}] of equal strides")
-        rc = kvev.load().kvev_paged_write(
-            self._desc, k.data_ptr(), v.data_ptr(), st[0], st[1], _int32(slots, shape[0], "slots"), shape[0], self._status,
-            _raw_stream(self._device) if stream is None else stream.cuda_stream)
+        rc = self._lib.write(*self._call, None if stream is None else stream.cuda_stream, k, v, slots)
         if rc:
             raise kvev.KvevError(rc, "kvev_paged_write")
 
     def workspace(self, H_q: int | None = None, stream=None):
         """The scratch that attention calls on a stream use, made at the first of them (before a capture of
         the stream, let one call or this one make it): all layers' calls on a stream share one."""
-        return _workspace(self._device, _raw_stream(self._device) if stream is None else stream.cuda_stream)[2]
+        return _workspace(self._device, self._lib.current_stream(self._device) if stream is None else stream.cuda_stream)[2]
 
     def attention(self, q, cu, kv_lens, *, scale=0.0, window=0, out=None, lse=None, workspace=None, stream=None):
         """Causal attention of the new tokens' queries q [T][H_q][d] (request s: rows cu[s]..cu[s+1], the last of
         its kv_lens[s] positions).  lse: fp32 [T][H_q] for the rows' log-sum-exp.  Returns out."""
-        shape = q.shape
-        sq = self._rows(q, shape, "q")
-        T, H_q, _ = shape
-        B = kv_lens.numel()
-        if B > self.max_requests:
-            raise ValueError("more requests than the block table has rows")
         if out is None:
-            out = torch.empty(shape, dtype=q.dtype, device=q.device)
-        elif out.shape != shape:
-            raise ValueError("out: q's shape")
-        so = self._rows(out, shape, "out")
-        if lse is None:
-            lse_ptr = None
-        else:
-            if lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.shape != shape[:2]:
-                raise ValueError("lse: contiguous float32 [T][H_q]")
-            lse_ptr = lse.data_ptr()
-        at = _raw_stream(self._device) if stream is None else stream.cuda_stream
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        at = self._lib.current_stream(self._device) if stream is None else stream.cuda_stream
         ws = _workspace(self._device, at) if workspace is None else (workspace.data_ptr(), workspace.numel())
-        rc = kvev.load().kvev_paged_attention(
-            self._desc, q.data_ptr(), sq[0], sq[1], _int32(cu, B + 1, "cu"), _int32(kv_lens, B, "kv_lens"), self._table,
-            self.max_pages, B, T, H_q, scale, window, out.data_ptr(), so[0], so[1], lse_ptr, ws[0], ws[1], self._status, at)
+        rc = self._lib.attention(*self._call, at, q, cu, kv_lens, out, lse, scale, window, ws[0], ws[1])
         if rc:
             raise kvev.KvevError(rc, "kvev_paged_attention")
         return out
 
     def gather(self, lens, out_K, out_V, stream=None):
         """The first lens[s] tokens of every request into out_K, out_V [B][H_kv][S_cap][d] (contiguous)."""
-        B, shape = lens.numel(), out_K.shape
-        if (len(shape) != 4 or shape[0] != B or shape[1] != self.H_kv or shape[3] != self.d or out_V.shape != shape
-                or out_K.dtype is not self.dtype or out_V.dtype is not self.dtype
-                or not out_K.is_contiguous() or not out_V.is_contiguous()):
-            raise ValueError(f"out_K, out_V: contiguous [{B}][{self.H_kv}][S_cap][{self.d}] of the cache's type")
-        if B > self.max_requests:
-            raise ValueError("more requests than the block table has rows")
-        rc = kvev.load().kvev_paged_gather(
-            self._desc, self._table, self.max_pages, _int32(lens, B, "lens"), B, shape[2], out_K.data_ptr(), out_V.data_ptr(),
-            self._status, _raw_stream(self._device) if stream is None else stream.cuda_stream)
+        rc = self._lib.gather(*self._call, None if stream is None else stream.cuda_stream, lens, out_K, out_V)
         if rc:
             raise kvev.KvevError(rc, "kvev_paged_gather")
 

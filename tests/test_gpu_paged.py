@@ -431,3 +431,55 @@ def test_chunks_in_turn_equal_the_prompt_in_one(paged):
     assert c.status() == 0 and int(pool.device_status) == 0
     pool.release(lens, ints([1, 1, 1]))
     assert host(pool.free_count) == [100] and sorted(host(pool.free)) == list(range(100))
+
+
+# ---- what the tensor-level calls refuse ---------------------------------------------------------------
+
+def test_refused_tensors(paged):
+    table = ints([[0, 1], [2, 3]])
+    pool = paged.PagePool(8, 16, table)
+    c = paged.PagedCache.empty(8, 16, 2, 64, table)
+    lens, i64 = ints([5, 6]), torch.zeros(2, dtype=torch.int64, device="cuda")
+    k = torch.zeros((3, 2, 64), dtype=BF16, device="cuda")
+    q = torch.zeros((3, 4, 64), dtype=BF16, device="cuda")
+    cu, slots = ints([0, 1, 3]), ints([0, 1, 2])
+    o = torch.zeros((2, 2, 32, 64), dtype=BF16, device="cuda")
+    bad = [
+        lambda: paged.PagedCache(c.K.cpu(), c.V.cpu(), table), lambda: paged.PagedCache(c.K, c.V[:, :8], table),
+        lambda: paged.PagedCache(c.K.float(), c.V.float(), table), lambda: paged.PagedCache(c.K, c.V.half(), table),
+        lambda: paged.PagedCache(c.K, c.V, table.long()), lambda: paged.PagedCache(c.K, c.V, table[:, :1]),
+        lambda: paged.PagedCache(c.K.transpose(2, 3), c.V.transpose(2, 3), table),
+        lambda: paged.PagePool(8, 16, table, ints([1, 2])), lambda: paged.PagePool(8, 16, table[0]),
+        lambda: pool.tables(lens, i64, 3), lambda: pool.tables(lens, lens[:1], 3), lambda: pool.tables(ints([1, 2, 3]), ints([1, 1, 1]), 3),
+        lambda: pool.tables(lens, lens, 3, slots=ints([0, 0])), lambda: pool.tables(lens, ints([1, 7, 2, 7])[::2], 3),
+        lambda: pool.tables(lens.cpu(), lens, 3), lambda: pool.tables(lens, None, 3), lambda: pool.release(lens, i64),
+        lambda: pool.release(lens, ints([1])), lambda: c.write(k, k[:2], slots), lambda: c.write(k, k, slots[:2]),
+        lambda: c.write(k.half(), k.half(), slots), lambda: c.write(k[..., :32], k[..., :32], slots), lambda: c.write(q, q, slots),
+        lambda: c.write(k, k.transpose(0, 1).contiguous().transpose(0, 1), slots), lambda: c.write(k.cpu(), k.cpu(), slots),
+        lambda: c.write(k, k, slots.long()), lambda: c.attention(q, cu, ints([5])), lambda: c.attention(q, ints([0, 1]), lens),
+        lambda: c.attention(q, cu, lens, out=q[:2]), lambda: c.attention(q, cu, lens, out=q.half()),
+        lambda: c.attention(q, cu, lens, lse=torch.zeros((3, 2), device="cuda")),
+        lambda: c.attention(q, cu, lens, lse=torch.zeros((3, 4), device="cuda", dtype=torch.float64)),
+        lambda: c.attention(q[0], cu, lens), lambda: c.attention(q, ints([0, 1, 2, 3]), ints([1, 1, 1])),
+        lambda: c.attention(q, cu, lens, window=2 ** 40),
+        lambda: c.gather(lens, o[:1], o[:1]), lambda: c.gather(lens, o, o[:, :1]), lambda: c.gather(lens, o.half(), o.half()),
+        lambda: c.gather(lens, o.transpose(2, 3).contiguous().transpose(2, 3), o)]
+    for i, f in enumerate(bad):
+        with pytest.raises(ValueError):
+            f()
+            pytest.fail(f"case {i} was taken")
+    with pytest.raises(kvev.KvevError) as e:  # heads that no group divides: the library's own refusal
+        c.attention(q[:, :3], cu, lens)
+    assert e.value.code == kvev.EINVAL
+    assert c.status() == 0 and int(pool.device_status) == 0
+
+
+def test_one_token_views_with_any_stride(paged):
+    # a dimension of one element may carry any stride
+    c, q, cu, kv, table = attend_case(paged, [(200, 1)], 4, 2, 64, 16, BF16, False)
+    odd = torch.as_strided(q, q.shape, (3, q.stride(1), 1))
+    o, lse = run_attention(c, odd, cu, kv)
+    ref.check_attention(o, lse, ref.attention(c.K, c.V, table, q, cu, kv), BF16)
+    k = torch.randn((1, 2, 64), device="cuda").to(BF16)
+    c.write(torch.as_strided(k, k.shape, (5, 64, 1)), torch.as_strided(k, k.shape, (64, 64, 1)), ints([7]))
+    assert torch.equal(c.K[0, 7], k[0]) and torch.equal(c.V[0, 7], k[0]) and c.status() == 0
