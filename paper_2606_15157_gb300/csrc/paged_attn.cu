@@ -1135,23 +1135,29 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
       bool slow = edge || j == first;
       if (!slow) {
         // the first half's weights by the maximum so far, while the tile's own is being formed
-        uint32_t u[2][32], w[32];
+        uint32_t u[4][32], w[32];
         float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        tmem_ld64_async(ts, u[0], u[1]);
-        tmem_wait64(u[0], u[1]);
         const float nb = kUp - finite_or_0(m);
+        tmem_ld32_async(ts, u[0]);
+        tmem_wait32(u[0]);
+        tmem_ld32_async(ts + 32, u[1]);
         weights<kFp16>(u[0], c, nb, w, 0, acc);
+        float top = max32u(u[0]);
+        tmem_wait32(u[1]);
+        tmem_ld32_async(ts + 64, u[2]);
         weights<kFp16>(u[1], c, nb, w, 16, acc);
-        float top = fmaxf(max32u(u[0]), max32u(u[1]));
-        tmem_ld64_async(ts + 64, u[0], u[1]);
-        tmem_wait64(u[0], u[1]);
-        top = fmaxf(top, fmaxf(max32u(u[0]), max32u(u[1]))) * c;
+        top = fmaxf(top, max32u(u[1]));
+        tmem_wait32(u[2]);
+        tmem_ld32_async(ts + 96, u[3]);
+        top = fmaxf(top, max32u(u[2]));
+        tmem_wait32(u[3]);
+        top = fmaxf(top, max32u(u[3])) * c;
         slow = __any_sync(0xffffffffu, valid && top > m + kRaise);
         if (!slow) {
           tmem_st32(ts, w);
           hand_over(0);
-          weights<kFp16>(u[0], c, nb, w, 0, acc);
-          weights<kFp16>(u[1], c, nb, w, 16, acc);
+          weights<kFp16>(u[2], c, nb, w, 0, acc);
+          weights<kFp16>(u[3], c, nb, w, 16, acc);
           tmem_st32(ts + 32, w);
           const float2 sum = fadd2(fadd2(acc[0], acc[1]), fadd2(acc[2], acc[3]));
           l += sum.x + sum.y;
