@@ -342,8 +342,6 @@ KVEV_API int kvev_plan_debug_stall_unit(kvev_plan *plan, int unit);
  *   - The call allocates nothing: no cudaMalloc/cudaFree and no allocating
  *     library routine.  Inputs and outputs are the caller's, as for
  *     kvev_evict_prefill().
- *   - num_pages * page_size and max_pages * page_size stay below 2^31, and a call
- *     takes at most KVEV_PAGED_MAX_REQUESTS requests (ENOTSUP).
  *   - device_status: required device int32 (4-byte aligned; NULL is
  *     EINVAL) that the call zeroes on `stream` and in which the kernels
  *     record their status bits (1 = a bounded wait ran out, 2 = an in-kernel
@@ -457,8 +455,9 @@ KVEV_API int kvev_decode_step_attn(kvev_plan *plan, int B, int growth, void *dec
  *   - All calls are asynchronous on `stream`, read lengths and tables on the
  *     device and allocate nothing, so a captured graph can be replayed with
  *     other lengths.  They need no plan.
- *   - num_pages * page_size and max_pages * page_size stay below 2^31, and a call
- *     takes at most KVEV_PAGED_MAX_REQUESTS requests (ENOTSUP).
+ *   - num_pages * page_size stays below 2^31, max_pages * page_size and the rows of a
+ *     call at or below 2^30, and a call takes at most KVEV_PAGED_MAX_REQUESTS requests
+ *     (ENOTSUP).
  *   - device_status: required device int32 in which the kernels record status
  *     bits (1 = a bounded wait ran out, 2 = a length, slot or page out of range,
  *     which the kernels skip); the calls only add bits, the caller clears it. */
@@ -546,8 +545,8 @@ KVEV_API int kvev_paged_gather(const kvev_paged_cache *cache, const int32_t *blo
 
 /* Scratch of kvev_paged_attention(), whatever the lengths: *bytes (256-byte
  * aligned device memory).  Its first KVEV_PAGED_SYNC_BYTES must be zero before
- * the first call and are left zero by every call that ends without a status
- * bit; the rest needs no initialisation.  Calls whose GPU work overlaps need a
+ * the first call and are left zero by every call that does not end with status
+ * bit 1; the rest needs no initialisation.  Calls whose GPU work overlaps need a
  * workspace each.  EINVAL: H_q not a multiple of H_kv, or bytes NULL; ENOTSUP
  * as below. */
 #define KVEV_PAGED_SYNC_BYTES 4096

@@ -17,7 +17,7 @@ namespace {
 // cluster, of eight when there may be more than a thread's worth.  Bound by its round trips to L2
 // (lengths; table or stack), 2 us, and the launch.
 // ---------------------------------------------------------------------------
-constexpr int kTableThreads = 1024;
+constexpr int kTableThreads = 1024;  // most of a CTA; no more than requests, tokens or pages
 constexpr int kTableCluster = 8;  // most CTAs of a cluster that every device takes
 
 struct TableParams {
@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kTableThreads) tables_kernel(const __grid_cons
   const int top = *p.free_count, count = min(max(top, 0), p.num_pages);
   bool bad = top != count;
   __syncthreads();
-  for (int s0 = 0; s0 < p.B; s0 += kTableThreads) {
+  for (int s0 = 0; s0 < p.B; s0 += blockDim.x) {
     const int s = s0 + tid;
     int n = 0, q = 0, k = 0;
     bool fits = true;
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kTableThreads) tables_kernel(const __grid_cons
     const longlong2 upto = block_scan(q, k, ws);
     const long long c0 = carry[0], c1 = carry[1];
     __syncthreads();
-    if (tid == kTableThreads - 1) { carry[0] = c0 + upto.x; carry[1] = c1 + upto.y; }
+    if (tid == blockDim.x - 1) { carry[0] = c0 + upto.x; carry[1] = c1 + upto.y; }
     if (s < p.B) {
       const bool ok = fits && (k == 0 || c1 + upto.y <= count);
       cu[s] = static_cast<int>(min(c0 + upto.x - q, static_cast<long long>(INT_MAX)));
@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kTableThreads) tables_kernel(const __grid_cons
   if (tid == 0) cu[p.B] = static_cast<int>(min(carry[0], static_cast<long long>(INT_MAX)));
   cluster_sync();
   const int total = cu[p.B];
-  const int t0 = blockIdx.x * kTableThreads + tid, step = cluster_size() * kTableThreads;
+  const int t0 = blockIdx.x * blockDim.x + tid, step = cluster_size() * blockDim.x;
   if (t0 == 0) {
     *p.count_out = count - given;
     bad |= total > p.T;
@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(kTableThreads) release_kernel(const __grid_con
   const int top = *p.free_count, count = min(max(top, 0), p.num_pages);
   bool bad = top != count;
   __syncthreads();
-  for (int s0 = 0; s0 < p.B; s0 += kTableThreads) {
+  for (int s0 = 0; s0 < p.B; s0 += blockDim.x) {
     const int s = s0 + tid;
     int k = 0;
     if (s < p.B) {
@@ -188,14 +188,14 @@ __global__ void __launch_bounds__(kTableThreads) release_kernel(const __grid_con
     const longlong2 upto = block_scan(k, 0, ws);
     const long long c = carry;
     __syncthreads();
-    if (tid == kTableThreads - 1) carry = c + upto.x;
+    if (tid == blockDim.x - 1) carry = c + upto.x;
     if (s < p.B) first[s] = static_cast<int>(min(c + upto.x - k, static_cast<long long>(INT_MAX)));
     __syncthreads();
   }
   cluster_sync();
   bad |= carry > p.num_pages - count;
   const int total = static_cast<int>(min(carry, static_cast<long long>(p.num_pages - count)));
-  const int t0 = blockIdx.x * kTableThreads + tid, step = cluster_size() * kTableThreads;
+  const int t0 = blockIdx.x * blockDim.x + tid, step = cluster_size() * blockDim.x;
   if (t0 == 0) *p.count_out = count + total;
   for (int s = t0; s < p.B; s += step) p.lens_out[s] = len[s];
   for (int k0 = t0; k0 < total; k0 += 4 * step) {  // four entries in flight per thread
@@ -278,7 +278,7 @@ __global__ void __launch_bounds__(kRowThreads) write_kernel(const __grid_constan
 struct PageGatherParams {
   PagedView c;
   const int *table, *lens;
-  int B, max_pages, S_cap, dv_shift;
+  int B, max_pages, S_cap, dv_shift, blocks;  // blocks: CTAs per request
   uint4 *out_K, *out_V;
   int* status;
 };
@@ -289,9 +289,9 @@ __global__ void __launch_bounds__(kRowThreads) page_gather_kernel(const __grid_c
   __shared__ long long from[1 << kGatherShift];  // a position's row in the pool, -1: none
   pdl_wait();
   pdl_trigger();
-  const int s = blockIdx.y, k0 = blockIdx.x << kGatherShift;
+  const int s = blockIdx.x / p.blocks, k0 = (blockIdx.x - s * p.blocks) << kGatherShift;
   const int len = p.lens[s], n = min(max(len, 0), min(p.S_cap, p.max_pages << p.c.page_shift));
-  if (n != len && threadIdx.x == 0 && blockIdx.x == 0) atomicOr(p.status, kStatusDevice);
+  if (n != len && threadIdx.x == 0 && k0 == 0) atomicOr(p.status, kStatusDevice);
   if (k0 >= n) return;
   if (threadIdx.x < (1 << kGatherShift)) {
     const int k = k0 + threadIdx.x;
@@ -335,9 +335,11 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 
 int launched(cudaError_t e) { return e == cudaSuccess ? KVEV_OK : KVEV_ECUDA; }
 
+int table_threads(int64_t work) { return work >= kTableThreads ? kTableThreads : work <= 32 ? 32 : static_cast<int>((work + 31) & ~31); }
+
 bool tables_sizes(int B, int page_size, int num_pages, int max_pages) {
   return B >= 0 && paged_page_size(page_size) && num_pages >= 1 && max_pages >= 1 &&
-         static_cast<int64_t>(num_pages) * page_size <= INT_MAX && static_cast<int64_t>(max_pages) * page_size <= INT_MAX;
+         static_cast<int64_t>(num_pages) * page_size <= INT_MAX && static_cast<int64_t>(max_pages) * page_size <= kMaxTokens;
 }
 
 }  // namespace
@@ -387,7 +389,7 @@ extern "C" int kvev_paged_tables(const int32_t* lens, const int32_t* new_lens, i
   TableParams p = {lens, new_lens, free_pages, free_count, block_table, kv_lens, cu_new, slots, positions, granted,
                    free_count_out, device_status, B, log2_of(page_size), num_pages, max_pages, T};
   const int ctas = T > kTableThreads ? kTableCluster : 1;
-  return launched(launch_overlapped(tables_kernel, p, ctas, kTableThreads, kPerRequest * B + sizeof(int),
+  return launched(launch_overlapped(tables_kernel, p, ctas, table_threads(B > T ? B : T), kPerRequest * B + sizeof(int),
                                     static_cast<cudaStream_t>(stream), ctas));
 }
 
@@ -407,8 +409,9 @@ extern "C" int kvev_paged_release(const int32_t* lens, const int32_t* done, int 
                            KVEV_PAGED_MAX_REQUESTS * kPerRequest) != cudaSuccess)
     return KVEV_ECUDA;
   // how many pages come back only the device knows: more than a CTA's threads, as far as the table's size tells
-  const int ctas = static_cast<int64_t>(B) * max_pages > kTableThreads ? kTableCluster : 1;
-  return launched(launch_overlapped(release_kernel, p, ctas, kTableThreads, kPerRequest * B,
+  const int64_t pages = static_cast<int64_t>(B) * max_pages;
+  const int ctas = pages > kTableThreads ? kTableCluster : 1;
+  return launched(launch_overlapped(release_kernel, p, ctas, table_threads(pages), kPerRequest * B,
                                     static_cast<cudaStream_t>(stream), ctas));
 }
 
@@ -456,7 +459,7 @@ extern "C" int kvev_paged_gather(const kvev_paged_cache* cache, const int32_t* b
   p.out_V = static_cast<uint4*>(out_V);
   p.status = device_status;
   p.dv_shift = log2_of(p.c.dv);
-  page_gather_kernel<<<dim3((S_cap + (1 << kGatherShift) - 1) >> kGatherShift, B), kRowThreads, 0,
-                       static_cast<cudaStream_t>(stream)>>>(p);
-  return launched(cudaGetLastError());
+  p.blocks = (S_cap + (1 << kGatherShift) - 1) >> kGatherShift;
+  if (static_cast<int64_t>(p.blocks) * B > INT_MAX) return KVEV_ENOTSUP;
+  return launched(launch_overlapped(page_gather_kernel, p, p.blocks * B, kRowThreads, 0, static_cast<cudaStream_t>(stream)));
 }

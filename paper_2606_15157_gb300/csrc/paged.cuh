@@ -15,6 +15,7 @@ struct PagedView {
 // Whether the cache's sizes, strides and pointers are in range; its view.
 int paged_view(const kvev_paged_cache* c, PagedView* v);
 bool paged_page_size(int page_size);
+constexpr int kMaxTokens = 1 << 30;  // of a request, or rows of a call: positions and their differences are ints
 inline int log2_of(int x) { return 31 - __builtin_clz(static_cast<unsigned>(x)); }
 
 }  // namespace kvev

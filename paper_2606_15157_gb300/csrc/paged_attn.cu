@@ -7,27 +7,44 @@
 // l kept in registers and o in tensor memory.
 //
 // Work.  The G query heads of a KV head and neighbouring tokens share K and V, so
-// their rows fill the 128 lanes of a tensor-core tile: P = 128 / G tokens x G
+// their rows make up the 128 rows of a tensor-core tile: P = 128 / G tokens x G
 // heads.  A unit is up to two such tiles (2 P tokens of a request and KV head)
-// against its key tiles; a CTA runs two "sides", each a tile of rows with its own
-// scores, output accumulator and softmax warpgroup, so that one side's softmax
-// runs while the tensor core works for the other:
+// against its key tiles; a CTA runs two "sides", each with its own scores, output
+// accumulator and softmax warpgroup, so that one side's softmax runs while the tensor
+// core works for the other:
 //   - full unit (more than P tokens): side x holds the x-th tile of rows, and
 //     both take every key tile;
-//   - paired unit (a single tile of rows: single tokens, short chunks): both
-//     sides hold the same rows and take the key tiles in turn, and are merged.
-// All units' key tiles are laid end to end and cut into equal shares, one per CTA
-// (cost of a tile: 2 in a full unit, 1 in a paired one, kUnitCost for a unit's
-// start and end), so that any mix of lengths keeps every SM busy to the end and a
-// long context is split where there are few rows.  The pieces of a unit that
-// was cut leave (m, l, o) records in the workspace; the piece that arrives last
-// merges them in order, so the result does not depend on who that is.
+//   - paired unit (17 rows to P tokens): both sides hold the same rows and
+//     take the key tiles in turn, and are merged;
+//   - few rows (up to 16: single tokens): the same with the products transposed, keys on the
+//     lanes, so that a thread per key forms the weights of all rows.  (In rows of
+//     lanes, 4 lanes of 128 had work, one after another: 64 generations at 4K
+//     167 us with pages of 64, and 163 so.)
+// All units' key tiles are laid end to end and cut into equal shares, one per CTA, so that
+// any mix of lengths keeps every SM busy to the end and a long context is split
+// where there are few rows.  The pieces of a unit that was cut leave (m, l, o) records in the
+// workspace; the piece that arrives last merges them in order, so the result does
+// not depend on which that is.
 //
-// Roles (384 threads): warp 0 loads Q tiles and pages by TMA (a lane per page
-// box), warp 1 issues the MMAs, warp 2 deals the entries
-// (pieces of units) to the others through a ring, warps 4-7 and 8-11 are the sides' softmax warpgroups, a
-// thread per row.  S = Q K^T is read from tensor memory into registers, and the
-// weights go back into the same columns as the A operand of O += P V.
+// Roles (384 threads): warp 0 loads Q tiles and page boxes by TMA, warp 1 issues the
+// MMAs, warp 2 deals the entries (pieces of units) to the others through a ring, warps 4-7
+// and 8-11 are the sides' softmax warpgroups.  S = Q K^T is read from tensor memory
+// into registers, and the weights go back into the same columns as the A operand of
+// O += P V (few rows: to shared memory as the B operand of O^T += V^T P^T).
+//
+// Bounds and measurements (one GB300, 32 query and 8 KV heads of 128, pages of 16):
+//   - generations: HBM.  64 at 4K 160 us, 6.7 TB/s; 16 at 16K 158 us, 6.8 TB/s.  One at 4K
+//     10.7 us: the dependent steps of one pass (schedule 2 us, first tiles 1.5, products
+//     and softmax 2, records and merge 2), the launch 2.
+//   - chunks: a side's softmax and the two products after it, which wait for one another
+//     (1,640 and 1,220 cycles a tile, the tensor core's own work 1,024 of the sides' 2,860);
+//     tensor pipe active 70 %.  Four chunks of 1,200 tokens over 9,000 415 us, 1,590
+//     TFLOP/s; the last 4K of a 32K prompt 1.23 ms, 1,677 (1.40 ms under the power cap, the
+//     clock at 1.64 of 2.07 GHz).  An 8K prompt 360-386 us: 1,024 units whose start
+//     and end cost 3 tiles.
+// Measured against it: MMAs issued by a thread per side, whose products interleave, 664 us
+// for 541; by one thread for both 586; four softmax warpgroups of 64 columns each (96
+// registers a thread) 488 us for 441.
 #include <atomic>
 #include <climits>
 #include <cmath>
@@ -42,16 +59,23 @@ constexpr int kRegsAttnControl = 56, kRegsAttnSoftmax = 224;
 constexpr int kRegsAttnNeeded = 128 * kRegsAttnControl + 256 * kRegsAttnSoftmax;
 constexpr int kMaxCtas = 152;
 constexpr int kEntries = 4;         // ring of dealt entries
-// Kinds of unit, and the cost of a key tile and of a unit's start and end in each.
 enum Kind : int { kFew = 0, kPaired = 1, kFull = 2 };
 constexpr int kFewRows = 16;
+// What the shares are cut by: the cost of a key tile, and of a unit's start and end.  Beside
+// chunks a generation's tile takes 0.5 to 0.9 of a chunk's, by how many others load.  Us of
+// 28 generations and 4 chunks with a window, without one, 60 and 2, an 8K prompt, with
+// tiles of full and other units and their ends at
+//   5, 3; 16, 8     285  690  207  358        5, 3; 20, 10    285  692  206  384
+//   5, 2.5; 16, 5   283  745  190  365        5, 2; 16, 4     343  885  196  359
 __host__ __device__ constexpr int tile_cost(int kind) { return kind == kFull ? 5 : 3; }
 __host__ __device__ constexpr int unit_cost(int kind) { return kind == kFull ? 16 : 8; }
 // Least cost of a share (a tile's or more: no piece of a cut unit is empty).  Records of
-// more than a few rows are up to 64 KB a side and piece, and one CTA merges them.
+// more than a few rows are up to 64 KB a side and piece, and one CTA merges them: a
+// chunk of 32 tokens over 4K 25.4 us with shares from 5 on, 21.9 from 20, 29 from 48.
 constexpr int kMinShare = 5, kMinShareRows = 20;
 constexpr int kRows = 128;          // rows of a side
 constexpr int kParts = 2;           // halves of a tile's weights, which the second product takes as they come
+                                    // (whole: 457 us for 449, four chunks of 1,200 over 9,000)
 constexpr float kRaise = 8.f;       // a row's maximum is raised when a tile's is this much (log2) above it
 constexpr uint64_t kAttnWaitNs = 2000000000ull;
 
@@ -91,7 +115,7 @@ struct AttnSmem {
   uint64_t qfull[2], qempty[2], full[kStages], empty[kStages];
   uint64_t sfull[2], pfull[2][kParts], ofull[2];
   uint64_t efull[kEntries], eempty[kEntries];
-  uint64_t xfull, xfree;             // paired units: both sides' (m, l) are there; both sides are done with O
+  uint64_t xfull, xfree;             // rows that both sides share: their (m, l) are there; their O is done with
   uint64_t done;
   long long carry, start;
   union {
@@ -385,9 +409,9 @@ __device__ __forceinline__ Share share_of(const PagedAttnParams& p, S& sm) {
   return r;
 }
 
-// The same by one warp for up to 32 requests, with no barrier for the block: a single
-// generation at a 4K context 13.1 -> 10.4 us.
-// Lane s keeps request s and its cost for one KV head.
+// The same by one warp for up to 32 requests, with no barrier for the block (one generation
+// at a 4K context 13.1 us with the block's, 11.3 so).  Lane s keeps request s and its cost
+// for one KV head.
 __device__ __forceinline__ Share share_of_warp(const PagedAttnParams& p, Request& held, long long& held_cost) {
   const int lane = threadIdx.x & 31;
   bool bad = false;
@@ -604,9 +628,8 @@ __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>&
 // the rows' Q tile from its row 32 on.
 __device__ __forceinline__ uint32_t few_p_offset(int side) { return 4096 + side * 4096; }
 
-template <int D>
+// Tensor memory columns of a side's scores (then weights) and of its output.
 __device__ __forceinline__ uint32_t s_col(int side) { return side * 128; }
-template <int D>
 __device__ __forceinline__ uint32_t o_col(int side) { return 256 + side * 128; }
 
 // One warp issues every MMA: the sides' products run in turn, whole (issued by a thread
@@ -645,7 +668,7 @@ __device__ __forceinline__ void mma_warp(const PagedAttnParams& p, AttnSmem<D>& 
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
           const uint32_t off = (k >> 2) * (kBlock / 16) + (k & 3) * 2;
-          umma_ss(tmem + s_col<D>(x), kdesc + off, qdesc + off, kIdescKQ, k > 0);
+          umma_ss(tmem + s_col(x), kdesc + off, qdesc + off, kIdescKQ, k > 0);
         }
         umma_commit_elect(&sm.sfull[x]);
         umma_commit_elect(&sm.empty[st]);
@@ -663,7 +686,7 @@ __device__ __forceinline__ void mma_warp(const PagedAttnParams& p, AttnSmem<D>& 
         const uint64_t pdesc = sw128_desc(smem_u32(sm.q[q0]) + few_p_offset(x));
 #pragma unroll
         for (int k = 0; k < kRows / 16; ++k)
-          umma_ss(tmem + o_col<D>(x), vdesc + k * (16 * 128 / 16), pdesc + (k >> 2) * (kFewRows * 128 / 16) + (k & 3) * 2,
+          umma_ss(tmem + o_col(x), vdesc + k * (16 * 128 / 16), pdesc + (k >> 2) * (kFewRows * 128 / 16) + (k & 3) * 2,
                   kIdescVP, j >= 2 || k > 0);
         umma_commit_elect(&sm.empty[st]);
         if (j + 2 >= n) umma_commit_elect(&sm.ofull[x]);
@@ -680,7 +703,7 @@ __device__ __forceinline__ void mma_warp(const PagedAttnParams& p, AttnSmem<D>& 
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
           const uint32_t off = (k >> 2) * (kBlock / 16) + (k & 3) * 2;
-          umma_ss(tmem + s_col<D>(x), qdesc + off, kdesc + off, kIdescQK, k > 0);
+          umma_ss(tmem + s_col(x), qdesc + off, kdesc + off, kIdescQK, k > 0);
         }
         umma_commit_elect(&sm.sfull[x]);
       };
@@ -721,7 +744,7 @@ __device__ __forceinline__ void mma_warp(const PagedAttnParams& p, AttnSmem<D>& 
             if (ok) {
 #pragma unroll
               for (int k = part * 8 / kParts; k < (part + 1) * 8 / kParts; ++k)
-                umma_ts(tmem + o_col<D>(x), tmem + s_col<D>(x) + k * 8, vdesc + k * (16 * 128 / 16), kIdescPV, !first || k > 0);
+                umma_ts(tmem + o_col(x), tmem + s_col(x) + k * 8, vdesc + k * (16 * 128 / 16), kIdescPV, !first || k > 0);
             }
           }
           if (!ok) break;
@@ -840,7 +863,7 @@ __device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D>& 
                                          SideState& st) {
   const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, key = warp * 32 + lane;
   const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
-  const uint32_t ts = tmem + lanes + s_col<D>(x);
+  const uint32_t ts = tmem + lanes + s_col(x);
   const float c = p.scale_log2;
   constexpr float kUp = kFp16 ? 7.f : 0.f;
   // this key's 2 bytes of row r: r * 128 + ((chunk ^ r) & 7) * 16 + ... in the 64-key half
@@ -895,10 +918,10 @@ __device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D>& 
       if (j != first) {
         // S of this tile is complete, so is O of the side's tile before it, and the next waits for us
         uint32_t o[R];
-        tmem_ld_cols<R>(tmem + lanes + o_col<D>(x), o);
+        tmem_ld_cols<R>(tmem + lanes + o_col(x), o);
 #pragma unroll
         for (int r = 0; r < R; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * f[r]);
-        tmem_st_cols<R>(tmem + lanes + o_col<D>(x), o);
+        tmem_st_cols<R>(tmem + lanes + o_col(x), o);
         tmem_wait_st();
       }
     }
@@ -950,7 +973,7 @@ __device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D>& 
   float v[R];
   {
     uint32_t o[R];
-    tmem_ld_cols<R>(tmem + lanes + o_col<D>(0), o);
+    tmem_ld_cols<R>(tmem + lanes + o_col(0), o);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const float2 a = sm.ml[0][r], b = both ? sm.ml[1][r] : make_float2(-INFINITY, 0.f);
@@ -960,7 +983,7 @@ __device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D>& 
       v[r] = l[r] == 0.f ? 0.f : __uint_as_float(o[r]) * f;
     }
     if (both) {
-      tmem_ld_cols<R>(tmem + lanes + o_col<D>(1), o);
+      tmem_ld_cols<R>(tmem + lanes + o_col(1), o);
 #pragma unroll
       for (int r = 0; r < R; ++r)
         if (l[r] != 0.f) v[r] = fmaf(__uint_as_float(o[r]), ex2_approx(sm.ml[1][r].x - finite_or_0(m[r])), v[r]);
@@ -1099,7 +1122,7 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
   const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
   const int r = warp * 32 + lane;  // row of the side = TMEM lane
   const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
-  const uint32_t ts = tmem + lanes + s_col<D>(x);
+  const uint32_t ts = tmem + lanes + s_col(x);
   const float c = p.scale_log2;
   // half precision: the weights are kept 2^7 larger, clear of its subnormals (a lagging maximum adds 2^kRaise)
   constexpr float kUp = kFp16 ? 7.f : 0.f;
@@ -1186,10 +1209,10 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
 #pragma unroll 1
             for (int q = 0; q < D; q += 16) {
               uint32_t o[16];
-              tmem_ld_cols<16>(tmem + lanes + o_col<D>(x) + q, o);
+              tmem_ld_cols<16>(tmem + lanes + o_col(x) + q, o);
 #pragma unroll
               for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-              tmem_st_cols<16>(tmem + lanes + o_col<D>(x) + q, o);
+              tmem_st_cols<16>(tmem + lanes + o_col(x) + q, o);
             }
           }
         }
@@ -1223,7 +1246,7 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
   // factors of the accumulators, and the columns that this side writes
   float fa = 1.f, fb = 0.f;
   int col0 = 0, cols = D;
-  uint32_t oa = o_col<D>(x);
+  uint32_t oa = o_col(x);
   bool both = false;
   if (paired) {
     sm.ml[x][r] = make_float2(m, l);
@@ -1238,7 +1261,7 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
     fa = ex2_approx(a.x - finite_or_0(m));
     fb = ex2_approx(b.x - finite_or_0(m));
     l = fmaf(a.y, fa, b.y * fb);
-    oa = o_col<D>(0);
+    oa = o_col(0);
     cols = D / 2;
     col0 = x * cols;
   }
@@ -1267,7 +1290,7 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
 #pragma unroll
       for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(o[k]) * fa;
       if (both) {
-        tmem_ld32_async(tmem + lanes + o_col<D>(1) + q, o);
+        tmem_ld32_async(tmem + lanes + o_col(1) + q, o);
         tmem_wait32(o);
 #pragma unroll
         for (int k = 0; k < 32; ++k) v[k] = fmaf(__uint_as_float(o[k]), fb, v[k]);
@@ -1518,8 +1541,8 @@ extern "C" int kvev_paged_attention(const kvev_paged_cache* cache, const void* q
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || !device_status) return KVEV_EINVAL;
   for (int64_t st : {q_token_stride, q_head_stride, out_token_stride, out_head_stride})
     if (st <= 0 || (st & 7)) return KVEV_EINVAL;
-  if (B < 0 || T < 0 || max_pages < 1 || static_cast<int64_t>(max_pages) * cache->page_size > INT_MAX || window < 0 ||
-      !(scale >= 0.f) || !std::isfinite(scale))
+  if (B < 0 || T < 0 || T > kMaxTokens || max_pages < 1 || static_cast<int64_t>(max_pages) * cache->page_size > kMaxTokens ||
+      window < 0 || !(scale >= 0.f) || !std::isfinite(scale))
     return KVEV_EINVAL;
   if (B > KVEV_PAGED_MAX_REQUESTS) return KVEV_ENOTSUP;
   if (workspace_bytes < need) return KVEV_ENOMEM;

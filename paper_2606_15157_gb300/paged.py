@@ -197,4 +197,10 @@ class PagedCache:
         v = int(self.device_status.item())
         if v:
             self.device_status.zero_()
+        if v & 1:  # a wait ran out: the pieces counted so far would be counted again
+            torch.cuda.synchronize(self._device)
+            for (device, _), ws in _workspaces.items():
+                if device == self._device:
+                    ws[2][:kvev.PAGED_SYNC_BYTES].zero_()
+            torch.cuda.synchronize(self._device)
         return v
