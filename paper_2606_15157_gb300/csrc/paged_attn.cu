@@ -837,11 +837,12 @@ __device__ __forceinline__ bool arrived_last(const PagedAttnParams& p, AttnSmem<
   if ((threadIdx.x & 127) == 0) {
     int last = 0;
     if (ok) {
-      __threadfence();  // (for the whole group's records: the barrier orders them before it)
+      // releases the whole group's records (the barrier orders them before it), acquires the others'
       int* cnt = p.sync + 2 * en.first + x;
-      last = atomicAdd(cnt, 1) == en.pieces - 1;
-      if (last) atomicExch(cnt, 0);
-      __threadfence();
+      int n;
+      asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(n) : "l"(cnt) : "memory");
+      last = n == en.pieces - 1;
+      if (last) *cnt = 0;
     }
     sm.last[x] = last;
   }
