@@ -538,7 +538,8 @@ KVEV_API int kvev_paged_write(const kvev_paged_cache *cache, const void *k, cons
  * kvev_evict_prefill() reads: out_K, out_V device [B][H_kv][S_cap][d] (16-byte
  * aligned); rows from lens[s] on are not written.  A length outside
  * 0..min(S_cap, max_pages * page_size) is cut to it, and the rows of a page
- * outside the pool are left out, both with status bit 2.  EINVAL as above. */
+ * outside the pool are left out, both with status bit 2.  EINVAL as above; ENOTSUP:
+ * B * S_cap of 2^35 or more. */
 KVEV_API int kvev_paged_gather(const kvev_paged_cache *cache, const int32_t *block_table, int max_pages,
                                const int32_t *lens, int B, int S_cap, void *out_K, void *out_V,
                                int32_t *device_status, void *stream);

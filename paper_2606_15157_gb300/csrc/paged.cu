@@ -376,7 +376,7 @@ extern "C" int kvev_paged_tables(const int32_t* lens, const int32_t* new_lens, i
                                  int max_pages, int T, int32_t* kv_lens, int32_t* cu_new, int32_t* slots,
                                  int32_t* positions, int32_t* granted, int32_t* free_count_out,
                                  int32_t* device_status, void* stream) {
-  if (!free_pages || !free_count || !cu_new || !free_count_out || !device_status || T < 0 ||
+  if (!free_pages || !free_count || !cu_new || !free_count_out || !device_status || T < 0 || T > kMaxTokens ||
       !tables_sizes(B, page_size, num_pages, max_pages) || (T > 0 && (!slots || !positions)) ||
       (B > 0 && (!lens || !new_lens || !block_table || !kv_lens || !granted)))
     return KVEV_EINVAL;
@@ -421,7 +421,7 @@ extern "C" int kvev_paged_write(const kvev_paged_cache* cache, const void* k, co
   WriteParams p = {};
   const int rc = paged_view(cache, &p.c);
   if (rc != KVEV_OK) return rc;
-  if (!device_status || T < 0 || token_stride <= 0 || head_stride <= 0 || (token_stride & 7) || (head_stride & 7))
+  if (!device_status || T < 0 || T > kMaxTokens || token_stride <= 0 || head_stride <= 0 || (token_stride & 7) || (head_stride & 7))
     return KVEV_EINVAL;
   if (T == 0) return KVEV_OK;
   if (!k || !v || !aligned16(k) || !aligned16(v) || !slots) return KVEV_EINVAL;
@@ -460,6 +460,6 @@ extern "C" int kvev_paged_gather(const kvev_paged_cache* cache, const int32_t* b
   p.status = device_status;
   p.dv_shift = log2_of(p.c.dv);
   p.blocks = (S_cap + (1 << kGatherShift) - 1) >> kGatherShift;
-  if (static_cast<int64_t>(p.blocks) * B > INT_MAX) return KVEV_ENOTSUP;
+  if (static_cast<int64_t>(p.blocks) * B > INT_MAX) return KVEV_ENOTSUP;  // CTAs of a launch
   return launched(launch_overlapped(page_gather_kernel, p, p.blocks * B, kRowThreads, 0, static_cast<cudaStream_t>(stream)));
 }

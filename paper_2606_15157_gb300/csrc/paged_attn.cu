@@ -72,6 +72,7 @@ __host__ __device__ constexpr int unit_cost(int kind) { return kind == kFull ? 1
 // Least cost of a share (a tile's or more: no piece of a cut unit is empty).  Records of
 // more than a few rows are up to 64 KB a side and piece, and one CTA merges them: a
 // chunk of 32 tokens over 4K 25.4 us with shares from 5 on, 21.9 from 20, 29 from 48.
+// (Batches of over 32 requests have larger shares anyway.)
 constexpr int kMinShare = 5, kMinShareRows = 20;
 constexpr int kRows = 128;          // rows of a side
 constexpr int kParts = 2;           // halves of a tile's weights, which the second product takes as they come
@@ -723,7 +724,7 @@ __device__ __forceinline__ void mma_warp(const PagedAttnParams& p, AttnSmem<D>& 
         advance();
       }
       for (int j = 0; ok && j < n; ++j) {
-        // both tiles of the round are there before the first weights are waited for
+        // the V tile and the next K tile are there before the first weights are waited for
         const uint32_t vs = st;
         tile();
         advance();
@@ -867,7 +868,7 @@ __device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D>& 
   const uint32_t ts = tmem + lanes + s_col(x);
   const float c = p.scale_log2;
   constexpr float kUp = kFp16 ? 7.f : 0.f;
-  // this key's 2 bytes of row r: r * 128 + ((chunk ^ r) & 7) * 16 + ... in the 64-key half
+  // this key's 2 bytes of row r are at r * 128 + ((chunk ^ r) & 7) * 16 from here
   uint8_t* const pw = sm.q[st.qn & 1] + few_p_offset(x) + (key >> 6) * (kFewRows * 128) + (key & 7) * 2;
   const int chunk = (key & 63) >> 3;
   const int rows = en.n * p.G;

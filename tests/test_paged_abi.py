@@ -56,6 +56,8 @@ for _op in ("tables", "release"):
     BAD_ARGS += [(_op, {"B": -1}, "EINVAL"), (_op, {"B": 8193}, "ENOTSUP"), (_op, {"page_size": 12}, "EINVAL"), (_op, {"num_pages": 0}, "EINVAL"),
                  (_op, {"num_pages": 1 << 28}, "EINVAL"), (_op, {"max_pages": 0}, "EINVAL"), (_op, {"max_pages": 1 << 28}, "EINVAL")]
 BAD_ARGS += [("tables", {"T": -1}, "EINVAL")]
+BAD_ARGS += [(_op, {"T": (1 << 30) + 1}, "EINVAL") for _op in ("tables", "write", "attention")]
+BAD_ARGS += [("gather", {"B": 8192, "S_cap": 1 << 23}, "ENOTSUP")]
 BAD_ARGS += [("write", {k: 0}, "EINVAL") for k in ("cache", "k", "v", "slots", "device_status", "token_stride", "head_stride")]
 BAD_ARGS += [("write", {"k": P + 8}, "EINVAL"), ("write", {"v": P + 4}, "EINVAL"), ("write", {"T": -1}, "EINVAL"),
              ("write", {"token_stride": 1028}, "EINVAL"), ("write", {"head_stride": -128}, "EINVAL")]
