@@ -1157,14 +1157,15 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
     };
     if (work) {
       const bool edge = j < f0 || j >= f1;
-      bool slow = edge || j == first;
+      bool slow = edge;
       if (!slow) {
         // the first half's weights by the maximum so far, while the tile's own is being formed
         uint32_t u[4][32], w[32];
         float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        const float nb = kUp - finite_or_0(m);
         tmem_ld32_async(ts, u[0]);
         tmem_wait32(u[0]);
+        if (j == first) m = max32u(u[0]) * c;  // (nothing summed yet: any start will do that the others are not far above)
+        const float nb = kUp - finite_or_0(m);
         tmem_ld32_async(ts + 32, u[1]);
         weights<kFp16>(u[0], c, nb, w, 0, acc);
         float top = max32u(u[0]);
@@ -1190,7 +1191,7 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
         }
       }
       if (slow) {
-        // an edge of the rows' keys, the first tile, or a maximum to raise: in 32-key pieces
+        // an edge of the rows' keys or a maximum to raise: in 32-key pieces
         // and two passes, which keep the code short (the instruction cache is the limit of short units)
         float top = -INFINITY;
 #pragma unroll 1
