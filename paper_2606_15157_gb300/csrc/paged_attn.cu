@@ -34,13 +34,13 @@
 //
 // Bounds and measurements (one GB300, 32 query and 8 KV heads of 128, pages of 16):
 //   - generations: HBM.  64 at 4K 160 us, 6.7 TB/s; 16 at 16K 158 us, 6.8 TB/s.  One at 4K
-//     10.7 us: the dependent steps of one pass (schedule 2 us, first tiles 1.5, products
+//     10.2 us: the dependent steps of one pass (schedule 2 us, first tiles 1.5, products
 //     and softmax 2, records and merge 2), the launch 2.
 //   - chunks: a side's softmax and the two products after it, which wait for one another
 //     (1,640 and 1,220 cycles a tile, the tensor core's own work 1,024 of the sides' 2,860);
-//     tensor pipe active 70 %.  Four chunks of 1,200 tokens over 9,000 415 us, 1,590
-//     TFLOP/s; the last 4K of a 32K prompt 1.23 ms, 1,677 (1.40 ms under the power cap, the
-//     clock at 1.64 of 2.07 GHz).  An 8K prompt 360-386 us: 1,024 units whose start
+//     tensor pipe active 70 %.  Four chunks of 1,200 tokens over 9,000 408 us, 1,620
+//     TFLOP/s; the last 4K of a 32K prompt 1.20 ms, 1,722 (1.40 ms under the power cap, the
+//     clock at 1.64 of 2.07 GHz).  An 8K prompt 350-380 us: 1,024 units whose start
 //     and end cost 3 tiles.
 // Measured against it: MMAs issued by a thread per side, whose products interleave, 664 us
 // for 541; by one thread for both 586; four softmax warpgroups of 64 columns each (96
