@@ -41,7 +41,10 @@ CXX = os.environ.get("CXX", "g++")
 def _bind_flags() -> tuple[list[str], list[str]]:
     """(compiler, linker) flags of the extension module: Python's, torch's and CUDA's headers and libraries."""
     import importlib.util
-    torch_dir = os.path.dirname(importlib.util.find_spec("torch").origin)  # (without importing it)
+    spec = importlib.util.find_spec("torch")  # (without importing it)
+    if spec is None:
+        raise RuntimeError(f"{BIND} needs torch's headers and libraries: torch is not installed")
+    torch_dir = os.path.dirname(spec.origin)
     cuda = os.path.dirname(os.path.dirname(NVCC))
     libs = os.path.join(torch_dir, "lib")
     return (["-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I", os.path.join(torch_dir, "include"),

@@ -106,6 +106,12 @@ struct Entry {
 template <int D>
 struct AttnSmem {
   static constexpr int kTileBytes = kRows * D * 2;
+  // Units lie request by request, head by head; with 64-element heads head by head, request by request: the
+  // heads of the same tokens, 128 bytes each next to one another in tokens-first pages, of which L2 fetches
+  // 256, are then read by different CTAs at about the same time.  (64 generations at 4K 148 us in the
+  // first order, 108 with L2 fetching 128, 101 so; on a faster box 91 either way.  128-element heads:
+  // generations the same within 1 %, four chunks of 1,200 over 9,000 409 us in the first order, 421 in the other.)
+  static constexpr bool kHeadsOuter = D == 64;
   static constexpr int kStages = D == 128 ? 5 : 10;
   // (with 64-element rows the transposed products also read the tile's size of
   // bytes after a V tile, for lanes that nothing reads: the Q tiles, after the last)
@@ -363,29 +369,40 @@ __device__ __forceinline__ long long block_prefix(S& sm, long long v, long long*
 // cost before it (all threads; the block's result).
 struct Share {
   long long x0, x1, before, share;
-  int s;
+  int s, h;  // (h: kHeadsOuter)
 };
+// The CTA's share of `outer` rounds of cost `round`; before: the cost of the rounds before its own.
+__device__ __forceinline__ Share share_at(long long round, int outer, int least) {
+  Share r;
+  const long long total = round * outer;
+  r.share = max(static_cast<long long>(least), divide(total + gridDim.x - 1, gridDim.x));
+  r.x0 = min(total, r.share * blockIdx.x);
+  r.x1 = min(total, r.x0 + r.share);
+  r.h = outer > 1 && round > 0 ? static_cast<int>(divide(r.x0, round)) : 0;
+  r.before = r.h * round;
+  return r;
+}
+
 template <class S>
 __device__ __forceinline__ Share share_of(const PagedAttnParams& p, S& sm) {
   const int tid = threadIdx.x;
   bool bad = false;
   long long total = 0, mine = 0, first_before = 0;
+  const int per = S::kHeadsOuter ? 1 : p.H_kv, outer = S::kHeadsOuter ? p.H_kv : 1;
   for (int s0 = 0; s0 < p.B; s0 += kAttnThreads) {
     mine = 0;
-    if (s0 + tid < p.B) mine = head_cost(p, request(p, s0 + tid, &bad)) * p.H_kv;
+    if (s0 + tid < p.B) mine = head_cost(p, request(p, s0 + tid, &bad)) * per;
     long long all;
     const long long before = block_prefix(sm, mine, &all);
     if (s0 == 0) first_before = before;
     total += all;
   }
   if (bad && blockIdx.x == 0) atomicOr(p.status, kStatusDevice);
-  Share r;
-  r.share = max(static_cast<long long>(kMinShare), divide(total + gridDim.x - 1, gridDim.x));
-  r.x0 = min(total, r.share * blockIdx.x);
-  r.x1 = min(total, r.x0 + r.share);
+  Share r = share_at(total, outer, kMinShare);
+  const long long x = r.x0 - r.before;
   // the thread whose request holds x0 says so
   if (p.B <= kAttnThreads) {
-    if (mine > 0 && first_before <= r.x0 && r.x0 < first_before + mine) {
+    if (mine > 0 && first_before <= x && x < first_before + mine) {
       sm.start = tid;
       sm.carry = first_before;
     }
@@ -393,33 +410,34 @@ __device__ __forceinline__ Share share_of(const PagedAttnParams& p, S& sm) {
     long long sum = 0;
     for (int s0 = 0; s0 < p.B; s0 += kAttnThreads) {
       bool b = false;
-      const long long c = s0 + tid < p.B ? head_cost(p, request(p, s0 + tid, &b)) * p.H_kv : 0;
+      const long long c = s0 + tid < p.B ? head_cost(p, request(p, s0 + tid, &b)) * per : 0;
       long long all;
       const long long before = sum + block_prefix(sm, c, &all);
-      if (c > 0 && before <= r.x0 && r.x0 < before + c) {
+      if (c > 0 && before <= x && x < before + c) {
         sm.start = s0 + tid;
         sm.carry = before;
       }
       sum += all;
-      if (sum > r.x0) break;
+      if (sum > x) break;
     }
   }
   __syncthreads();
   r.s = static_cast<int>(sm.start);
-  r.before = sm.carry;
+  r.before += sm.carry;
   return r;
 }
 
 // The same by one warp for up to 32 requests, with no barrier for the block (one generation
 // at a 4K context 13.1 us with the block's, 11.3 so).  Lane s keeps request s and its cost
 // for one KV head.
+template <class S>
 __device__ __forceinline__ Share share_of_warp(const PagedAttnParams& p, Request& held, long long& held_cost) {
   const int lane = threadIdx.x & 31;
   bool bad = false;
   held = {};
   if (lane < p.B) held = request(p, lane, &bad);
   held_cost = head_cost(p, held);
-  const long long mine = held_cost * p.H_kv;
+  const long long mine = S::kHeadsOuter ? held_cost : held_cost * p.H_kv;
   if (bad && blockIdx.x == 0) atomicOr(p.status, kStatusDevice);
   long long upto = mine;
 #pragma unroll
@@ -427,15 +445,12 @@ __device__ __forceinline__ Share share_of_warp(const PagedAttnParams& p, Request
     const long long x = __shfl_up_sync(0xffffffffu, upto, o);
     if (lane >= o) upto += x;
   }
-  const long long total = __shfl_sync(0xffffffffu, upto, 31);
-  Share r;
   const bool rows = __any_sync(0xffffffffu, held.q * p.G > kFewRows);
-  r.share = max(static_cast<long long>(rows ? kMinShareRows : kMinShare), divide(total + gridDim.x - 1, gridDim.x));
-  r.x0 = min(total, r.share * blockIdx.x);
-  r.x1 = min(total, r.x0 + r.share);
-  const uint32_t here = __ballot_sync(0xffffffffu, mine > 0 && upto - mine <= r.x0 && r.x0 < upto);
+  Share r = share_at(__shfl_sync(0xffffffffu, upto, 31), S::kHeadsOuter ? p.H_kv : 1, rows ? kMinShareRows : kMinShare);
+  const long long x = r.x0 - r.before;
+  const uint32_t here = __ballot_sync(0xffffffffu, mine > 0 && upto - mine <= x && x < upto);
   r.s = here ? __ffs(here) - 1 : 0;  // (none: the share is empty)
-  r.before = __shfl_sync(0xffffffffu, upto - mine, r.s);
+  r.before += __shfl_sync(0xffffffffu, upto - mine, r.s);
   return r;
 }
 
@@ -447,7 +462,7 @@ __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, Share sh) 
   const bool short_batch = p.B <= 32;
   Request held;
   long long held_cost;
-  if (short_batch) sh = share_of_warp(p, held, held_cost);
+  if (short_batch) sh = share_of_warp<S>(p, held, held_cost);
   auto get = [&](int s) {
     if (short_batch)
       return Request{__shfl_sync(0xffffffffu, held.c0, s), __shfl_sync(0xffffffffu, held.q, s), __shfl_sync(0xffffffffu, held.kv, s)};
@@ -468,9 +483,12 @@ __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, Share sh) 
     int s = sh.s;
     Request r = get(s);
     long long a = sh.before;  // cost before the unit
-    const long long hc = short_batch ? __shfl_sync(0xffffffffu, held_cost, s) : head_cost(p, r);
-    int h = static_cast<int>(divide(sh.x0 - a, hc)), m = 0;
-    a += h * hc;
+    int h = sh.h, m = 0;
+    if (!S::kHeadsOuter) {
+      const long long hc = short_batch ? __shfl_sync(0xffffffffu, held_cost, s) : head_cost(p, r);
+      h = static_cast<int>(divide(sh.x0 - a, hc));
+      a += h * hc;
+    }
     Unit u = unit_of(p, r, m);
     while (a + cost_of(u) <= sh.x0) {
       a += cost_of(u);
@@ -504,7 +522,15 @@ __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, Share sh) 
       if (a >= sh.x1) break;
       if (2 * p.P * ++m >= r.q) {
         m = 0;
-        if (++h == p.H_kv) {
+        if (S::kHeadsOuter) {
+          do {
+            if (++s == p.B) {
+              s = 0;
+              ++h;
+            }
+            r = get(s);
+          } while (r.q == 0);
+        } else if (++h == p.H_kv) {
           h = 0;
           do r = get(++s);
           while (r.q == 0);
@@ -1501,16 +1527,13 @@ int attn_ready(int d, bool fp16, int* grid) {
   return KVEV_OK;
 }
 
-// (L2 fetches no more around a row's 128 bytes than they are: with 64-element heads of
-// tokens-first pages the rest would be other heads' rows, 64 generations at 4K 148 us
-// instead of 109)
 bool encode16(CUtensorMap* m, bool fp16, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
               const cuuint32_t* box) {
   auto fn = encode_fn();
   if (!fn) return false;
   const cuuint32_t ones[4] = {1, 1, 1, 1};
   return fn(m, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims,
-            strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, dims[0] == 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
