@@ -51,6 +51,7 @@ def _bind_flags() -> tuple[list[str], list[str]]:
              "-I", os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"),
              "-I", sysconfig.get_paths()["include"], "-I", os.path.join(cuda, "include"), "-I", os.path.join(ROOT, "include")],
             ["-L", libs, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", f"-Wl,-rpath,{libs}",
+             "-L", os.path.join(cuda, "lib64"), "-lcudart",
              "-L", LIBDIR, "-l:libkvev.so", "-Wl,-rpath,$ORIGIN"])
 
 

@@ -44,19 +44,33 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
-# Scratch of the attention calls on a stream, (device, stream) -> (pointer, bytes, tensor): calls on a stream
+# Scratch of the attention calls made on a stream, (device, stream) -> (pointer, bytes, tensor): calls on a stream
 # follow one another, whatever layer they are for, so they share it.
 _workspaces: dict = {}
+# Scratch of the calls that a capture on the stream records, (device, stream) -> (capture's id, the same).  A graph's
+# replays follow neither the stream's calls nor other graphs, so each capture has scratch of its own, from the
+# graph's memory pool, whose counts the graph itself zeroes before its first attention.  Only the last capture's is
+# kept: after a capture its memory is the graph's.
+_captured: dict = {}
 
 
-def _workspace(device: int, stream: int):
+def _scratch(device: int, stream: int):
+    n = kvev.kvev_paged_attention_workspace(1, 1, 128)  # what the largest call needs
+    with torch.cuda.device(device), torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
+        t = torch.empty(n, dtype=torch.uint8, device="cuda")
+        t[:kvev.PAGED_SYNC_BYTES].zero_()
+    return t.data_ptr(), n, t
+
+
+def _workspace(device: int, stream: int, capture: int):
+    if capture:
+        held = _captured.get((device, stream))
+        if held is None or held[0] != capture:
+            held = _captured[device, stream] = (capture, _scratch(device, stream))
+        return held[1]
     ws = _workspaces.get((device, stream))
     if ws is None:
-        n = kvev.kvev_paged_attention_workspace(1, 1, 128)  # what the largest call needs
-        with torch.cuda.device(device), torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
-            t = torch.empty(n, dtype=torch.uint8, device="cuda")
-            t[:kvev.PAGED_SYNC_BYTES].zero_()
-        ws = _workspaces[device, stream] = (t.data_ptr(), n, t)
+        ws = _workspaces[device, stream] = _scratch(device, stream)
     return ws
 
 
@@ -170,17 +184,22 @@ class PagedCache:
             raise kvev.KvevError(rc, "kvev_paged_write")
 
     def workspace(self, H_q: int | None = None, stream=None):
-        """The scratch that attention calls on a stream use, made at the first of them (before a capture of
-        the stream, let one call or this one make it): all layers' calls on a stream share one."""
-        return _workspace(self._device, self._lib.current_stream(self._device) if stream is None else stream.cuda_stream)[2]
+        """The scratch that attention calls on a stream use, made at the first of them or here: all layers' calls
+        on a stream share one, whatever their heads (H_q is not needed).  While the stream is being captured, the
+        capture's own."""
+        return _workspace(self._device, *self._lib.stream(self._device, None if stream is None else stream.cuda_stream))[2]
 
     def attention(self, q, cu, kv_lens, *, scale=0.0, window=0, out=None, lse=None, workspace=None, stream=None):
         """Causal attention of the new tokens' queries q [T][H_q][d] (request s: rows cu[s]..cu[s+1], the last of
-        its kv_lens[s] positions).  lse: fp32 [T][H_q] for the rows' log-sum-exp.  Returns out."""
+        its kv_lens[s] positions).  lse: fp32 [T][H_q] for the rows' log-sum-exp.  Returns out.
+
+        Graphs captured with ``torch.cuda.graph`` may be replayed in any order, beside one another and beside other
+        calls.  A graph captured by other means needs a ``workspace`` that it keeps (uint8 of
+        ``kvev.kvev_paged_attention_workspace`` bytes, the first ``kvev.PAGED_SYNC_BYTES`` zero before its first use)."""
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        at = self._lib.current_stream(self._device) if stream is None else stream.cuda_stream
-        ws = _workspace(self._device, at) if workspace is None else (workspace.data_ptr(), workspace.numel())
+        at, capture = self._lib.stream(self._device, None if stream is None else stream.cuda_stream)
+        ws = _workspace(self._device, at, capture) if workspace is None else (workspace.data_ptr(), workspace.numel())
         rc = self._lib.attention(*self._call, at, q, cu, kv_lens, out, lse, scale, window, ws[0], ws[1])
         if rc:
             raise kvev.KvevError(rc, "kvev_paged_attention")
@@ -197,7 +216,7 @@ class PagedCache:
         v = int(self.device_status.item())
         if v:
             self.device_status.zero_()
-        if v & 1:  # a wait ran out: the pieces counted so far would be counted again
+        if v & 1:  # a wait ran out: the pieces counted so far would be counted again (a graph zeroes its own)
             torch.cuda.synchronize(self._device)
             for (device, _), ws in _workspaces.items():
                 if device == self._device:

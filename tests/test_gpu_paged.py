@@ -483,3 +483,39 @@ def test_one_token_views_with_any_stride(paged):
     k = torch.randn((1, 2, 64), device="cuda").to(BF16)
     c.write(torch.as_strided(k, k.shape, (5, 64, 1)), torch.as_strided(k, k.shape, (64, 64, 1)), ints([7]))
     assert torch.equal(c.K[0, 7], k[0]) and torch.equal(c.V[0, 7], k[0]) and c.status() == 0
+
+
+# ---- captured graphs ------------------------------------------------------------------------------------
+
+def test_graphs_in_any_order_and_side_by_side(paged):
+    """Graphs captured on torch's own capture stream, with no call there before, each with units cut over many CTAs."""
+    cases = []
+    for seed, reqs in enumerate(([(9000, 1), (5, 1)], [(4000, 60), (300, 200)], [(12000, 3)])):
+        c, q, cu, kv, table = attend_case(paged, reqs, 8, 2, 128, 16, BF16, False, seed=seed)
+        dcu, dkv = ints(cu), ints(kv)
+        want = c.attention(q, dcu, dkv)
+        cases.append((c, q, dcu, dkv, want, torch.empty_like(q)))
+    torch.cuda.synchronize()
+    graphs = []
+    for c, q, dcu, dkv, _, out in cases:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            c.attention(q, dcu, dkv, out=out)
+            c.attention(q, dcu, dkv, out=out)
+        graphs.append(g)
+    for order in ((2, 1, 0), (1, 0, 2, 1)):
+        for i in order:
+            cases[i][5].zero_()
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(cases[i][5], cases[i][4])
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(20):  # side by side, and beside calls that no graph holds
+        for case, g, s in zip(cases, graphs, streams):
+            with torch.cuda.stream(s):
+                case[5].zero_()
+                g.replay()
+        again = [c.attention(q, dcu, dkv) for c, q, dcu, dkv, _, _ in cases]
+        torch.cuda.synchronize()
+        for case, o in zip(cases, again):
+            assert torch.equal(case[5], case[4]) and torch.equal(o, case[4]) and case[0].status() == 0
