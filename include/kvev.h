@@ -454,7 +454,8 @@ KVEV_API int kvev_decode_step_attn(kvev_plan *plan, int B, int growth, void *dec
  *   - The slot of a token is page * page_size + row: its row in the pool.
  *   - All calls are asynchronous on `stream`, read lengths and tables on the
  *     device and allocate nothing, so a captured graph can be replayed with
- *     other lengths.  They need no plan.
+ *     other lengths.  They need no plan, and run on the current device, which holds
+ *     the memory.
  *   - num_pages * page_size stays below 2^31, max_pages * page_size and the rows of a
  *     call at or below 2^30, and a call takes at most KVEV_PAGED_MAX_REQUESTS requests
  *     (ENOTSUP).

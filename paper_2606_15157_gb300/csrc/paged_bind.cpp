@@ -1,13 +1,15 @@
 // paged_bind.cpp -- the calls of paged.py on torch tensors: their checks and the call of the
 // C entry point in one function each.  These calls take 2 to 4 us on the device and are made
 // for every layer of every token; through Python's own attribute reads and ctypes the
-// host's share was larger (a tables call 6.1 us, a write 4.4, an attention 8.1; here 2.2, 1.9
+// host's share was larger (a tables call 6.1 us, a write 4.4, an attention 8.1; here 2.3, 2.0
 // and 3.2).
 //
 // Each function returns the entry point's status code and raises ValueError where a tensor has
-// the wrong type, shape or place.
+// the wrong type, shape or place.  The entry points launch on the current device: each call makes
+// the tensors' GPU current for its time.
 #include <Python.h>
 #include <climits>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <cuda_runtime_api.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -109,6 +111,7 @@ PyObject* guarded(Py_ssize_t got, Py_ssize_t want, F f) {
 PyObject* tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 19, [&] {
     const int dev = small(a[7], "device");
+    const c10::cuda::CUDAGuard on(static_cast<c10::DeviceIndex>(dev));
     const int B = requests(count(a[9], "lens"), a[4]), T = small(a[11], "T");
     return kvev_paged_tables(ints(a[9], B, dev, "lens"), ints(a[10], B, dev, "new_lens"), B, small(a[0], "page_size"),
                              small(a[1], "num_pages"), static_cast<int32_t*>(address(a[2])), ints(a[17], 1, dev, "free_count"),
@@ -122,6 +125,7 @@ PyObject* tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* release(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 14, [&] {
     const int dev = small(a[7], "device");
+    const c10::cuda::CUDAGuard on(static_cast<c10::DeviceIndex>(dev));
     const int B = requests(count(a[9], "lens"), a[4]);
     return kvev_paged_release(ints(a[9], B, dev, "lens"), ints(a[10], B, dev, "done"), B, small(a[0], "page_size"),
                               small(a[1], "num_pages"), static_cast<int32_t*>(address(a[3])), small(a[5], "max_pages"),
@@ -136,6 +140,7 @@ PyObject* write(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 10, [&] {
     const kvev_paged_cache& c = cache(a[0]);
     const int dev = small(a[5], "device");
+    const c10::cuda::CUDAGuard on(static_cast<c10::DeviceIndex>(dev));
     const Rows k = rows(a[7], c, dev, "k"), v = rows(a[8], c, dev, "v");
     if (k.heads != c.H_kv || v.heads != k.heads || v.tokens != k.tokens || v.token_stride != k.token_stride ||
         v.head_stride != k.head_stride)
@@ -149,6 +154,7 @@ PyObject* gather(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 10, [&] {
     const kvev_paged_cache& c = cache(a[0]);
     const int dev = small(a[5], "device");
+    const c10::cuda::CUDAGuard on(static_cast<c10::DeviceIndex>(dev));
     const int B = requests(count(a[7], "lens"), a[2]);
     const at::Tensor &K = tensor(a[8], "out_K"), &V = tensor(a[9], "out_V");
     for (const at::Tensor* t : {&K, &V}) {
@@ -167,6 +173,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 16, [&] {
     const kvev_paged_cache& c = cache(a[0]);
     const int dev = small(a[5], "device");
+    const c10::cuda::CUDAGuard on(static_cast<c10::DeviceIndex>(dev));
     const Rows q = rows(a[7], c, dev, "q"), out = rows(a[10], c, dev, "out");
     const int B = requests(count(a[9], "kv_lens"), a[2]);
     if (out.tokens != q.tokens || out.heads != q.heads) refuse("out", "q's shape");
@@ -189,11 +196,13 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // (device, stream): the stream's number (the current one's for None), and the id of the capture that it is part of, 0 if
-// none.  (An attention call 2.8 us with it on the host, 2.6 without.)
+// none.  (0.2 us of an attention call.)
 PyObject* stream(PyObject*, PyObject* const* a, Py_ssize_t n) {
   try {
     if (n != 2) throw Refused();
-    const cudaStream_t s = static_cast<cudaStream_t>(stream_of(a[1], small(a[0], "device")));
+    const int dev = small(a[0], "device");
+    const c10::cuda::CUDAGuard on(static_cast<c10::DeviceIndex>(dev));
+    const cudaStream_t s = static_cast<cudaStream_t>(stream_of(a[1], dev));
     cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
     unsigned long long id = 0;
     const cudaError_t e = cudaStreamGetCaptureInfo(s, &status, &id);

@@ -101,3 +101,81 @@ def test_scratch_of_streams_forked_in_a_capture(host):
     b = attend(c)
     c.fake.current = 11
     assert a != b and attend(c) == a
+
+
+# ---- the extension module's calls, with a stub in the library's place ---------------------------------
+
+@pytest.fixture(scope="module")
+def stubbed(tmp_path_factory):
+    """(module, stub): kvev_paged_bind linked against tests/paged_bind_stub.cpp."""
+    import ctypes
+    import importlib.util
+    import os
+    import subprocess
+
+    from paper_2606_15157_gb300 import build
+    build.build()
+    tmp = tmp_path_factory.mktemp("bind")
+    cflags, lflags = build._bind_flags()
+    obj, so = str(tmp / "stub.o"), str(tmp / build.BIND)
+    subprocess.run([build.CXX, *cflags, "-c", os.path.join(build.ROOT, "tests", "paged_bind_stub.cpp"), "-o", obj], check=True)
+    subprocess.run([build.CXX, "-shared", "-Wl,-Bsymbolic", "-o", so, os.path.join(build.OBJDIR, "paged_bind.cpp.o"), obj,
+                    *(f for f in lflags if "libkvev" not in f)], check=True)
+    spec = importlib.util.spec_from_file_location("kvev_paged_bind", so)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m, ctypes.CDLL(so)
+
+
+def on(device, dtype, *size):
+    """A tensor that says it is on that GPU; nothing reads its memory."""
+    stride = [1] * len(size)
+    for i in range(len(size) - 2, -1, -1):
+        stride[i] = stride[i + 1] * max(size[i + 1], 1)
+    n = max(1, stride[0] * size[0]) * torch.empty(0, dtype=dtype).element_size()
+    storage = torch._C._construct_storage_from_data_pointer(1 << 20, torch.device("cuda", device), n)
+    return torch._C._construct_CUDA_Tensor_From_Storage_And_Metadata(
+        {"storage_offset": 0, "dtype": dtype, "size": size, "stride": tuple(stride)}, storage)
+
+
+def bind_calls(m, dev):
+    """The five calls on tensors of GPU `dev`, on a stream given by number."""
+    import ctypes
+
+    from paper_2606_15157_gb300 import kvev
+    i32, bf = torch.int32, torch.bfloat16
+    I = lambda *n: on(dev, i32, *n)  # noqa: E731
+    global desc  # (the calls hold its address)
+    desc = kvev.PagedCacheDesc(1 << 20, 1 << 20, 16 * 128, 128, 64, 8, 16, 2, 64, kvev.BF16)
+    P = 1 << 20
+    pool, cache = (16, 8, P, P, 2, 4, P, dev), (ctypes.addressof(desc), P, 2, 4, P, dev)
+    rows, q, kv = on(dev, bf, 3, 2, 64), on(dev, bf, 3, 4, 64), on(dev, bf, 2, 2, 32, 64)
+    return {"tables": lambda: m.tables(*pool, 5, I(2), I(2), 3, I(2), I(3), I(3), I(3), I(2), I(1), I(1)),
+            "release": lambda: m.release(*pool, 5, I(2), I(2), I(2), I(1), I(1)),
+            "write": lambda: m.write(*cache, 5, rows, rows, I(3)),
+            "gather": lambda: m.gather(*cache, 5, I(2), kv, kv),
+            "attention": lambda: m.attention(*cache, 5, q, I(3), I(2), q, None, 0.0, 0, P, 1 << 30)}
+
+
+@pytest.mark.parametrize("name", ["tables", "release", "write", "gather", "attention"])
+@pytest.mark.parametrize("current,dev", [(0, 1), (1, 0), (1, 1)])
+def test_calls_run_on_the_tensors_gpu(stubbed, name, current, dev):
+    import ctypes
+    m, stub = stubbed
+    at, seen = ctypes.c_int.in_dll(stub, "stub_device"), ctypes.c_int.in_dll(stub, "stub_seen")
+    at.value, seen.value = current, -1
+    assert bind_calls(m, dev)[name]() == 0
+    assert seen.value == dev and at.value == current  # and the caller's device is current again
+
+
+def test_a_refused_call_leaves_the_current_gpu(stubbed):
+    import ctypes
+    m, stub = stubbed
+    at, calls = ctypes.c_int.in_dll(stub, "stub_device"), ctypes.c_int.in_dll(stub, "stub_calls")
+    at.value = 0
+    before = calls.value
+    f = bind_calls(m, 1)
+    wrong = on(0, torch.int32, 2)  # on another GPU than the cache
+    with pytest.raises(ValueError):
+        m.release(16, 8, 1 << 20, 1 << 20, 2, 4, 1 << 20, 1, 5, wrong, wrong, wrong, wrong, wrong)
+    assert at.value == 0 and calls.value == before and f["write"]() == 0
