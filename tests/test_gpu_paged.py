@@ -396,6 +396,19 @@ def test_attention_many_requests(paged):
     check(paged, reqs, 4, 2, 64, 16)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B", [31, 32, 33, 64, 383, 384, 385, 700])
+def test_attention_batches_around_the_schedule_s_sizes(paged, B, d):
+    # the schedule of a warp, of a block in one pass and in several, in both orders of units: requests
+    # without rows (the first and last among them), single tokens, chunks, and contexts cut over many CTAs
+    rng = random.Random(f"{B}/{d}")
+    reqs = [(n, min(n, rng.choice([0, 1, 1, 1, 2, 40, 200]))) for n in (rng.randint(0, 400) for _ in range(B))]
+    reqs[0], reqs[-1] = (50, 0), (0, 0)
+    reqs[rng.randrange(1, B - 1)] = (9000, 1)
+    reqs[rng.randrange(1, B - 1)] = (3000, 300)
+    check(paged, reqs, 6, 3, d, 16)
+
+
 def test_chunks_in_turn_equal_the_prompt_in_one(paged):
     """A ragged batch prefilled chunk by chunk through tables, write and attention against one causal pass."""
     H_q, H, d, page = 8, 2, 128, 16
