@@ -503,8 +503,8 @@ typedef struct kvev_paged_cache {
  *                    token; -1 for a refused request's tokens and for the rows
  *                    from cu_new[B] to T.
  *   free_count_out   device int32: what is left on the stack.  May be free_count.
- * A negative length counts as 0, more new tokens than T are cut off, both with
- * status bit 2.  Asynchronous.  EINVAL: a NULL pointer, B or T < 0, page_size or
+ * A negative length counts as 0, more new tokens than T are cut off, tokens of a
+ * page outside the pool get slot -1, all with status bit 2.  Asynchronous.  EINVAL: a NULL pointer, B or T < 0, page_size or
  * sizes out of range. */
 KVEV_API int kvev_paged_tables(const int32_t *lens, const int32_t *new_lens, int B, int page_size,
                                int num_pages, const int32_t *free_pages, const int32_t *free_count,
@@ -516,7 +516,8 @@ KVEV_API int kvev_paged_tables(const int32_t *lens, const int32_t *new_lens, int
  * stack, request after request and entry after entry, and their lengths become 0:
  * lens_out[s] = done[s] ? 0 : lens[s] (may be lens itself), *free_count_out = the
  * stack's new height (may be free_count).  block_table is only read.  Entries
- * that would not fit on a stack of num_pages are dropped with status bit 2.
+ * outside the pool, and those that would not fit on a stack of num_pages, are left
+ * out with status bit 2.
  * Errors as kvev_paged_tables. */
 KVEV_API int kvev_paged_release(const int32_t *lens, const int32_t *done, int B, int page_size,
                                 int num_pages, const int32_t *block_table, int max_pages,

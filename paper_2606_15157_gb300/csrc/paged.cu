@@ -64,13 +64,27 @@ __device__ __forceinline__ int pages_of(int n, int shift) {
 }
 
 // Every CTA of the cluster is here, and what their threads read before has been read.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+  cluster_arrive();
+  cluster_wait();
 }
 __device__ __forceinline__ int cluster_size() {
   int n;
   asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n));
   return n;
+}
+
+// Sets the flag at this place of every CTA's shared memory (all of them are running).
+__device__ __forceinline__ void cluster_raise(int* flag) {
+  const uint32_t at = smem_u32(flag);
+  for (int r = 0; r < cluster_size(); ++r)
+    asm volatile(
+        "{\n\t.reg .b32 a;\n\t"
+        "mapa.shared::cluster.u32 a, %0, %1;\n\t"
+        "st.shared::cluster.u32 [a], %2;\n\t}" ::"r"(at), "r"(r), "r"(1)
+        : "memory");
 }
 
 __global__ void __launch_bounds__(kTableThreads) tables_kernel(const __grid_constant__ TableParams p) {
@@ -166,10 +180,13 @@ __global__ void __launch_bounds__(kTableThreads) release_kernel(const __grid_con
   int* const len = sm + p.B;    // [B] what is left of the lengths
   __shared__ longlong2 ws[32];
   __shared__ long long carry;
+  __shared__ int any_odd;  // an entry outside the pool comes back
+  const int tid = threadIdx.x;
+  if (tid == 0) { carry = 0; any_odd = 0; }
+  __syncwarp();
+  cluster_arrive();  // (from where it is waited for on, other CTAs may set any_odd)
   pdl_wait();
   pdl_trigger();
-  const int tid = threadIdx.x;
-  if (tid == 0) carry = 0;
   const int top = *p.free_count, count = min(max(top, 0), p.num_pages);
   bool bad = top != count;
   __syncthreads();
@@ -192,29 +209,52 @@ __global__ void __launch_bounds__(kTableThreads) release_kernel(const __grid_con
     if (s < p.B) first[s] = static_cast<int>(min(c + upto.x - k, static_cast<long long>(INT_MAX)));
     __syncthreads();
   }
-  cluster_sync();
-  bad |= carry > p.num_pages - count;
-  const int total = static_cast<int>(min(carry, static_cast<long long>(p.num_pages - count)));
+  const int room = p.num_pages - count;
+  bad |= carry > room;
+  const int total = static_cast<int>(min(carry, static_cast<long long>(room)));
   const int t0 = blockIdx.x * blockDim.x + tid, step = cluster_size() * blockDim.x;
-  if (t0 == 0) *p.count_out = count + total;
-  for (int s = t0; s < p.B; s += step) p.lens_out[s] = len[s];
-  for (int k0 = t0; k0 < total; k0 += 4 * step) {  // four entries in flight per thread
-    int page[4];
+  auto entry = [&](int k) {  // the k-th entry that comes back
+    const int s = find_request(first, p.B, k);
+    return p.table[static_cast<long long>(s) * p.max_pages + k - first[s]];
+  };
+  auto outside = [&](int page) { return static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages); };
+  // Entries outside the pool must not reach the stack: every entry is looked at before the first is put there, and
+  // each CTA is told whether there was one, by the barrier after which outputs may be written.  A thread keeps its
+  // first four, in flight together.
+  int page[4];
+  bool odd = false;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int k = k0 + q * step;
-      if (k >= total) continue;
-      const int s = find_request(first, p.B, k);
-      page[q] = p.table[static_cast<long long>(s) * p.max_pages + k - first[s]];
-    }
+  for (int q = 0; q < 4; ++q) page[q] = t0 + q * step < total ? entry(t0 + q * step) : 0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) odd |= outside(page[q]);
+  for (int k = t0 + 4 * step; k < total; k += step) odd |= outside(entry(k));
+  __syncwarp();
+  cluster_wait();
+  if (odd) cluster_raise(&any_odd);
+  __syncwarp();
+  cluster_sync();
+  for (int s = t0; s < p.B; s += step) p.lens_out[s] = len[s];
+  if (any_odd == 0) {
+    if (t0 == 0) *p.count_out = count + total;
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-      if (k0 + q * step < total) {
-        bad |= static_cast<unsigned>(page[q]) >= static_cast<unsigned>(p.num_pages);
-        p.free_pages[count + k0 + q * step] = page[q];
-      }
+      if (t0 + q * step < total) p.free_pages[count + t0 + q * step] = page[q];
+    for (int k = t0 + 4 * step; k < total; k += step) p.free_pages[count + k] = entry(k);
+  } else if (blockIdx.x == 0) {  // one CTA puts the others there, in order
+    const int all = static_cast<int>(min(carry, static_cast<long long>(INT_MAX)));
+    long long kept = 0;
+    for (long long k0 = 0; k0 < all && kept < room; k0 += blockDim.x) {
+      const int x = k0 + tid < all ? entry(static_cast<int>(k0 + tid)) : -1;
+      const long long upto = kept + block_scan(outside(x) ? 0 : 1, 0, ws).x;
+      if (!outside(x) && upto <= room) p.free_pages[count + upto - 1] = x;
+      __syncthreads();
+      if (tid == blockDim.x - 1) carry = upto;
+      __syncthreads();
+      kept = carry;
+    }
+    if (tid == 0) *p.count_out = count + static_cast<int>(min(kept, static_cast<long long>(room)));
   }
-  if (bad) atomicOr(p.status, kStatusDevice);
+  if (bad || odd) atomicOr(p.status, kStatusDevice);
 }
 
 // ---------------------------------------------------------------------------

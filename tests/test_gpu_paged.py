@@ -532,3 +532,34 @@ def test_graphs_in_any_order_and_side_by_side(paged):
         torch.cuda.synchronize()
         for case, o in zip(cases, again):
             assert torch.equal(case[5], case[4]) and torch.equal(o, case[4]) and case[0].status() == 0
+
+
+# ---- released entries outside the pool --------------------------------------------------------------------
+
+@pytest.mark.parametrize("B,page,ctx,room", [(3, 16, 40, 0), (40, 8, 1500, 0), (700, 8, 1500, 0), (300, 8, 900, 500)])
+def test_release_leaves_out_pages_outside_the_pool(paged, B, page, ctx, room):
+    rng = random.Random(B)
+    lens = [ctx] + [rng.randint(0, ctx) for _ in range(B - 1)]
+    done = [1] + [rng.choice([0, 1, 1]) for _ in range(B - 1)]
+    held = [ref.pages_of(n, page) for n in lens]
+    num_pages, max_pages = sum(held) + 9, max(held) + 1
+    table, free, count = pool_state(rng, lens, page, num_pages, max_pages, B)
+    if room:  # more comes back than the stack holds
+        free, count = [0] * num_pages, num_pages - room
+    bad = 0
+    for s in range(B):
+        for j in range(held[s]):
+            if rng.random() < 0.05 or (s, j) in ((0, 0), (B - 1, held[s] - 1)):
+                table[s][j] = rng.choice([-1, num_pages, 2 ** 31 - 1, -2 ** 31])
+                bad += done[s]
+    back = [table[s][j] for s in range(B) if done[s] for j in range(held[s]) if 0 <= table[s][j] < num_pages]
+    want = (free[:count] + back)[:num_pages]
+    pool = paged.PagePool(num_pages, page, ints(table), ints(free), ints([count]))
+    dlens = ints(lens)
+    pool.release(dlens, ints(done))
+    assert bad and host(pool.free_count) == [len(want)] and host(pool.free)[:len(want)] == want
+    assert host(dlens) == [0 if f else n for n, f in zip(lens, done)] and int(pool.device_status) == 2
+    pool.device_status.zero_()
+    # what is given out afterwards is in the pool, and the last ones first
+    kv, cu, slots, pos, granted = pool.tables(ints([0]), ints([2 * page]), 2 * page)
+    assert host(slots)[::page] == [want[-1] * page, want[-2] * page] and int(pool.device_status) == 0
