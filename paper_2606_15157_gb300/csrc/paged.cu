@@ -260,7 +260,9 @@ __global__ void __launch_bounds__(kTableThreads) release_kernel(const __grid_con
 // ---------------------------------------------------------------------------
 // Rows.  A CTA moves the rows of 2^row_shift tokens, of every head, K and V: its
 // vectors of 16 bytes are numbered head by head, token by token, and a thread has the
-// loads of kBatch of them in flight, K's and V's, before the first store.
+// loads of kBatch of them in flight, K's and V's, before the first store.  Plain loads, not
+// __ldg, here and in the attention: the launches overlap the kernels before them, which may write
+// what is read, so it is constant only from pdl_wait on and not for as long as the grid exists.
 // ---------------------------------------------------------------------------
 struct WriteParams {
   PagedView c;
@@ -303,8 +305,8 @@ __global__ void __launch_bounds__(kRowThreads) write_kernel(const __grid_constan
       if (at[q] < 0) continue;
       at[q] += h * p.c.head_stride + x;
       const long long from = (t0 + k) * p.token_stride + h * p.head_stride + x;
-      a[q] = __ldg(p.k + from);
-      b[q] = __ldg(p.v + from);
+      a[q] = p.k[from];
+      b[q] = p.v[from];
     }
 #pragma unroll
     for (int q = 0; q < kBatch; ++q)
@@ -359,8 +361,8 @@ __global__ void __launch_bounds__(kRowThreads) page_gather_kernel(const __grid_c
       at[q] = -1;
       if (row < 0) continue;
       at[q] = ((out0 + static_cast<long long>(h) * p.S_cap + k) << p.dv_shift) + x;
-      a[q] = __ldg(p.c.K + row + h * p.c.head_stride + x);
-      b[q] = __ldg(p.c.V + row + h * p.c.head_stride + x);
+      a[q] = p.c.K[row + h * p.c.head_stride + x];
+      b[q] = p.c.V[row + h * p.c.head_stride + x];
     }
 #pragma unroll
     for (int q = 0; q < kBatch; ++q)

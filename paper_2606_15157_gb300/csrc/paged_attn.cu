@@ -296,9 +296,9 @@ struct Request {
 };
 __device__ __forceinline__ Request request(const PagedAttnParams& p, int s, bool* bad) {
   Request r;
-  r.c0 = __ldg(p.cu + s);
-  const int c1 = __ldg(p.cu + s + 1);
-  r.kv = __ldg(p.kv_lens + s);
+  r.c0 = p.cu[s];
+  const int c1 = p.cu[s + 1];
+  r.kv = p.kv_lens[s];
   const bool ok = r.c0 >= 0 && c1 >= r.c0 && c1 <= p.T && r.kv >= 0 && r.kv <= (p.max_pages << p.page_shift);
   r.q = ok ? c1 - r.c0 : 0;
   if (!ok) *bad = true;
@@ -581,7 +581,7 @@ __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>&
     const int* row = p.table + static_cast<long long>(uniform(en.s)) * p.max_pages;
     auto page_of = [&](int t) {
       const int k = t * kRows + (lane << box_shift);
-      return t < t1 && lane < boxes && k < khi && k + (1 << box_shift) > klo ? __ldg(row + (k >> p.page_shift)) : INT_MAX;
+      return t < t1 && lane < boxes && k < khi && k + (1 << box_shift) > klo ? row[k >> p.page_shift] : INT_MAX;
     };
     int r0 = page_of(t0), r1 = page_of(t0 + 1), r2 = page_of(t0 + 2);
     // ---- Q tiles ----

@@ -179,3 +179,17 @@ def test_a_refused_call_leaves_the_current_gpu(stubbed):
     with pytest.raises(ValueError):
         m.release(16, 8, 1 << 20, 1 << 20, 2, 4, 1 << 20, 1, 5, wrong, wrong, wrong, wrong, wrong)
     assert at.value == 0 and calls.value == before and f["write"]() == 0
+
+
+# ---- sources ----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("name", ["paged.cu", "paged_attn.cu", "paged.cuh"])
+def test_overlapped_kernels_load_nothing_as_constant(name):
+    """Launches that overlap the kernel before them read what it writes: no load may claim that it is constant while the grid exists."""
+    import os
+    import re
+
+    from paper_2606_15157_gb300 import build
+    with open(os.path.join(build.CSRC, name)) as f:
+        code = re.sub(r"//[^\n]*", "", f.read())
+    assert not re.search(r"__ldg\s*\(|\.global[.\w]*\.nc\b|__restrict__", code)
