@@ -1,14 +1,15 @@
 // paged_bind.cpp -- the calls of paged.py on torch tensors: their checks and the call of the
 // C entry point in one function each.  These calls take 2 to 4 us on the device and are made
 // for every layer of every token; through Python's own attribute reads and ctypes the
-// host's share was larger (a tables call 6.1 us, a write 4.4, an attention 8.1; here 2.3, 2.0
-// and 3.2).
+// host's share was larger (a tables call 6.1 us, a write 4.4, an attention 8.1; here 2.2, 1.9
+// and 2.9).
 //
 // Each function returns the entry point's status code and raises ValueError where a tensor has
 // the wrong type, shape or place.  The entry points launch on the current device: each call makes
 // the tensors' GPU current for its time.
 #include <Python.h>
 #include <climits>
+#include <stdexcept>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <cuda_runtime_api.h>
@@ -58,6 +59,18 @@ int32_t* ints(PyObject* o, int64_t n, int device, const char* name) {
 }
 
 int64_t count(PyObject* o, const char* name) { return tensor(o, name).numel(); }
+
+// Makes the GPU current for the call.  (The guard by itself also asks at its end which one is: 0.1 us of an
+// attention call's 2.9, on the host.)
+struct OnDevice {
+  c10::cuda::OptionalCUDAGuard guard;
+  explicit OnDevice(int device) {
+    c10::DeviceIndex at = -1;
+    const cudaError_t e = c10::cuda::GetDevice(&at);
+    if (e != cudaSuccess) throw std::runtime_error(cudaGetErrorString(e));
+    if (at != device) guard.set_index(static_cast<c10::DeviceIndex>(device));
+  }
+};
 
 // The stream's number, or the device's current stream for None.
 void* stream_of(PyObject* o, int device) {
@@ -111,7 +124,7 @@ PyObject* guarded(Py_ssize_t got, Py_ssize_t want, F f) {
 PyObject* tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 19, [&] {
     const int dev = small(a[7], "device");
-    const c10::cuda::CUDAGuard on(static_cast<c10::DeviceIndex>(dev));
+    const OnDevice on(dev);
     const int B = requests(count(a[9], "lens"), a[4]), T = small(a[11], "T");
     return kvev_paged_tables(ints(a[9], B, dev, "lens"), ints(a[10], B, dev, "new_lens"), B, small(a[0], "page_size"),
                              small(a[1], "num_pages"), static_cast<int32_t*>(address(a[2])), ints(a[17], 1, dev, "free_count"),
@@ -125,7 +138,7 @@ PyObject* tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* release(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 14, [&] {
     const int dev = small(a[7], "device");
-    const c10::cuda::CUDAGuard on(static_cast<c10::DeviceIndex>(dev));
+    const OnDevice on(dev);
     const int B = requests(count(a[9], "lens"), a[4]);
     return kvev_paged_release(ints(a[9], B, dev, "lens"), ints(a[10], B, dev, "done"), B, small(a[0], "page_size"),
                               small(a[1], "num_pages"), static_cast<int32_t*>(address(a[3])), small(a[5], "max_pages"),
@@ -140,7 +153,7 @@ PyObject* write(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 10, [&] {
     const kvev_paged_cache& c = cache(a[0]);
     const int dev = small(a[5], "device");
-    const c10::cuda::CUDAGuard on(static_cast<c10::DeviceIndex>(dev));
+    const OnDevice on(dev);
     const Rows k = rows(a[7], c, dev, "k"), v = rows(a[8], c, dev, "v");
     if (k.heads != c.H_kv || v.heads != k.heads || v.tokens != k.tokens || v.token_stride != k.token_stride ||
         v.head_stride != k.head_stride)
@@ -154,7 +167,7 @@ PyObject* gather(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 10, [&] {
     const kvev_paged_cache& c = cache(a[0]);
     const int dev = small(a[5], "device");
-    const c10::cuda::CUDAGuard on(static_cast<c10::DeviceIndex>(dev));
+    const OnDevice on(dev);
     const int B = requests(count(a[7], "lens"), a[2]);
     const at::Tensor &K = tensor(a[8], "out_K"), &V = tensor(a[9], "out_V");
     for (const at::Tensor* t : {&K, &V}) {
@@ -173,7 +186,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 16, [&] {
     const kvev_paged_cache& c = cache(a[0]);
     const int dev = small(a[5], "device");
-    const c10::cuda::CUDAGuard on(static_cast<c10::DeviceIndex>(dev));
+    const OnDevice on(dev);
     const Rows q = rows(a[7], c, dev, "q"), out = rows(a[10], c, dev, "out");
     const int B = requests(count(a[9], "kv_lens"), a[2]);
     if (out.tokens != q.tokens || out.heads != q.heads) refuse("out", "q's shape");
@@ -201,7 +214,7 @@ PyObject* stream(PyObject*, PyObject* const* a, Py_ssize_t n) {
   try {
     if (n != 2) throw Refused();
     const int dev = small(a[0], "device");
-    const c10::cuda::CUDAGuard on(static_cast<c10::DeviceIndex>(dev));
+    const OnDevice on(dev);
     const cudaStream_t s = static_cast<cudaStream_t>(stream_of(a[1], dev));
     cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
     unsigned long long id = 0;
