@@ -212,14 +212,15 @@ class PagedCache:
             raise kvev.KvevError(rc, "kvev_paged_gather")
 
     def status(self) -> int:
-        """Synchronises, reads and clears the device status word (0: every call so far was in order)."""
+        """Waits for the GPU, whatever the calls' streams, then reads and clears the device status word (0: every
+        call so far was in order)."""
+        torch.cuda.synchronize(self._device)
         v = int(self.device_status.item())
         if v:
             self.device_status.zero_()
-        if v & 1:  # a wait ran out: the pieces counted so far would be counted again (a graph zeroes its own)
-            torch.cuda.synchronize(self._device)
-            for (device, _), ws in _workspaces.items():
-                if device == self._device:
-                    ws[2][:kvev.PAGED_SYNC_BYTES].zero_()
+            if v & 1:  # a wait ran out: the pieces counted so far would be counted again (a graph zeroes its own)
+                for (device, _), ws in _workspaces.items():
+                    if device == self._device:
+                        ws[2][:kvev.PAGED_SYNC_BYTES].zero_()
             torch.cuda.synchronize(self._device)
         return v

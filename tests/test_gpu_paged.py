@@ -563,3 +563,21 @@ def test_release_leaves_out_pages_outside_the_pool(paged, B, page, ctx, room):
     # what is given out afterwards is in the pool, and the last ones first
     kv, cu, slots, pos, granted = pool.tables(ints([0]), ints([2 * page]), 2 * page)
     assert host(slots)[::page] == [want[-1] * page, want[-2] * page] and int(pool.device_status) == 0
+
+
+# ---- streams ------------------------------------------------------------------------------------------------
+
+def test_status_waits_for_every_stream(paged):
+    c = make_cache(paged, 2, 16, 2, 64, ints([[0]]), BF16, False)
+    k = torch.ones((1, 2, 64), dtype=BF16, device="cuda")
+    bad, good = ints([99]), ints([3])
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(1000)
+        c.write(k, k, good)
+    assert c.status() == 0  # (and all kernels are loaded)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(200_000_000)  # 0.1 s
+    c.write(k, k, bad, stream=s)
+    assert c.status() == 2 and c.status() == 0
