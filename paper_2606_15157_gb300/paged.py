@@ -4,13 +4,16 @@
 are a scheduler step.  :class:`PagedCache` is one layer's pages under such a table: ``write`` the new
 tokens' rows, ``attention`` over them, ``gather`` whole prompts for ``Plan.evict_prefill``.  Lengths,
 tables and slots stay on the device throughout.  Argument checks raise ``ValueError`` (shapes, types)
-or ``KvevError`` (what the library refuses).
+or ``KvevError`` (what the library refuses).  Calls run on the current stream or on ``stream``, and what
+they return as new tensors is allocated on that stream: other streams wait for it and keep it
+(``record_stream``) as they do with any tensor of torch's.
 
 These are calls of a few microseconds on the device, made for every layer of every token: the checks
 and the calls themselves are in the extension module ``kvev_paged_bind`` (``csrc/paged_bind.cpp``).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import importlib.util
 import os
@@ -74,6 +77,14 @@ def _workspace(device: int, stream: int, capture: int):
     return ws
 
 
+_here = contextlib.nullcontext()
+
+
+def _on(stream):
+    """Outputs made for a call belong to its stream: what the current one left in their memory may still be in use there."""
+    return _here if stream is None else torch.cuda.stream(stream)
+
+
 def _table(block_table) -> int:
     _need(block_table.dim() == 2 and block_table.is_cuda and block_table.dtype is _I32 and block_table.is_contiguous(),
           "block_table: contiguous int32 [requests][pages] on a GPU")
@@ -124,7 +135,8 @@ class PagePool:
         if kv_lens is None or cu is None or slots is None or positions is None or granted is None:
             B = lens.numel()
             e = lambda t, n: torch.empty(n, dtype=_I32, device=lens.device) if t is None else t
-            kv_lens, cu, slots, positions, granted = e(kv_lens, B), e(cu, B + 1), e(slots, T), e(positions, T), e(granted, B)
+            with _on(stream):
+                kv_lens, cu, slots, positions, granted = e(kv_lens, B), e(cu, B + 1), e(slots, T), e(positions, T), e(granted, B)
         if free_count is None:
             free_count = self.free_count
         rc = self._lib.tables(*self._call, None if stream is None else stream.cuda_stream, lens, new_lens, T, kv_lens, cu, slots,
@@ -197,7 +209,8 @@ class PagedCache:
         calls.  A graph captured by other means needs a ``workspace`` that it keeps (uint8 of
         ``kvev.kvev_paged_attention_workspace`` bytes, the first ``kvev.PAGED_SYNC_BYTES`` zero before its first use)."""
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            with _on(stream):
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         at, capture = self._lib.stream(self._device, None if stream is None else stream.cuda_stream)
         ws = _workspace(self._device, at, capture) if workspace is None else (workspace.data_ptr(), workspace.numel())
         rc = self._lib.attention(*self._call, at, q, cu, kv_lens, out, lse, scale, window, ws[0], ws[1])

@@ -581,3 +581,16 @@ def test_status_waits_for_every_stream(paged):
         torch.cuda._sleep(200_000_000)  # 0.1 s
     c.write(k, k, bad, stream=s)
     assert c.status() == 2 and c.status() == 0
+
+
+def test_new_outputs_on_another_stream(paged):
+    c, q, cu, kv, table = attend_case(paged, [(900, 3), (40, 40)], 8, 2, 128, 16, BF16, False)
+    dcu, dkv = ints(cu), ints(kv)
+    want = c.attention(q, dcu, dkv)
+    pool = paged.PagePool(8, 16, ints([[0] * 4]))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    out = c.attention(q, dcu, dkv, stream=s)
+    got = pool.tables(ints([0]), ints([20]), 20, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and host(got[0]) == [20] and host(got[1]) == [0, 20] and c.status() == 0

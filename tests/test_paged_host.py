@@ -18,6 +18,10 @@ class FakeBind:
         self.calls.append(a)
         return 0
 
+    def tables(self, *a):
+        self.calls.append(a)
+        return 0
+
     def workspace_of_last(self):
         return self.calls[-1][-2:]
 
@@ -101,6 +105,33 @@ def test_scratch_of_streams_forked_in_a_capture(host):
     b = attend(c)
     c.fake.current = 11
     assert a != b and attend(c) == a
+
+
+class FakeStream:
+    cuda_stream = 77
+
+
+@pytest.mark.parametrize("stream,at", [(None, 5), (FakeStream(), 77)])
+def test_outputs_are_allocated_on_the_call_s_stream(host, stream, at):
+    """Memory that the allocator hands out is free for the stream it was asked on: another's work may still read it."""
+    from paper_2606_15157_gb300 import paged
+    c = host
+    c.fake.current = 5
+    attend(c, stream=stream)  # (its scratch)
+    del c.streams[:]
+    q = torch.zeros((1, 1, 64), dtype=torch.bfloat16)
+    out = c.attention(q, None, None, stream=stream)
+    assert [(s, t.data_ptr()) for s, t in c.streams] == [(at, out.data_ptr())] and out.shape == q.shape
+    pool = object.__new__(paged.PagePool)
+    pool._call, pool._lib, pool.free_count = (), c.fake, None
+    del c.streams[:]
+    lens = torch.zeros(2, dtype=torch.int32)
+    got = pool.tables(lens, lens, 3, stream=stream)
+    assert [s for s, _ in c.streams] == [at] * 5 and [t.data_ptr() for _, t in c.streams] == [t.data_ptr() for t in got]
+    assert [t.numel() for t in got] == [2, 3, 3, 3, 2]
+    del c.streams[:]
+    pool.tables(lens, lens, 3, stream=stream, kv_lens=lens)  # some given
+    assert [s for s, _ in c.streams] == [at] * 4
 
 
 # ---- the extension module's calls, with a stub in the library's place ---------------------------------
