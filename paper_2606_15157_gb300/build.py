@@ -4,10 +4,12 @@
 ``libkvev_synth.so``  the device-side synthetic input generator
                       (C ABI of ``include/kvev_synth.h``);
 ``kvev_paged_bind.so`` the extension module through which ``paged.py`` calls ``libkvev.so``
-                      with torch tensors (host code only).
+                      with torch tensors (host code only; left out where torch is not installed).
 
 Translation units are compiled in parallel with nvcc, then linked; a unit is
-rebuilt only when it or a header it includes changed.
+rebuilt only when it or a header it includes changed, the extension module also
+for another torch, Python or compiler.  What fails to build of the extension module
+is raised when the C libraries are there.
 """
 from __future__ import annotations
 
@@ -15,6 +17,7 @@ import concurrent.futures as cf
 import glob
 import os
 import subprocess
+import sys
 import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -38,13 +41,15 @@ BIND = "kvev_paged_bind.so"
 CXX = os.environ.get("CXX", "g++")
 
 
-def _bind_flags() -> tuple[list[str], list[str]]:
-    """(compiler, linker) flags of the extension module: Python's, torch's and CUDA's headers and libraries."""
+def _torch_dir() -> str | None:
     import importlib.util
     spec = importlib.util.find_spec("torch")  # (without importing it)
-    if spec is None:
-        raise RuntimeError(f"{BIND} needs torch's headers and libraries: torch is not installed")
-    torch_dir = os.path.dirname(spec.origin)
+    return None if spec is None else os.path.dirname(spec.origin)
+
+
+def _bind_flags() -> tuple[list[str], list[str]]:
+    """(compiler, linker) flags of the extension module: Python's, torch's and CUDA's headers and libraries."""
+    torch_dir = _torch_dir()
     cuda = os.path.dirname(os.path.dirname(NVCC))
     libs = os.path.join(torch_dir, "lib")
     return (["-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I", os.path.join(torch_dir, "include"),
@@ -61,12 +66,22 @@ def _run(cmd: list[str], what: str):
         raise RuntimeError(f"{what}:\n{r.stdout}\n{r.stderr}")
 
 
+def _bind_made_with() -> str:
+    """What the extension module's object depends on beside the sources."""
+    with open(os.path.join(_torch_dir(), "version.py")) as f:
+        return "\n".join([CXX, *_bind_flags()[0], sys.version, f.read()])
+
+
 def _compile_bind() -> str:
     src, obj = os.path.join(CSRC, "paged_bind.cpp"), os.path.join(OBJDIR, "paged_bind.cpp.o")
-    if _stale(obj, [src] + _headers()):
+    made, want = obj + ".made_with", _bind_made_with()
+    same = os.path.exists(made) and open(made).read() == want
+    if not same or _stale(obj, [src] + _headers()):
         tmp = obj + f".tmp{os.getpid()}"
         _run([CXX, *_bind_flags()[0], "-c", src, "-o", tmp], f"{CXX} failed for {src}")
         os.replace(tmp, obj)
+        with open(made, "w") as f:
+            f.write(want)
     return obj
 
 
@@ -94,15 +109,14 @@ def _compile(src: str, extra: list[str]) -> str:
 
 
 def build(verbose: bool = False, extra: list[str] | None = None) -> dict[str, str]:
-    """Compile every library; returns {name: path}."""
+    """Compile every library; returns {name: path} of those that there are."""
     os.makedirs(OBJDIR, exist_ok=True)
     extra = list(extra or [])
     out = {}
     srcs = sorted({s for v in LIBS.values() for s in v})
     with cf.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 4)) as ex:
-        bind = ex.submit(_compile_bind)
+        bind = ex.submit(_compile_bind) if _torch_dir() else None
         objs = dict(zip(srcs, ex.map(lambda s: _compile(os.path.join(CSRC, s), extra), srcs)))
-        bind_obj = bind.result()
     for lib, units in LIBS.items():
         path = os.path.join(LIBDIR, lib)
         deps = [objs[u] for u in units]
@@ -116,6 +130,11 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> dict[str, st
         if verbose:
             print("built", path)
         out[lib] = path
+    if bind is None:
+        if verbose:
+            print("not built:", BIND, "(torch is not installed)")
+        return out
+    bind_obj = bind.result()
     path = os.path.join(LIBDIR, BIND)
     if _stale(path, [bind_obj, out["libkvev.so"]]):
         tmp = path + f".tmp{os.getpid()}"
