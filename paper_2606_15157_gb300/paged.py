@@ -107,7 +107,8 @@ class PagePool:
     """Free pages and the block table of up to ``block_table.shape[0]`` requests.
 
     ``free`` is the stack's memory, int32 [num_pages]; ``free_count`` (int32 [1], on the device) its
-    height.  Without them the pool starts full, pages 0, 1, ... given out in that order."""
+    height.  Without them the pool starts full, pages 0, 1, ... given out in that order.  With ``free`` alone
+    its own count starts at 0, none free: for programs that hand a count to each call."""
 
     def __init__(self, num_pages: int, page_size: int, block_table, free=None, free_count=None):
         dev = block_table.device
