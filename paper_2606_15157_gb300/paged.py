@@ -77,6 +77,12 @@ def _workspace(device: int, stream: int, capture: int):
     return ws
 
 
+def _given(ws, device: int):
+    _need(isinstance(ws, torch.Tensor) and ws.is_cuda and ws.get_device() == device and ws.is_contiguous(),
+          "workspace: a contiguous tensor on the cache's GPU")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 _here = contextlib.nullcontext()
 
 
@@ -207,13 +213,13 @@ class PagedCache:
         its kv_lens[s] positions).  lse: fp32 [T][H_q] for the rows' log-sum-exp.  Returns out.
 
         Graphs captured with ``torch.cuda.graph`` may be replayed in any order, beside one another and beside other
-        calls.  A graph captured by other means needs a ``workspace`` that it keeps (uint8 of
-        ``kvev.kvev_paged_attention_workspace`` bytes, the first ``kvev.PAGED_SYNC_BYTES`` zero before its first use)."""
+        calls.  A graph captured by other means needs a ``workspace`` that it keeps
+        (``kvev.kvev_paged_attention_workspace`` bytes, 256-byte aligned, the first ``kvev.PAGED_SYNC_BYTES`` zero before its first use)."""
         if out is None:
             with _on(stream):
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         at, capture = self._lib.stream(self._device, None if stream is None else stream.cuda_stream)
-        ws = _workspace(self._device, at, capture) if workspace is None else (workspace.data_ptr(), workspace.numel())
+        ws = _workspace(self._device, at, capture) if workspace is None else _given(workspace, self._device)
         rc = self._lib.attention(*self._call, at, q, cu, kv_lens, out, lse, scale, window, ws[0], ws[1])
         if rc:
             raise kvev.KvevError(rc, "kvev_paged_attention")

@@ -224,3 +224,18 @@ def test_overlapped_kernels_load_nothing_as_constant(name):
     with open(os.path.join(build.CSRC, name)) as f:
         code = re.sub(r"//[^\n]*", "", f.read())
     assert not re.search(r"__ldg\s*\(|\.global[.\w]*\.nc\b|__restrict__", code)
+
+
+# ---- scratch given by the caller ------------------------------------------------------------------------
+
+def test_scratch_given_is_checked_and_counted_in_bytes(host):
+    c = host
+    given = on(0, torch.float32, 1000)
+    assert attend(c, workspace=given) == given.data_ptr() and c.fake.workspace_of_last()[1] == 4000
+    made = len(c.fake.calls)
+    rows = torch._C._construct_CUDA_Tensor_From_Storage_And_Metadata(
+        {"storage_offset": 0, "dtype": torch.uint8, "size": (4, 8), "stride": (16, 1)}, given.untyped_storage())
+    for bad in (torch.zeros(1000), on(1, torch.uint8, 1000), rows, 12345):
+        with pytest.raises(ValueError):
+            attend(c, workspace=bad)
+    assert len(c.fake.calls) == made
