@@ -498,7 +498,8 @@ typedef struct kvev_paged_cache {
  *                    May be lens itself.
  *   cu_new           device int32 [B + 1]: first token of each request among the
  *                    new tokens, laid out request after request; cu_new[B] is
- *                    their number (refused requests' tokens included).
+ *                    their number (refused requests' tokens included; cut off at
+ *                    2^31 - 1).
  *   slots, positions device int32 [T]: the slot and the position of each new
  *                    token; -1 for a refused request's tokens and for the rows
  *                    from cu_new[B] to T.

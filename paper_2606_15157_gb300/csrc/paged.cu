@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(kTableThreads) tables_kernel(const __grid_cons
   int* const cu = sm;                     // [B + 1] first token
   int* const first = sm + p.B + 1;        // [B] new pages of the requests before
   int* const len = sm + 2 * p.B + 1;      // [B] tokens held
-  int* const granted = sm + 3 * p.B + 1;  // [B]
+  int* const grant = sm + 3 * p.B + 1;    // [B] new tokens, -1: refused
   __shared__ longlong2 ws[32];
   __shared__ long long carry[2];
   __shared__ int given;
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kTableThreads) tables_kernel(const __grid_cons
       cu[s] = static_cast<int>(min(c0 + upto.x - q, static_cast<long long>(INT_MAX)));
       first[s] = static_cast<int>(min(c1 + upto.y - k, static_cast<long long>(INT_MAX)));
       len[s] = n;
-      granted[s] = ok;
+      grant[s] = ok ? q : -1;
       if (ok && k > 0) atomicMax(&given, static_cast<int>(c1 + upto.y));
     }
     __syncthreads();
@@ -143,8 +143,8 @@ __global__ void __launch_bounds__(kTableThreads) tables_kernel(const __grid_cons
   for (int s = t0; s <= p.B; s += step) {
     p.cu[s] = cu[s];
     if (s < p.B) {
-      p.granted[s] = granted[s];
-      p.kv_lens[s] = granted[s] ? len[s] + (cu[s + 1] - cu[s]) : len[s];
+      p.granted[s] = grant[s] >= 0;
+      p.kv_lens[s] = len[s] + max(grant[s], 0);  // (not from cu, which is cut off at INT_MAX)
     }
   }
   // pages given out, the k-th of them to the request whose range holds k
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kTableThreads) tables_kernel(const __grid_cons
     int slot = -1, pos = -1;
     if (t < total) {
       const int s = find_request(cu, p.B, t);
-      if (granted[s]) {
+      if (grant[s] >= 0) {
         pos = len[s] + t - cu[s];
         const int j = pos >> p.page_shift, held = pages_of(len[s], p.page_shift);
         const int page = j < held ? p.table[static_cast<long long>(s) * p.max_pages + j]

@@ -594,3 +594,15 @@ def test_new_outputs_on_another_stream(paged):
     got = pool.tables(ints([0]), ints([20]), 20, stream=s)
     torch.cuda.synchronize()
     assert torch.equal(out, want) and host(got[0]) == [20] and host(got[1]) == [0, 20] and c.status() == 0
+
+
+# ---- sums past 32 bits ----------------------------------------------------------------------------------------
+
+def test_tables_lengths_behind_refused_requests_of_any_size(paged):
+    big = 2 ** 31 - 1
+    pool = paged.PagePool(64, 16, ints([[60, -1], [61, -1], [62, -1], [63, -1]]), ints(list(range(64))), ints([60]))
+    kv, cu, slots, pos, granted = pool.tables(ints([0, 0, 5, 15]), ints([big, big, 3, 2]), 16)
+    assert host(granted) == [0, 0, 1, 1] and host(kv) == [0, 0, 8, 17]
+    assert host(cu) == [0, big, big, big, big]  # cut off at the most that an int holds
+    assert host(slots) == [-1] * 16 and host(pos) == [-1] * 16 and int(pool.device_status) == 2
+    assert host(pool.free_count) == [59] and host(pool.block_table)[3] == [63, 59]
