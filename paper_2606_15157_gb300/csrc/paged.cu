@@ -501,7 +501,7 @@ extern "C" int kvev_paged_gather(const kvev_paged_cache* cache, const int32_t* b
   p.out_V = static_cast<uint4*>(out_V);
   p.status = device_status;
   p.dv_shift = log2_of(p.c.dv);
-  p.blocks = (S_cap + (1 << kGatherShift) - 1) >> kGatherShift;
+  p.blocks = ((S_cap - 1) >> kGatherShift) + 1;
   if (static_cast<int64_t>(p.blocks) * B > INT_MAX) return KVEV_ENOTSUP;  // CTAs of a launch
   return launched(launch_overlapped(page_gather_kernel, p, p.blocks * B, kRowThreads, 0, static_cast<cudaStream_t>(stream)));
 }

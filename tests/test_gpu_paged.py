@@ -606,3 +606,15 @@ def test_tables_lengths_behind_refused_requests_of_any_size(paged):
     assert host(cu) == [0, big, big, big, big]  # cut off at the most that an int holds
     assert host(slots) == [-1] * 16 and host(pos) == [-1] * 16 and int(pool.device_status) == 2
     assert host(pool.free_count) == [59] and host(pool.block_table)[3] == [63, 59]
+
+
+def test_gather_into_rows_of_the_largest_capacity(paged):
+    import ctypes
+    c = make_cache(paged, 4, 16, 1, 64, ints([[2, 1]]), BF16, False)
+    o = torch.zeros((2, 20, 64), dtype=BF16, device="cuda")  # of one request and head: the rows past lens are not touched
+    lens = ints([20])
+    rc = kvev.kvev_paged_gather(ctypes.addressof(c.desc), c.block_table.data_ptr(), 2, lens.data_ptr(), 1, 2 ** 31 - 1,
+                                o[0].data_ptr(), o[1].data_ptr(), c.device_status.data_ptr(),
+                                torch.cuda.current_stream().cuda_stream)
+    assert rc == kvev.OK and c.status() == 0
+    assert torch.equal(o[0, :16], c.K[2, :, 0]) and torch.equal(o[1, 16:], c.V[1, :4, 0])
