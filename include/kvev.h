@@ -457,8 +457,8 @@ KVEV_API int kvev_decode_step_attn(kvev_plan *plan, int B, int growth, void *dec
  *     other lengths.  They need no plan, and run on the current device, which holds
  *     the memory.
  *   - num_pages * page_size stays below 2^31, max_pages * page_size and the rows of a
- *     call at or below 2^30, and a call takes at most KVEV_PAGED_MAX_REQUESTS requests
- *     (ENOTSUP).
+ *     call at or below 2^30 (EINVAL), and a call takes at most
+ *     KVEV_PAGED_MAX_REQUESTS requests (ENOTSUP).
  *   - device_status: required device int32 in which the kernels record status
  *     bits (1 = a bounded wait ran out, 2 = a length, slot or page out of range,
  *     which the kernels skip); the calls only add bits, the caller clears it. */
@@ -530,7 +530,7 @@ KVEV_API int kvev_paged_release(const int32_t *lens, const int32_t *done, int B,
  *   k, v   device [T][H_kv][d] of the cache's type, with token_stride and
  *          head_stride elements (multiples of 8) from token to token and head to
  *          head, 16-byte aligned: slices of a fused projection need no copy.
- * Two tokens with one slot leave either's row.  A slot past the pool is skipped
+ * Two tokens with one slot leave a mix of their rows.  A slot past the pool is skipped
  * with status bit 2.  EINVAL: NULL or misaligned pointers, strides or sizes out
  * of range. */
 KVEV_API int kvev_paged_write(const kvev_paged_cache *cache, const void *k, const void *v,

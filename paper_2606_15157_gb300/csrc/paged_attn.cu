@@ -40,7 +40,7 @@
 //     (1,640 and 1,220 cycles a tile, the tensor core's own work 1,024 of the sides' 2,860);
 //     tensor pipe active 70 %.  Four chunks of 1,200 tokens over 9,000 408 us, 1,620
 //     TFLOP/s; the last 4K of a 32K prompt 1.20 ms, 1,722 (1.40 ms under the power cap, the
-//     clock at 1.64 of 2.07 GHz).  An 8K prompt 350-380 us: 1,024 units whose start
+//     clock at 1.64 of 2.07 GHz).  An 8K prompt 350-385 us: 1,024 units whose start
 //     and end cost 3 tiles.
 // Measured against it: MMAs issued by a thread per side, whose products interleave, 664 us
 // for 541; by one thread for both 586; four softmax warpgroups of 64 columns each (96
@@ -108,9 +108,16 @@ struct AttnSmem {
   static constexpr int kTileBytes = kRows * D * 2;
   // Units lie request by request, head by head; with 64-element heads head by head, request by request: the
   // heads of the same tokens, 128 bytes each next to one another in tokens-first pages, of which L2 fetches
-  // 256, are then read by different CTAs at about the same time.  (64 generations at 4K 148 us in the
-  // first order, 108 with L2 fetching 128, 101 so; on a faster box 91 either way.  128-element heads:
-  // generations the same within 1 %, four chunks of 1,200 over 9,000 409 us in the first order, 421 in the other.)
+  // 256, are then read by different CTAs at about the same time.  Pages with heads first and chunks gain nothing
+  // by it and lose nothing, so the head's size alone decides.  Us in the first order and in the other, 32 query
+  // and 8 KV heads of 64, pages of 16:
+  //                             tokens first     heads first
+  //   64 generations at 4K       150.1  105.9     90.3   90.2
+  //   16 at 16K                  133.6  108.7     90.6   89.4
+  //   4 chunks of 1,200/9,000    318.6  317.5    318.2  317.2
+  //   an 8K prompt               278.9  278.3    278.9  278.2
+  // 128-element heads stay in the first: generations the same within 1 %, four chunks of 1,200 over 9,000
+  // 409 us, 421 in the other.
   static constexpr bool kHeadsOuter = D == 64;
   static constexpr int kStages = D == 128 ? 5 : 10;
   // (with 64-element rows the transposed products also read the tile's size of
