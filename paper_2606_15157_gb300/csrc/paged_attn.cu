@@ -34,7 +34,7 @@
 //
 // Bounds and measurements (one GB300, 32 query and 8 KV heads of 128, pages of 16):
 //   - generations: HBM.  64 at 4K 160 us, 6.7 TB/s; 16 at 16K 158 us, 6.8 TB/s.  One at 4K
-//     10.2 us: the dependent steps of one pass (schedule 2 us, first tiles 1.5, products
+//     10.3 us: the dependent steps of one pass (schedule 2 us, first tiles 1.5, products
 //     and softmax 2, records and merge 2), the launch 2.
 //   - chunks: a side's softmax and the two products after it, which wait for one another
 //     (1,640 and 1,220 cycles a tile, the tensor core's own work 1,024 of the sides' 2,860);
