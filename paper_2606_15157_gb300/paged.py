@@ -213,8 +213,9 @@ class PagedCache:
         its kv_lens[s] positions).  lse: fp32 [T][H_q] for the rows' log-sum-exp.  Returns out.
 
         Graphs captured with ``torch.cuda.graph`` may be replayed in any order, beside one another and beside other
-        calls.  A graph captured by other means needs a ``workspace`` that it keeps
-        (``kvev.kvev_paged_attention_workspace`` bytes, 256-byte aligned, the first ``kvev.PAGED_SYNC_BYTES`` zero before its first use)."""
+        calls (graphs that share a memory pool one after another, as torch has it).  A graph captured by other means needs a ``workspace`` that it keeps
+        (``kvev.kvev_paged_attention_workspace`` bytes, 256-byte aligned, the first ``kvev.PAGED_SYNC_BYTES`` zero
+        before its first use)."""
         if out is None:
             with _on(stream):
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
