@@ -590,6 +590,80 @@ KVEV_API int kvev_paged_attention(const kvev_paged_cache *cache, const void *q, 
                                   int64_t out_head_stride, float *lse, void *workspace,
                                   size_t workspace_bytes, int32_t *device_status, void *stream);
 
+/* ---- paged caches: requests that share a prefix ---------------------------------- */
+
+/* kvev_paged_attention() for a batch in which groups of requests begin with the same
+ * tokens, held once: the block-table rows of a group's requests name the same pages
+ * for them.  What kvev_paged_attention() without a window gives, but a group's common
+ * keys are read once for all of its rows (up to 256 / (H_q / H_kv) tokens' at a time), and
+ * each request's own keys beside them.
+ *   groups      device int32 [N + 1], ascending in 0..B: group g is the requests
+ *               groups[g] .. groups[g + 1] - 1; a request of no group attends to its pages alone.
+ *   shared_lens device int32 [N]: so many tokens are the same for all requests of the
+ *               group.  What does not fill a page is left to each request, and so are the
+ *               common tokens of a request that holds fewer before its new ones, and
+ *               those of a group of one request.
+ *   N           0 .. KVEV_PAGED_MAX_REQUESTS - B.
+ * Pages of the common tokens are taken from the block-table row of the group's first request.
+ * A row's two parts are held as fp32 in the workspace and put together by their
+ * log-sum-exp.  A shared length that is negative or more than max_pages * page_size
+ * counts as 0, and groups that do not ascend as none, both with status bit 2; the rest, errors among it,
+ * as kvev_paged_attention().  EINVAL also: N < 0, groups or shared_lens NULL with N > 0; ENOTSUP: B + N past
+ * KVEV_PAGED_MAX_REQUESTS. */
+KVEV_API int kvev_paged_attention_shared(const kvev_paged_cache *cache, const void *q, int64_t q_token_stride,
+                                         int64_t q_head_stride, const int32_t *cu_new, const int32_t *kv_lens,
+                                         const int32_t *block_table, int max_pages, int B, int T, int H_q,
+                                         float scale, const int32_t *groups, const int32_t *shared_lens, int N,
+                                         void *out, int64_t out_token_stride, int64_t out_head_stride,
+                                         float *lse, void *workspace, size_t workspace_bytes,
+                                         int32_t *device_status, void *stream);
+
+/* Scratch of kvev_paged_attention_shared() with up to T rows: as
+ * kvev_paged_attention_workspace(), which a call with N = 0 needs, and the rows' parts. */
+KVEV_API int kvev_paged_attention_shared_workspace(int H_q, int H_kv, int d, int T, size_t *bytes);
+
+/* ---- paged caches of 8 bits -------------------------------------------------------- */
+
+/* One layer's pages as e4m3 codes (sign, 4 exponent and 3 mantissa bits; no infinity,
+ * 0x7f and 0xff NaN) with a power of two for each token and head.  A row x of d elements,
+ * a the largest magnitude of its finite ones, is held as
+ *   e = the smallest whole number with a <= 448 * 2^e, within -120 .. 120 (bf16) or
+ *       -15 .. 8 (fp16), in the byte e + 127, and
+ *   c = e4m3(x * 2^-e), rounded to nearest, ties to even, within +-448 (+-240 where e is the largest),
+ * NaN for a NaN or infinite element.  c * 2^e is a value of the 16-bit type, so reading back rounds
+ * nothing; a power of two keeps every rounding at the codes' own half step.
+ * Codes are bytes with strides as in kvev_paged_cache (in elements, multiples of 16, positive, K and V
+ * 16-byte aligned); the byte of (page p, token row r, head h) is at
+ * p * scale_page_stride + h * page_size + r of K_scale and of V_scale (scale_page_stride >=
+ * H_kv * page_size).  dtype: KVEV_BF16 or KVEV_FP16, the type of rows written, read back and
+ * attended with.  Bytes outside those ranges, which kvev_paged_q8_write() leaves nowhere, stand for no value. */
+typedef struct kvev_paged_q8_cache {
+  void *K, *V;
+  uint8_t *K_scale, *V_scale;
+  int64_t page_stride, token_stride, head_stride, scale_page_stride;
+  int32_t num_pages, page_size, H_kv, d;
+  int32_t dtype;
+} kvev_paged_q8_cache;
+
+/* kvev_paged_write(), the rows quantised on their way. */
+KVEV_API int kvev_paged_q8_write(const kvev_paged_q8_cache *cache, const void *k, const void *v,
+                                 int64_t token_stride, int64_t head_stride, const int32_t *slots, int T,
+                                 int32_t *device_status, void *stream);
+
+/* kvev_paged_gather(), the rows as the values that they stand for, in the cache's 16-bit type. */
+KVEV_API int kvev_paged_q8_gather(const kvev_paged_q8_cache *cache, const int32_t *block_table, int max_pages,
+                                  const int32_t *lens, int B, int S_cap, void *out_K, void *out_V,
+                                  int32_t *device_status, void *stream);
+
+/* kvev_paged_attention() over the values that the codes stand for; q and out in the cache's 16-bit type.
+ * The workspace is that of kvev_paged_attention_workspace(). */
+KVEV_API int kvev_paged_q8_attention(const kvev_paged_q8_cache *cache, const void *q, int64_t q_token_stride,
+                                     int64_t q_head_stride, const int32_t *cu_new, const int32_t *kv_lens,
+                                     const int32_t *block_table, int max_pages, int B, int T, int H_q,
+                                     float scale, int window, void *out, int64_t out_token_stride,
+                                     int64_t out_head_stride, float *lse, void *workspace,
+                                     size_t workspace_bytes, int32_t *device_status, void *stream);
+
 /* ---- measurement ---------------------------------------------------------- */
 
 /* Kernels of one kvev_evict_prefill() call, in launch order. */

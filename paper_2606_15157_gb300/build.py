@@ -3,12 +3,13 @@
 ``libkvev.so``        the eviction library (C ABI of ``include/kvev.h``);
 ``libkvev_synth.so``  the device-side synthetic input generator
                       (C ABI of ``include/kvev_synth.h``);
-``kvev_paged_bind.so`` the extension module through which ``paged.py`` calls ``libkvev.so``
+``kvev_paged_bind.so``, ``kvev_paged_q8_bind.so``
+                      the extension modules through which ``paged.py`` calls ``libkvev.so``
                       with torch tensors (host code only; left out where torch is not installed).
 
 Translation units are compiled in parallel with nvcc, then linked; a unit is
-rebuilt only when it or a header it includes changed, the extension module also
-for another torch, Python or compiler.  What fails to build of the extension module
+rebuilt only when it or a header it includes changed, the extension modules also
+for another torch, Python or compiler.  What fails to build of the extension modules
 is raised when the C libraries are there.
 """
 from __future__ import annotations
@@ -32,12 +33,13 @@ FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", 
 
 LIBS = {
     "libkvev.so": ["api.cu", "score.cu", "h2o_full.cu", "select.cu", "gather.cu", "decode.cu", "planner.cu",
-                   "paged.cu", "paged_attn.cu"],
+                   "paged.cu", "paged_attn.cu", "paged_shared.cu", "paged_q8.cu", "paged_q8_attn.cu"],
     "libkvev_synth.so": ["synth.cu"],
 }
 
 
 BIND = "kvev_paged_bind.so"
+BINDS = {BIND: "paged_bind.cpp", "kvev_paged_q8_bind.so": "paged_q8_bind.cpp"}
 CXX = os.environ.get("CXX", "g++")
 
 
@@ -48,7 +50,7 @@ def _torch_dir() -> str | None:
 
 
 def _bind_flags() -> tuple[list[str], list[str]]:
-    """(compiler, linker) flags of the extension module: Python's, torch's and CUDA's headers and libraries."""
+    """(compiler, linker) flags of the extension modules: Python's, torch's and CUDA's headers and libraries."""
     torch_dir = _torch_dir()
     cuda = os.path.dirname(os.path.dirname(NVCC))
     libs = os.path.join(torch_dir, "lib")
@@ -67,13 +69,13 @@ def _run(cmd: list[str], what: str):
 
 
 def _bind_made_with() -> str:
-    """What the extension module's object depends on beside the sources."""
+    """What an extension module's object depends on beside the sources."""
     with open(os.path.join(_torch_dir(), "version.py")) as f:
         return "\n".join([CXX, *_bind_flags()[0], sys.version, f.read()])
 
 
-def _compile_bind() -> str:
-    src, obj = os.path.join(CSRC, "paged_bind.cpp"), os.path.join(OBJDIR, "paged_bind.cpp.o")
+def _compile_bind(name: str) -> str:
+    src, obj = os.path.join(CSRC, name), os.path.join(OBJDIR, name + ".o")
     made, want = obj + ".made_with", _bind_made_with()
     same = os.path.exists(made) and open(made).read() == want
     if not same or _stale(obj, [src] + _headers()):
@@ -86,7 +88,7 @@ def _compile_bind() -> str:
 
 
 def _headers():
-    return glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
+    return glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
 
 
 def _stale(target: str, deps: list[str]) -> bool:
@@ -115,7 +117,7 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> dict[str, st
     out = {}
     srcs = sorted({s for v in LIBS.values() for s in v})
     with cf.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 4)) as ex:
-        bind = ex.submit(_compile_bind) if _torch_dir() else None
+        binds = {lib: ex.submit(_compile_bind, src) for lib, src in BINDS.items()} if _torch_dir() else None
         objs = dict(zip(srcs, ex.map(lambda s: _compile(os.path.join(CSRC, s), extra), srcs)))
     for lib, units in LIBS.items():
         path = os.path.join(LIBDIR, lib)
@@ -130,19 +132,20 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> dict[str, st
         if verbose:
             print("built", path)
         out[lib] = path
-    if bind is None:
+    if binds is None:
         if verbose:
-            print("not built:", BIND, "(torch is not installed)")
+            print("not built:", *BINDS, "(torch is not installed)")
         return out
-    bind_obj = bind.result()
-    path = os.path.join(LIBDIR, BIND)
-    if _stale(path, [bind_obj, out["libkvev.so"]]):
-        tmp = path + f".tmp{os.getpid()}"
-        _run([CXX, "-shared", "-o", tmp, bind_obj, *_bind_flags()[1]], f"link failed for {BIND}")
-        os.replace(tmp, path)
-    if verbose:
-        print("built", path)
-    out[BIND] = path
+    for lib, bind in binds.items():
+        bind_obj = bind.result()
+        path = os.path.join(LIBDIR, lib)
+        if _stale(path, [bind_obj, out["libkvev.so"]]):
+            tmp = path + f".tmp{os.getpid()}"
+            _run([CXX, "-shared", "-o", tmp, bind_obj, *_bind_flags()[1]], f"link failed for {lib}")
+            os.replace(tmp, path)
+        if verbose:
+            print("built", path)
+        out[lib] = path
     return out
 
 

@@ -1,0 +1,32 @@
+// paged_q8_attn.cu -- attention over paged caches of 8-bit codes (kernel: paged_attn.cuh).
+#include "paged_attn.cuh"
+
+using namespace kvev;
+
+extern "C" int kvev_paged_q8_attention(const kvev_paged_q8_cache* cache, const void* q, int64_t q_token_stride,
+                                       int64_t q_head_stride, const int32_t* cu_new, const int32_t* kv_lens,
+                                       const int32_t* block_table, int max_pages, int B, int T, int H_q, float scale,
+                                       int window, void* out, int64_t out_token_stride, int64_t out_head_stride,
+                                       float* lse, void* workspace, size_t workspace_bytes, int32_t* device_status,
+                                       void* stream) {
+  PagedQ8View view = {};
+  int rc = paged_q8_view(cache, &view);
+  if (rc != KVEV_OK) return rc;
+  const AttnCall a = {q, q_token_stride, q_head_stride, cu_new, kv_lens, block_table, max_pages, B, T, H_q, scale, window,
+                      out, out_token_stride, out_head_stride, lse, workspace, device_status, static_cast<cudaStream_t>(stream)};
+  bool nothing = false;
+  rc = attn_check(a, cache->H_kv, cache->d, cache->page_size, workspace_bytes, attn_workspace_bytes(cache->d), &nothing);
+  if (rc != KVEV_OK || nothing) return rc;
+  PagedAttnParams p = {};
+  rc = attn_params(a, cache->H_kv, cache->d, view.fp16, cache->page_size, cache->num_pages, &p);
+  if (rc != KVEV_OK) return rc;
+  p.K = view.K;
+  p.V = view.V;
+  p.K_scale = view.K_scale;
+  p.V_scale = view.V_scale;
+  p.page_stride = view.page_stride;
+  p.token_stride = view.token_stride;
+  p.head_stride = view.head_stride;
+  p.scale_page = view.scale_page;
+  return attn_launch<kQ8>(p, cache->d, view.fp16, a.stream);
+}

@@ -38,7 +38,9 @@ EXPORTS = ["kvev_alloc_from_scores", "kvev_alloc_rescale", "kvev_plan_create",
            "kvev_profile_cosine", "kvev_score_ppl", "kvev_score_entropy",
            "kvev_route_toprank", "kvev_route_install", "kvev_plan_save", "kvev_plan_load",
            "kvev_plan_set_h2o_full_prompt", "kvev_paged_tables", "kvev_paged_release", "kvev_paged_write",
-           "kvev_paged_gather", "kvev_paged_attention_workspace", "kvev_paged_attention"]
+           "kvev_paged_gather", "kvev_paged_attention_workspace", "kvev_paged_attention",
+           "kvev_paged_attention_shared", "kvev_paged_attention_shared_workspace", "kvev_paged_q8_write",
+           "kvev_paged_q8_gather", "kvev_paged_q8_attention"]
 KERNEL_NAMES = ["prologue", "score", "select", "gather"]
 
 
@@ -108,6 +110,12 @@ def load(path: str = LIB_PATH):
         L.kvev_paged_attention_workspace.argtypes = [C.c_int, C.c_int, C.c_int, P(sz)]
         L.kvev_paged_attention.argtypes = [vp, vp, i64, i64, vp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_int,
                                            C.c_float, C.c_int, vp, i64, i64, vp, vp, sz, vp, vp]
+        L.kvev_paged_attention_shared.argtypes = [vp, vp, i64, i64, vp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_int,
+                                                  C.c_float, vp, vp, C.c_int, vp, i64, i64, vp, vp, sz, vp, vp]
+        L.kvev_paged_attention_shared_workspace.argtypes = [C.c_int, C.c_int, C.c_int, C.c_int, P(sz)]
+        L.kvev_paged_q8_write.argtypes = L.kvev_paged_write.argtypes
+        L.kvev_paged_q8_gather.argtypes = L.kvev_paged_gather.argtypes
+        L.kvev_paged_q8_attention.argtypes = L.kvev_paged_attention.argtypes
         for name in EXPORTS:
             if name != "kvev_plan_destroy":
                 getattr(L, name).restype = C.c_int
@@ -440,6 +448,44 @@ def kvev_paged_attention(cache, q, q_token_stride, q_head_stride, cu_new, kv_len
     return load().kvev_paged_attention(cache, q, q_token_stride, q_head_stride, cu_new, kv_lens, block_table, max_pages,
                                        B, T, H_q, scale, window, out, out_token_stride, out_head_stride, lse, workspace,
                                        workspace_bytes, device_status, stream)
+
+
+def kvev_paged_attention_shared_workspace(H_q: int, H_kv: int, d: int, T: int) -> int:
+    n = C.c_size_t()
+    _check(load().kvev_paged_attention_shared_workspace(H_q, H_kv, d, T, C.byref(n)), "kvev_paged_attention_shared_workspace")
+    return n.value
+
+
+def kvev_paged_attention_shared(cache, q, q_token_stride, q_head_stride, cu_new, kv_lens, block_table, max_pages, B, T,
+                                H_q, scale, groups, shared_lens, N, out, out_token_stride, out_head_stride, lse,
+                                workspace, workspace_bytes, device_status, stream) -> int:
+    return load().kvev_paged_attention_shared(cache, q, q_token_stride, q_head_stride, cu_new, kv_lens, block_table,
+                                              max_pages, B, T, H_q, scale, groups, shared_lens, N, out, out_token_stride,
+                                              out_head_stride, lse, workspace, workspace_bytes, device_status, stream)
+
+
+class PagedQ8CacheDesc(C.Structure):
+    """``kvev_paged_q8_cache``: one layer's pages of 8-bit codes (strides in elements)."""
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("K_scale", C.c_void_p), ("V_scale", C.c_void_p),
+                ("page_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("scale_page_stride", C.c_int64), ("num_pages", C.c_int32), ("page_size", C.c_int32), ("H_kv", C.c_int32),
+                ("d", C.c_int32), ("dtype", C.c_int32)]
+
+
+def kvev_paged_q8_write(cache, k, v, token_stride, head_stride, slots, T, device_status, stream) -> int:
+    return load().kvev_paged_q8_write(cache, k, v, token_stride, head_stride, slots, T, device_status, stream)
+
+
+def kvev_paged_q8_gather(cache, block_table, max_pages, lens, B, S_cap, out_K, out_V, device_status, stream) -> int:
+    return load().kvev_paged_q8_gather(cache, block_table, max_pages, lens, B, S_cap, out_K, out_V, device_status, stream)
+
+
+def kvev_paged_q8_attention(cache, q, q_token_stride, q_head_stride, cu_new, kv_lens, block_table, max_pages, B, T, H_q,
+                            scale, window, out, out_token_stride, out_head_stride, lse, workspace, workspace_bytes,
+                            device_status, stream) -> int:
+    return load().kvev_paged_q8_attention(cache, q, q_token_stride, q_head_stride, cu_new, kv_lens, block_table, max_pages,
+                                          B, T, H_q, scale, window, out, out_token_stride, out_head_stride, lse, workspace,
+                                          workspace_bytes, device_status, stream)
 
 
 # ---------------------------------------------------------------------------
