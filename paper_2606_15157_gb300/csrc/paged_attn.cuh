@@ -62,10 +62,12 @@ namespace {
 // What the kernel is compiled for, beside head size and type: kShared, groups of requests whose first keys are in
 // common pages, which a unit of the group's rows reads once (paged_shared.cu); kQ8, pages of 8-bit codes, which a
 // warpgroup of its own turns into 16-bit tiles (paged_q8_attn.cu).
-enum Mode : int { kPlain = 0, kShared = 1, kQ8 = 2 };
+// kFewOnly: the requests of few rows, which the kernel of paged_q8_few.cu takes with the codes as they are; kQ8 alone
+// leaves those out.
+enum Mode : int { kPlain = 0, kShared = 1, kQ8 = 2, kFewOnly = 4 };
 template <int kMode>
 struct Split {  // threads, and the warpgroups' registers
-  static constexpr int kThreads = kMode & kQ8 ? 512 : 384;
+  static constexpr int kThreads = (kMode & kQ8) && !(kMode & kFewOnly) ? 512 : 384;
   static constexpr int kControl = kMode & kQ8 ? 48 : 56, kSoftmax = kMode & kQ8 ? 184 : 224, kConvert = 96;
   static constexpr int kNeeded = 128 * kControl + 256 * kSoftmax + (kMode & kQ8 ? 128 * kConvert : 0);
 };
@@ -112,7 +114,9 @@ struct PagedAttnParams {
   const int *groups, *shared;
   int N;
   float *part_o, *part_lse;
-  // kQ8: codes and the rows' exponents, strides in bytes
+  // kQ8: queries, codes and the rows' exponents, strides in bytes
+  const uint8_t* q;
+  long long q_token, q_head;
   const uint8_t *K, *V, *K_scale, *V_scale;
   long long page_stride, token_stride, head_stride, scale_page;
 };
@@ -365,7 +369,11 @@ __device__ __forceinline__ int shared_of_request(const PagedAttnParams& p, int s
 // Request s to schedule; with kShared the first N are the groups over their common keys (ordered: they are in order).
 template <int kMode>
 __device__ __forceinline__ Request request(const PagedAttnParams& p, int s, bool ordered, bool* bad) {
-  if (!(kMode & kShared)) return own_request(p, s, bad);
+  if (!(kMode & kShared)) {
+    Request r = own_request(p, s, bad);
+    if ((kMode & kQ8) && (r.q <= kFewRows / p.G) != ((kMode & kFewOnly) != 0)) r.q = 0;
+    return r;
+  }
   if (s < p.N) {
     Request r = {};
     if (!ordered) return r;
@@ -1065,8 +1073,8 @@ __device__ __forceinline__ Records<D> records(const PagedAttnParams& p, long lon
 }
 
 // After the group's records of a piece are written: whether it is the last of the unit's pieces.
-template <int D>
-__device__ __forceinline__ bool arrived_last(const PagedAttnParams& p, AttnSmem<D>& sm, const Entry& en, int x, bool ok) {
+template <class S>
+__device__ __forceinline__ bool arrived_last(const PagedAttnParams& p, S& sm, const Entry& en, int x, bool ok) {
   group_sync(x);
   if ((threadIdx.x & 127) == 0) {
     int last = 0;
@@ -1679,6 +1687,15 @@ __global__ void __launch_bounds__(Split<kMode>::kThreads, 1) paged_attn_kernel(c
   }
   S& sm = *reinterpret_cast<S*>(smem_raw);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
+  if (kMode & kQ8) {  // (a batch of single tokens leaves nothing to do here)
+    pdl_wait();
+    bool some = false;
+    for (int s = threadIdx.x; s < p.B; s += Split<kMode>::kThreads) {
+      const int c0 = p.cu[s], c1 = p.cu[s + 1];
+      some |= c0 < 0 || c1 > p.T || c1 < c0 || c1 - c0 > kFewRows / p.G;  // (what is out of range is said by the schedule)
+    }
+    if (!__syncthreads_or(some)) return;
+  }
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sm.qfull[i], 1);
@@ -1757,30 +1774,39 @@ AttnFn attn_fn(int d, bool fp16) {
 }
 size_t attn_smem(int d) { return d == 64 ? sizeof(AttnSmem<64>) : sizeof(AttnSmem<128>); }
 
+// CTAs to launch of a kernel, per device; 0: it is not ready there yet.
+struct AttnReady {
+  static constexpr int kDevices = 64;
+  std::atomic<int> ctas[kDevices];
+};
+
 // Readies a kernel for the current device, once: its registers have to cover the
 // warpgroups' split (an increase that the launch's registers cannot cover would never
 // complete), its shared memory limit is raised.  grid: CTAs to launch.
-template <int kMode>
-int attn_ready(int d, bool fp16, int* grid) {
-  constexpr int kDevices = 64;
-  static std::atomic<int> ctas[4][kDevices];  // 0: not yet
+int ready_kernel(AttnReady& r, AttnFn fn, size_t smem, int threads, int registers, int* grid) {
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev >= kDevices) return KVEV_ECUDA;
-  std::atomic<int>& ready = ctas[(d == 64 ? 0 : 2) + (fp16 ? 1 : 0)][dev];
+  if (cudaGetDevice(&dev) != cudaSuccess || dev >= AttnReady::kDevices) return KVEV_ECUDA;
+  std::atomic<int>& ready = r.ctas[dev];
   *grid = ready.load(std::memory_order_relaxed);
   if (*grid > 0) return KVEV_OK;
   int sms = 0;
   cudaFuncAttributes a = {};
-  const AttnFn fn = attn_fn<kMode>(d, fp16);
   if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
       cudaFuncGetAttributes(&a, fn) != cudaSuccess)
     return KVEV_ECUDA;
-  if (a.numRegs * Split<kMode>::kThreads < Split<kMode>::kNeeded) return KVEV_ENOTSUP;
-  if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(attn_smem(d))) != cudaSuccess)
+  if (a.numRegs * threads < registers) return KVEV_ENOTSUP;
+  if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
     return KVEV_ECUDA;
   *grid = sms < kMaxCtas ? sms : kMaxCtas;
   ready.store(*grid, std::memory_order_relaxed);  // (two threads at once: the same values)
   return KVEV_OK;
+}
+
+template <int kMode>
+int attn_ready(int d, bool fp16, int* grid) {
+  static AttnReady ready[4];
+  return ready_kernel(ready[(d == 64 ? 0 : 2) + (fp16 ? 1 : 0)], attn_fn<kMode>(d, fp16), attn_smem(d), Split<kMode>::kThreads,
+                      Split<kMode>::kNeeded, grid);
 }
 
 bool encode16(CUtensorMap* m, bool fp16, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
@@ -1847,6 +1873,9 @@ int attn_params(const AttnCall& a, int H_kv, int d, bool fp16, int page_size, in
     return KVEV_ECUDA;
   p.out = static_cast<uint8_t*>(a.out);
   p.lse = a.lse;
+  p.q = static_cast<const uint8_t*>(a.q);
+  p.q_token = a.q_token * 2;
+  p.q_head = a.q_head * 2;
   p.out_token = a.out_token * 2;
   p.out_head = a.out_head * 2;
   p.cu = a.cu;

@@ -1,5 +1,7 @@
-// paged_q8_attn.cu -- attention over paged caches of 8-bit codes (kernel: paged_attn.cuh).
-#include "paged_attn.cuh"
+// paged_q8_attn.cu -- attention over paged caches of 8-bit codes: a kernel for the requests of few rows, which is bound
+// by the cache's bytes (paged_q8_few.cuh), and one for the others, bound by the products (paged_attn.cuh).  Which
+// request is which only the device knows; the host leaves a kernel out where the number of rows says that it has none.
+#include "paged_q8_few.cuh"
 
 using namespace kvev;
 
@@ -28,5 +30,8 @@ extern "C" int kvev_paged_q8_attention(const kvev_paged_q8_cache* cache, const v
   p.token_stride = view.token_stride;
   p.head_stride = view.head_stride;
   p.scale_page = view.scale_page;
-  return attn_launch<kQ8>(p, cache->d, view.fp16, a.stream);
+  const int few = kFewRows / p.G;  // most tokens of a request of few rows
+  if (few > 0) rc = few_launch(p, cache, a.stream);
+  if (rc == KVEV_OK && T > few) rc = attn_launch<kQ8>(p, cache->d, view.fp16, a.stream);
+  return rc;
 }
