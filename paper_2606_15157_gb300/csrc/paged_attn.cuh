@@ -757,6 +757,28 @@ __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>&
 // which they and their row's power of two have exactly, so that nothing after this differs from 16-bit pages.
 // Rows without a key of the unit, and those of pages outside the pool, become zeros.
 
+// Loads ahead of their use, under a condition, said in PTX: from a plain load with a constant in its place the compiler
+// makes one whose first use, a shift or a product, follows it at once and waits for it (an 8-bit tile's exponents, 4 chunks
+// of codes: %%C).
+__device__ __forceinline__ uint32_t load_byte_if(const uint8_t* at, bool there, uint32_t other) {
+  uint32_t v = other;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %2, 0;\n\t"
+      "@p ld.global.u8 %0, [%1];\n\t}"
+      : "+r"(v) : "l"(at), "r"(static_cast<uint32_t>(there)));
+  return v;
+}
+__device__ __forceinline__ uint4 load16_if(const uint8_t* at, bool there) {
+  uint4 v = make_uint4(0, 0, 0, 0);
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "@p ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+      : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w) : "l"(at), "r"(static_cast<uint32_t>(there)));
+  return v;
+}
+
 // 4 codes times a power of two as 16-bit values; s2: the power twice in 16 bits.
 template <bool kFp16>
 __device__ __forceinline__ uint2 values4(uint32_t codes, uint32_t s2) {
@@ -816,16 +838,11 @@ __device__ __forceinline__ void convert_group(const PagedAttnParams& p, AttnSmem
     auto fetch = [&](int q, int t, bool v, int ids) {  // vector q of tile t
       const int r = r0 + q * kStep, k = t * kRows + r;
       const int page = __shfl_sync(0xffffffffu, ids, r >> 3);
-      x[q] = make_uint4(0, 0, 0, 0);
-      b[q] = 0;
-      if (k < klo || k >= khi) return;
-      if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages)) {
-        atomicOr(p.status, kStatusDevice);
-        return;
-      }
       const int in = k & ((1 << p.page_shift) - 1);
-      x[q] = *reinterpret_cast<const uint4*>((v ? p.V : p.K) + page * p.page_stride + in * p.token_stride + h * p.head_stride + c * 16);
-      b[q] = (v ? p.V_scale : p.K_scale)[page * p.scale_page + (h << p.page_shift) + in];
+      const bool key = k >= klo && k < khi, there = key && static_cast<unsigned>(page) < static_cast<unsigned>(p.num_pages);
+      if (key && !there) atomicOr(p.status, kStatusDevice);
+      x[q] = load16_if((v ? p.V : p.K) + page * p.page_stride + in * p.token_stride + h * p.head_stride + c * 16, there);
+      b[q] = load_byte_if((v ? p.V_scale : p.K_scale) + page * p.scale_page + (h << p.page_shift) + in, there, 0);
     };
 #pragma unroll
     for (int q = 0; q < kV; ++q) fetch(q, t, v, ids);

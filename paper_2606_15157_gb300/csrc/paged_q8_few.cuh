@@ -27,19 +27,24 @@ constexpr int kQParts = 4;       // e4m3 parts of a row of q or of weights
 constexpr float kRest = 32.f;    // what a rest is multiplied by
 constexpr float kFewRaise = 3.f; // a maximum is raised when a tile's is this much above it,
 constexpr float kFewUp = 5.f;    // and the weights are 2^kFewUp larger: up to 2^8
-constexpr int kFewCols = kQParts * kFewRows;  // columns of a side's scores, and of its output
+constexpr int kRowGroup = 4;     // rows that a thread works on at once:
+constexpr int kGroupCols = kQParts * kRowGroup;  // columns [part][row] of such a group
+constexpr int kFewCols = kQParts * kFewRows;     // columns of a side's scores, and of its output: group after group
+constexpr int kFewCtas = 2;      // CTAs of an SM
 
 template <int D>
 struct Q8Smem {
-  static constexpr bool kHeadsOuter = AttnSmem<D>::kHeadsOuter;
+  // rows of 64 or 128 bytes: as for 16-bit rows of 64 elements
+  static constexpr bool kHeadsOuter = true;
   static constexpr int kTileBytes = kRows * D;
-  static constexpr int kStages = D == 128 ? 12 : 24;
+  static constexpr int kStages = D == 128 ? 5 : 10;
   uint8_t kv[kStages][kTileBytes];
-  uint8_t p[2][kFewCols * kRows];  // the sides' weights [part][row][128 keys]
-  uint8_t q[2][kFewCols * D];      // [part][row][D]
-  float qscale[2][kFewRows];       // of the rows: log2(e) scale over their power of two
+  uint8_t p[2][kFewCols * kRows];  // the sides' weights [column][128 keys]
+  uint8_t q[kFewCols * D];         // [column][D]
+  float qscale[2][kFewRows];       // of an entry's rows: log2(e) scale over their power of two
+  float m[2][kFewRows], mz[2][kFewRows], l[2][kFewRows];  // the sides' maxima, the weights' maxima, sums
   Entry ring[kEntries];
-  uint64_t qfull[2], qempty[2], full[kStages], empty[kStages];
+  uint64_t qfull[2], qempty, full[kStages], empty[kStages];  // (qfull: of every other entry)
   uint64_t sfull[2], pfull[2], ofull[2];
   uint64_t efull[kEntries], eempty[kEntries];
   uint64_t xfull, xfree, done;
@@ -48,12 +53,13 @@ struct Q8Smem {
     float red[2][2][4][kFewRows];  // a side's warps' maxima, or sums, of the rows
     long long scan[16];
   };
-  float mlz[2][3][kFewRows];  // the sides' m, l and the weights' maximum
   int last[2];
   int abort_flag;
   uint32_t tmem_slot;
 };
-static_assert(sizeof(Q8Smem<64>) <= 227 * 1024 && sizeof(Q8Smem<128>) <= 227 * 1024, "shared memory of a CTA");
+// (1 KB of an SM's 228 goes to each CTA beside what it asks for)
+static_assert(kFewCtas * (sizeof(Q8Smem<64>) + 1024) <= 228 * 1024 && kFewCtas * (sizeof(Q8Smem<128>) + 1024) <= 228 * 1024,
+              "shared memory of an SM");
 
 // D(tmem) (+)= A B, e4m3 operands in shared memory, fp32 sums.  From a whole converged warp.
 __device__ __forceinline__ void umma8_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
@@ -111,7 +117,10 @@ __device__ __forceinline__ void parts2(float a, float b, uint32_t (&c)[kQParts])
   }
 }
 
-__device__ __forceinline__ int columns_of(int rows) { return rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
+// Rows in whole groups: 4, 8 or 16.
+__device__ __forceinline__ int rows_held(int rows) { return rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
+// The column of part q of row r.
+__device__ __forceinline__ int column_of(int q, int r) { return r / kRowGroup * kGroupCols + q * kRowGroup + r % kRowGroup; }
 
 // ---- warp 3: the rows of q in parts --------------------------------------------------------
 
@@ -123,7 +132,7 @@ __device__ __forceinline__ void split_queries(const PagedAttnParams& p, Q8Smem<D
   for (uint32_t e = 0;; ++e, ++qn) {
     const Entry en = take(p, sm, e);
     if (uniform(en.n) == 0) return;
-    const int rows = uniform(en.n) * p.G, R = columns_of(rows), buf = qn & 1;
+    const int rows = uniform(en.n) * p.G, R = rows_held(rows);
     uint4 x[2];
     auto fetch = [&](int r) {
       x[0] = x[1] = make_uint4(0, 0, 0, 0);
@@ -135,7 +144,7 @@ __device__ __forceinline__ void split_queries(const PagedAttnParams& p, Q8Smem<D
       }
     };
     fetch(lane / kLanes);
-    if (!attn_wait_warp(sm, &sm.qempty[buf], ((qn >> 1) & 1) ^ 1, p.status)) return;
+    if (!attn_wait_warp(sm, &sm.qempty, (qn & 1) ^ 1, p.status)) return;
     for (int r0 = 0; r0 < R; r0 += 32 / kLanes) {
       const int r = r0 + lane / kLanes;
       const uint32_t u[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
@@ -170,14 +179,14 @@ __device__ __forceinline__ void split_queries(const PagedAttnParams& p, Q8Smem<D
       if (r < R) {
 #pragma unroll
         for (int q = 0; q < kQParts; ++q)
-          *reinterpret_cast<uint4*>(sm.q[buf] + chunk_at<D>(q * R + r, c)) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+          *reinterpret_cast<uint4*>(sm.q + chunk_at<D>(column_of(q, r), c)) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
       }
-      if (c == 0 && r < R) sm.qscale[buf][r] = p.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 - s) << 23);
+      if (c == 0 && r < R) sm.qscale[qn & 1][r] = p.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 - s) << 23);
       fetch(r + 32 / kLanes);
     }
     fence_proxy_async();
     __syncwarp();
-    mbar_arrive_elect(&sm.qfull[buf]);
+    mbar_arrive_elect(&sm.qfull[qn & 1]);
   }
 }
 
@@ -261,10 +270,9 @@ __device__ __forceinline__ void few_mma_warp(const PagedAttnParams& p, Q8Smem<D>
   for (uint32_t e = 0; ok; ++e, ++qn) {
     const Entry en = take(p, sm, e);
     if (uniform(en.n) == 0) break;
-    const int n = uniform(en.t1 - en.t0), N = kQParts * columns_of(uniform(en.n) * p.G);
-    const uint32_t q0 = qn & 1;
-    ok = attn_wait_warp(sm, &sm.qfull[q0], (qn >> 1) & 1, p.status);
-    const uint64_t qdesc = rows_desc<D>(smem_u32(sm.q[q0]));
+    const int n = uniform(en.t1 - en.t0), N = kQParts * rows_held(uniform(en.n) * p.G);
+    ok = attn_wait_warp(sm, &sm.qfull[qn & 1], (qn >> 1) & 1, p.status);
+    const uint64_t qdesc = rows_desc<D>(smem_u32(sm.q));
     const uint32_t idesc_kq = idesc8<false>(128, 0) | static_cast<uint32_t>(N >> 3) << 17;
     const uint32_t idesc_vp = idesc8<true>(128, 0) | static_cast<uint32_t>(N >> 3) << 17;
     auto kq = [&](int x) {
@@ -293,9 +301,12 @@ __device__ __forceinline__ void few_mma_warp(const PagedAttnParams& p, Q8Smem<D>
       umma_commit_elect(&sm.empty[st]);
       if (j + 2 >= n) umma_commit_elect(&sm.ofull[x]);
       advance();
-      if (j + 2 < n) kq(x);
+      if (j + 2 < n) {
+        kq(x);
+        if (j + 3 == n) umma_commit_elect(&sm.qempty);
+      }
     }
-    umma_commit_elect(&sm.qempty[q0]);
+    if (n <= 2) umma_commit_elect(&sm.qempty);
   }
   umma_commit_elect(&sm.done);
   attn_drain(&sm.done, 0);
@@ -321,23 +332,27 @@ __device__ __forceinline__ void few_mend_v(const PagedAttnParams& p, Q8Smem<D>& 
   if (b > 0) zero(b, min(kRows, (b + box - 1) & ~(box - 1)));
 }
 
-// The sum of a row's parts.
-template <int R>
-__device__ __forceinline__ float parts_sum(const uint32_t (&u)[kQParts * R], int r) {
-  const float a = fmaf(__uint_as_float(u[R + r]), 1.f / kRest, __uint_as_float(u[r]));
-  const float b = fmaf(__uint_as_float(u[3 * R + r]), 1.f / kRest, __uint_as_float(u[2 * R + r]));
-  return fmaf(b, 1.f / (kRest * kRest), a);
-}
-template <int R>
-__device__ __forceinline__ void load_parts(uint32_t taddr, uint32_t (&u)[kQParts * R]) {
+// 16 columns of a thread's lane, the parts of a group's rows, as the rows' sums.
+__device__ __forceinline__ void load_rows(uint32_t taddr, float (&v)[kRowGroup]) {
+  uint32_t u[kGroupCols];
+  tmem_ld_cols<kGroupCols>(taddr, u);
 #pragma unroll
-  for (int q = 0; q < kQParts * R; q += 16) {
-    uint32_t v[16];
-    tmem_ld_cols<16>(taddr + q, v);
-#pragma unroll
-    for (int k = 0; k < 16; ++k) u[q + k] = v[k];
+  for (int r = 0; r < kRowGroup; ++r) {
+    const float a = fmaf(__uint_as_float(u[kRowGroup + r]), 1.f / kRest, __uint_as_float(u[r]));
+    const float b = fmaf(__uint_as_float(u[3 * kRowGroup + r]), 1.f / kRest, __uint_as_float(u[2 * kRowGroup + r]));
+    v[r] = fmaf(b, 1.f / (kRest * kRest), a);
   }
 }
+
+// A cut unit's piece, side x: its rows' outputs [row][D], then their (m, l).
+template <int D>
+__device__ __forceinline__ Records<D> few_records(const PagedAttnParams& p, long long cta, bool first, int x) {
+  constexpr size_t kBytes = kFewRows * (D * sizeof(float) + sizeof(float2));
+  static_assert(kFewCtas * kBytes <= kRows * (D * sizeof(float) + sizeof(float2)), "within the workspace");
+  return {p.parts + ((2 * cta + (first ? 1 : 0)) * 2 + x) * kBytes};
+}
+template <int D>
+__device__ __forceinline__ float2* few_ml(const Records<D>& r) { return reinterpret_cast<float2*>(r.at + kFewRows * D * sizeof(float)); }
 
 __device__ __forceinline__ float warp_max(float v) {
   float r;
@@ -345,25 +360,21 @@ __device__ __forceinline__ float warp_max(float v) {
   return r;
 }
 
-template <int D, bool kFp16, int R>
+// kGroups groups of rows.
+template <int D, bool kFp16, int kGroups>
 __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>& sm, uint32_t tmem, int x, const Entry& en,
                                             SideState& st) {
+  constexpr int R = kGroups * kRowGroup;
   const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, key = warp * 32 + lane;
   const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
   const uint32_t ts = tmem + lanes + few_s_col(x), to = tmem + lanes + few_o_col(x);
   const int rows = en.n * p.G;
   const int f1 = rows < R ? 0 : (en.pos0 + 1) >> 7;  // [f0, f1): every row sees every key
   const int f0 = p.window > 0 ? (max(0, en.pos0 + en.n - p.window) + 127) >> 7 : 0;
-  const int first = en.t0 + x;
-  // (a side without a tile waits for none: nothing would keep the next rows but one from taking this buffer meanwhile)
-  if (first < en.t1) st.ok = st.ok && attn_wait_warp(sm, &sm.qfull[st.qn & 1], (st.qn >> 1) & 1, p.status);
-  float cq[R], m[R], l[R], mz[R];
+  float l[R];
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    cq[r] = first < en.t1 ? sm.qscale[st.qn & 1][r] : 0.f;
-    m[r] = mz[r] = -INFINITY;
-    l[r] = 0.f;
-  }
+  for (int r = 0; r < R; ++r) l[r] = 0.f;
+  if (key < R) sm.m[x][key] = sm.mz[x][key] = -INFINITY;
   // the key's exponents, one tile of the side ahead, and its page, two
   const int* row = p.table + static_cast<long long>(en.s) * p.max_pages;
   auto page_at = [&](int j) {
@@ -371,12 +382,18 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>&
     return j < en.t1 && k >= en.klo && k < en.khi ? row[k >> p.page_shift] : -1;
   };
   auto exponents_at = [&](int j, int page) {  // (K's, V's; of a zero row where there is none)
-    if (static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages)) return make_uint2(127u, 127u);
+    const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.num_pages);
     const long long at = page * p.scale_page + (en.h << p.page_shift) + ((j * kRows + key) & ((1 << p.page_shift) - 1));
-    return make_uint2(p.K_scale[at], p.V_scale[at]);
+    return make_uint2(load_byte_if(p.K_scale + at, there, 127u), load_byte_if(p.V_scale + at, there, 127u));
   };
+  const int first = en.t0 + x;
   uint2 ex = exponents_at(first, page_at(first));
   int page = page_at(first + 2);
+  // (The rows of the next entry but one come after this side has left this one: its phase cannot be missed.  A side without a
+  // tile needs none.)
+  if (first < en.t1) st.ok = st.ok && attn_wait_warp(sm, &sm.qfull[st.qn & 1], (st.qn >> 1) & 1, p.status);
+  const float* const qscale = sm.qscale[st.qn & 1];
+  group_sync(x);  // (the maxima are set)
   for (int j = first; j < en.t1; j += 2) {
     const uint2 next = exponents_at(j + 2, page);
     page = page_at(j + 4);
@@ -384,75 +401,101 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>&
     st.sph ^= 1;
     tc_fence_after();
     const float k2 = __uint_as_float(ex.x << 23), b = static_cast<float>(static_cast<int>(ex.y) - 127);
-    float y[R];
-    {
-      uint32_t u[kQParts * R];
-      load_parts<R>(ts, u);
+    const bool edge = j < f0 || j >= f1;
+    // the logits of group g
+    auto logits = [&](int g, float (&y)[kRowGroup]) {
+      load_rows(ts + g * kGroupCols, y);
 #pragma unroll
-      for (int r = 0; r < R; ++r) y[r] = parts_sum<R>(u, r) * cq[r] * k2;
-    }
-    if (j < f0 || j >= f1) {
-      const int k = j * kRows + key;
-      int t = en.pos0, g = 0;
+      for (int r = 0; r < kRowGroup; ++r) y[r] *= qscale[g * kRowGroup + r] * k2;
+      if (edge) {
+        const int k = j * kRows + key;
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        if (r >= rows || k > t || (p.window > 0 && k <= t - p.window)) y[r] = -INFINITY;
-        if (++g == p.G) { g = 0; ++t; }
+        for (int r = 0; r < kRowGroup; ++r) {
+          const int t = en.pos0 + (g * kRowGroup + r) / p.G;
+          if (g * kRowGroup + r >= rows || k > t || (p.window > 0 && k <= t - p.window)) y[r] = -INFINITY;
+        }
       }
-    }
+    };
+    float y[kRowGroup];  // (of more groups: formed again where they are used)
     bool up = false;
 #pragma unroll
-    for (int r = 0; r < R; ++r) up |= y[r] > m[r] + kFewRaise || y[r] + b > mz[r] + kFewRaise;
+    for (int g = 0; g < kGroups; ++g) {
+      logits(g, y);
+#pragma unroll
+      for (int r = 0; r < kRowGroup; ++r)
+        up |= y[r] > sm.m[x][g * kRowGroup + r] + kFewRaise || y[r] + b > sm.mz[x][g * kRowGroup + r] + kFewRaise;
+    }
     if (group_any(x, up)) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const float a = warp_max(y[r]), z = warp_max(y[r] + b);
-        if (lane == 0) { sm.red[x][0][warp][r] = a; sm.red[x][1][warp][r] = z; }
+      for (int g = 0; g < kGroups; ++g) {
+        if (kGroups > 1) logits(g, y);
+#pragma unroll
+        for (int r = 0; r < kRowGroup; ++r) {
+          const float a = warp_max(y[r]), z = warp_max(y[r] + b);
+          if (lane == 0) {
+            sm.red[x][0][warp][g * kRowGroup + r] = a;
+            sm.red[x][1][warp][g * kRowGroup + r] = z;
+          }
+        }
       }
       group_sync(x);
-      float f[R];
+      auto raised = [&](int i, int r) {
+        const float* top = &sm.red[x][i][0][r];
+        return fmaxf(fmaxf(fmaxf(top[0], top[kFewRows]), fmaxf(top[2 * kFewRows], top[3 * kFewRows])), i ? sm.mz[x][r] : sm.m[x][r]);
+      };
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        float top[2];
+      for (int g = 0; g < kGroups; ++g) {
+        float f[kRowGroup];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          top[i] = fmaxf(fmaxf(sm.red[x][i][0][r], sm.red[x][i][1][r]), fmaxf(sm.red[x][i][2][r], sm.red[x][i][3][r]));
-        const float mn = fmaxf(m[r], top[0]), zn = fmaxf(mz[r], top[1]);
-        l[r] *= ex2_approx(m[r] - finite_or_0(mn));
-        f[r] = ex2_approx(mz[r] - finite_or_0(zn));
-        m[r] = mn;
-        mz[r] = zn;
-      }
-      if (j != first) {
-        // S of this tile is complete, so is O of the side's tile before it, and the next waits for us
-#pragma unroll
-        for (int q = 0; q < kQParts; ++q) {
-          uint32_t o[R];
-          tmem_ld_cols<R>(to + q * R, o);
-#pragma unroll
-          for (int r = 0; r < R; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * f[r]);
-          tmem_st_cols<R>(to + q * R, o);
+        for (int r = 0; r < kRowGroup; ++r) {
+          const int q = g * kRowGroup + r;
+          l[q] *= ex2_approx(sm.m[x][q] - finite_or_0(raised(0, q)));
+          f[r] = ex2_approx(sm.mz[x][q] - finite_or_0(raised(1, q)));
         }
-        tmem_wait_st();
+        if (j != first) {
+          // S of this tile is complete, so is O of the side's tile before it, and the next waits for us
+          uint32_t o[kGroupCols];
+          tmem_ld_cols<kGroupCols>(to + g * kGroupCols, o);
+#pragma unroll
+          for (int c = 0; c < kGroupCols; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f[c % kRowGroup]);
+          tmem_st_cols<kGroupCols>(to + g * kGroupCols, o);
+        }
       }
+      if (j != first) tmem_wait_st();
+      float mn = 0.f, zn = 0.f;
+      if (key < R) {
+        mn = raised(0, key);
+        zn = raised(1, key);
+      }
+      group_sync(x);  // (everyone has read the old ones)
+      if (key < R) {
+        sm.m[x][key] = mn;
+        sm.mz[x][key] = zn;
+      }
+      group_sync(x);
     }
-    // this key's byte of part q of row r is at row n = q R + r
+    // this key's byte of a column is in the column's 128
     uint8_t* const pw = sm.p[x] + (key & 15);
     const int chunk = key >> 4;
 #pragma unroll
-    for (int r = 0; r < R; r += 2) {
-      float w[2];
+    for (int g = 0; g < kGroups; ++g) {
+      if (kGroups > 1) logits(g, y);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        l[r + i] += ex2_approx(y[r + i] - finite_or_0(m[r + i]));
-        w[i] = ex2_approx(y[r + i] + b - (finite_or_0(mz[r + i]) - kFewUp));
-      }
-      uint32_t c[kQParts];
-      parts2(w[0], w[1], c);
+      for (int r = 0; r < kRowGroup; r += 2) {
+        float w[2];
 #pragma unroll
-      for (int q = 0; q < kQParts; ++q) {
-        pw[chunk_at<128>(q * R + r, chunk)] = static_cast<uint8_t>(c[q]);
-        pw[chunk_at<128>(q * R + r + 1, chunk)] = static_cast<uint8_t>(c[q] >> 8);
+        for (int i = 0; i < 2; ++i) {
+          const int q = g * kRowGroup + r + i;
+          l[q] += ex2_approx(y[r + i] - finite_or_0(sm.m[x][q]));
+          w[i] = ex2_approx(y[r + i] + b - (finite_or_0(sm.mz[x][q]) - kFewUp));
+        }
+        uint32_t c[kQParts];
+        parts2(w[0], w[1], c);
+#pragma unroll
+        for (int q = 0; q < kQParts; ++q) {
+          pw[chunk_at<128>(column_of(q, g * kRowGroup + r), chunk)] = static_cast<uint8_t>(c[q]);
+          pw[chunk_at<128>(column_of(q, g * kRowGroup + r + 1), chunk)] = static_cast<uint8_t>(c[q] >> 8);
+        }
       }
     }
     few_mend_v<D>(p, sm, en, j, st);
@@ -463,32 +506,16 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>&
     ex = next;
   }
   // ---- the rows' output: sums over the keys, then both sides' accumulators ----
+  group_sync(x);  // (the maxima's readers are done)
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     float v = l[r];
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    l[r] = v;
-  }
-  group_sync(x);  // (the maxima's readers are done)
-  if (lane < R) {
-    float v = 0.f;
-#pragma unroll
-    for (int r = 0; r < R; ++r) v = r == lane ? l[r] : v;
-    sm.red[x][0][warp][lane] = v;
+    if (lane == 0) sm.red[x][0][warp][r] = v;
   }
   group_sync(x);
-  if (warp == 0 && lane < R) {
-    float a = 0.f, z = 0.f;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      a = r == lane ? m[r] : a;
-      z = r == lane ? mz[r] : z;
-    }
-    sm.mlz[x][0][lane] = a;
-    sm.mlz[x][1][lane] = (sm.red[x][0][0][lane] + sm.red[x][0][1][lane]) + (sm.red[x][0][2][lane] + sm.red[x][0][3][lane]);
-    sm.mlz[x][2][lane] = z;
-  }
+  if (key < R) sm.l[x][key] = (sm.red[x][0][0][key] + sm.red[x][0][1][key]) + (sm.red[x][0][2][key] + sm.red[x][0][3][key]);
   if (first < en.t1) {  // (side 1 of a single tile has no accumulator)
     st.ok = st.ok && attn_wait_warp(sm, &sm.ofull[x], st.oph, p.status);
     st.oph ^= 1;
@@ -499,29 +526,6 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>&
   st.ok = st.ok && attn_wait_warp(sm, &sm.xfull, st.xph, p.status);
   tc_fence_after();
   const bool both = en.t0 + 1 < en.t1, whole = en.pieces == 1;
-  float v[R];
-  {
-    uint32_t u[kQParts * R];
-    load_parts<R>(tmem + lanes + few_o_col(0), u);
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const float ma = sm.mlz[0][0][r], mb = both ? sm.mlz[1][0][r] : -INFINITY;
-      m[r] = fmaxf(ma, mb);
-      const float base = finite_or_0(m[r]);
-      l[r] = fmaf(sm.mlz[0][1][r], ex2_approx(ma - base), both ? sm.mlz[1][1][r] * ex2_approx(mb - base) : 0.f);
-      // the accumulators are 2^kFewUp sum 2^(y + b - mz) B
-      v[r] = l[r] == 0.f ? 0.f : parts_sum<R>(u, r) * ex2_approx(sm.mlz[0][2][r] - kFewUp - base);
-    }
-    if (both) {
-      load_parts<R>(tmem + lanes + few_o_col(1), u);
-#pragma unroll
-      for (int r = 0; r < R; ++r)
-        if (l[r] != 0.f) v[r] = fmaf(parts_sum<R>(u, r), ex2_approx(sm.mlz[1][2][r] - kFewUp - finite_or_0(m[r])), v[r]);
-    }
-  }
-  tc_fence_before();
-  __syncwarp();
-  mbar_arrive_elect(&sm.xfree);
   // side x writes the rows r with r mod 2 = x; the thread's element is d = key
   auto emit = [&](int r, float o, float mm, float ll) {
     const int i = r / p.G, head = en.h * p.G + r - i * p.G;
@@ -530,60 +534,70 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>&
                                    static_cast<long long>(head) * p.out_head + key * 2) = static_cast<uint16_t>(pack2<kFp16>(o, 0.f));
     if (p.lse && key == r) p.lse[static_cast<long long>(en.tok0 + i) * p.H_q + head] = lse_of(mm, ll);
   };
-  if (whole) {
+  const Records<D> mine = few_records<D>(p, blockIdx.x, en.first == static_cast<int>(blockIdx.x), x);
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-      if ((r & 1) == x && r < rows) emit(r, v[r] * (l[r] == 0.f ? 0.f : 1.f / l[r]), m[r], l[r]);
-  } else {
-    const Records<D> mine = records<D>(p, blockIdx.x, en.first == static_cast<int>(blockIdx.x), x);
+  for (int g = 0; g < kGroups; ++g) {
+    float a[kRowGroup], c[kRowGroup];
+    load_rows(tmem + lanes + few_o_col(0) + g * kGroupCols, a);
+    if (both) load_rows(tmem + lanes + few_o_col(1) + g * kGroupCols, c);
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-      if ((r & 1) == x && r < rows) {
-        if (key < D) __stcg(reinterpret_cast<float*>(mine.at) + r * D + key, v[r]);
-        if (key == r) __stcg(mine.ml() + r, make_float2(m[r], l[r]));
+    for (int r = 0; r < kRowGroup; ++r) {
+      const int q = g * kRowGroup + r;
+      if ((q & 1) != x || q >= rows) continue;
+      const float ma = sm.m[0][q], mb = both ? sm.m[1][q] : -INFINITY, mm = fmaxf(ma, mb), base = finite_or_0(mm);
+      const float ll = fmaf(sm.l[0][q], ex2_approx(ma - base), both ? sm.l[1][q] * ex2_approx(mb - base) : 0.f);
+      // the accumulators are 2^kFewUp sum 2^(y + b - mz) B
+      float v = 0.f;
+      if (ll != 0.f) {
+        v = a[r] * ex2_approx(sm.mz[0][q] - kFewUp - base);
+        if (both) v = fmaf(c[r], ex2_approx(sm.mz[1][q] - kFewUp - base), v);
       }
-    if (arrived_last(p, sm, en, x, st.ok)) {
-      // the side's rows together, 32 records in flight
-      constexpr int kR = R / 2, kU = 32 / kR;
-      float mm[kR], ll[kR], oo[kR];
-#pragma unroll
-      for (int r = 0; r < kR; ++r) { mm[r] = -INFINITY; ll[r] = oo[r] = 0.f; }
+      if (whole) {
+        emit(q, v * (ll == 0.f ? 0.f : 1.f / ll), mm, ll);
+      } else {
+        if (key < D) __stcg(reinterpret_cast<float*>(mine.at) + q * D + key, v);
+        if (key == q) __stcg(few_ml(mine) + q, make_float2(mm, ll));
+      }
+    }
+  }
+  tc_fence_before();
+  __syncwarp();
+  mbar_arrive_elect(&sm.xfree);
+  if (!whole && arrived_last(p, sm, en, x, st.ok)) {
+    // row by row, kU records in flight
+    constexpr int kU = 16;
+#pragma unroll 1
+    for (int q = x; q < rows; q += 2) {
+      float mm = -INFINITY, ll = 0.f, oo = 0.f;
+#pragma unroll 1
       for (int q0 = 0; q0 < en.pieces; q0 += kU) {
-        float2 z[kR][kU];
-        float o[kR][kU];
+        float2 z[kU];
+        float o[kU];
 #pragma unroll
-        for (int q = 0; q < kU; ++q) {
-          const Records<D> rec = records<D>(p, en.first + q0 + q, q0 + q == 0, x);
-#pragma unroll
-          for (int r = 0; r < kR; ++r) {
-            z[r][q] = make_float2(-INFINITY, 0.f);
-            o[r][q] = 0.f;
-            if (q0 + q < en.pieces && 2 * r + x < rows) {
-              z[r][q] = __ldcg(rec.ml() + 2 * r + x);
-              if (key < D) o[r][q] = __ldcg(reinterpret_cast<const float*>(rec.at) + (2 * r + x) * D + key);
-            }
+        for (int i = 0; i < kU; ++i) {
+          z[i] = make_float2(-INFINITY, 0.f);
+          o[i] = 0.f;
+          if (q0 + i < en.pieces) {
+            const Records<D> rec = few_records<D>(p, en.first + q0 + i, q0 + i == 0, x);
+            z[i] = __ldcg(few_ml(rec) + q);
+            if (key < D) o[i] = __ldcg(reinterpret_cast<const float*>(rec.at) + q * D + key);
           }
         }
+        float mn = mm;
 #pragma unroll
-        for (int r = 0; r < kR; ++r) {
-          float mn = mm[r];
+        for (int i = 0; i < kU; ++i) mn = fmaxf(mn, z[i].x);
+        const float bs = finite_or_0(mn), f0 = ex2_approx(mm - bs);
+        ll *= f0;
+        oo *= f0;
 #pragma unroll
-          for (int q = 0; q < kU; ++q) mn = fmaxf(mn, z[r][q].x);
-          const float bs = finite_or_0(mn), f0 = ex2_approx(mm[r] - bs);
-          ll[r] *= f0;
-          oo[r] *= f0;
-#pragma unroll
-          for (int q = 0; q < kU; ++q) {
-            const float f = ex2_approx(z[r][q].x - bs);
-            ll[r] = fmaf(z[r][q].y, f, ll[r]);
-            oo[r] = fmaf(o[r][q], f, oo[r]);
-          }
-          mm[r] = mn;
+        for (int i = 0; i < kU; ++i) {
+          const float f = ex2_approx(z[i].x - bs);
+          ll = fmaf(z[i].y, f, ll);
+          oo = fmaf(o[i], f, oo);
         }
+        mm = mn;
       }
-#pragma unroll
-      for (int r = 0; r < kR; ++r)
-        if (2 * r + x < rows) emit(2 * r + x, ll[r] == 0.f ? 0.f : oo[r] * (1.f / ll[r]), mm[r], ll[r]);
+      emit(q, ll == 0.f ? 0.f : oo * (1.f / ll), mm, ll);
     }
   }
   // both sides have read both accumulators and their maxima and sums before either goes on
@@ -594,7 +608,7 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>&
 }
 
 template <int D, bool kFp16>
-__global__ void __launch_bounds__(kFewThreads, 1) q8_few_kernel(const __grid_constant__ PagedAttnParams p) {
+__global__ void __launch_bounds__(kFewThreads, kFewCtas) q8_few_kernel(const __grid_constant__ PagedAttnParams p) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   using S = Q8Smem<D>;
   if (smem_u32(smem_raw) & 1023u) {  // the swizzles need 1024-byte aligned buffers
@@ -605,8 +619,6 @@ __global__ void __launch_bounds__(kFewThreads, 1) q8_few_kernel(const __grid_con
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sm.qfull[i], 1);
-      mbar_init(&sm.qempty[i], 1);
       mbar_init(&sm.sfull[i], 1);
       mbar_init(&sm.pfull[i], 4);
       mbar_init(&sm.ofull[i], 1);
@@ -619,6 +631,8 @@ __global__ void __launch_bounds__(kFewThreads, 1) q8_few_kernel(const __grid_con
       mbar_init(&sm.efull[i], 1);
       mbar_init(&sm.eempty[i], 11);  // the load, MMA and query warps and eight softmax warps
     }
+    for (int i = 0; i < 2; ++i) mbar_init(&sm.qfull[i], 1);
+    mbar_init(&sm.qempty, 1);
     mbar_init(&sm.xfull, 8);
     mbar_init(&sm.xfree, 8);
     mbar_init(&sm.done, 1);
@@ -653,9 +667,9 @@ __global__ void __launch_bounds__(kFewThreads, 1) q8_few_kernel(const __grid_con
       const Entry en = take(p, sm, e);
       if (group_any(x, en.n == 0)) break;  // no more, or a warp's wait for the entry ran out
       const int rows = en.n * p.G;
-      if (rows <= 4) q8_few_rows<D, kFp16, 4>(p, sm, tmem, x, en, st);
-      else if (rows <= 8) q8_few_rows<D, kFp16, 8>(p, sm, tmem, x, en, st);
-      else q8_few_rows<D, kFp16, 16>(p, sm, tmem, x, en, st);
+      if (rows <= 4) q8_few_rows<D, kFp16, 1>(p, sm, tmem, x, en, st);
+      else if (rows <= 8) q8_few_rows<D, kFp16, 2>(p, sm, tmem, x, en, st);
+      else q8_few_rows<D, kFp16, 4>(p, sm, tmem, x, en, st);
       st.tiles += 2 * (en.t1 - en.t0);
     }
   }
@@ -696,7 +710,8 @@ int few_launch(PagedAttnParams p, const kvev_paged_q8_cache* cache, cudaStream_t
                CU_TENSOR_MAP_INTERLEAVE_NONE, d == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       return KVEV_ECUDA;
-  return launch_overlapped(fn, p, grid, kFewThreads, smem, stream) == cudaSuccess ? KVEV_OK : KVEV_ECUDA;
+  static_assert(2 * kFewCtas * kMaxCtas * sizeof(int) <= KVEV_PAGED_SYNC_BYTES, "arrival counts");
+  return launch_overlapped(fn, p, kFewCtas * grid, kFewThreads, smem, stream) == cudaSuccess ? KVEV_OK : KVEV_ECUDA;
 }
 
 }  // namespace
