@@ -129,8 +129,19 @@ struct Entry {
   int part;                        // kShared: 0, 1: the rows' part of that number; -1: all of their keys
 };
 
+// kQ8: codes as they are loaded.
+template <int D, bool kHas>
+struct RawTiles {};
 template <int D>
-struct AttnSmem {
+struct RawTiles<D, true> {
+  static constexpr int kRaw = D == 128 ? 3 : 6, kRawBytes = kRows * D;
+  alignas(128) uint8_t raw[kRaw][kRawBytes];
+  uint64_t rawfull[kRaw], rawempty[kRaw];
+  uint32_t power[2][kRows];  // of a tile's rows: 2^e twice in 16 bits
+};
+
+template <int D, int kMode>
+struct AttnSmemBase {
   static constexpr int kTileBytes = kRows * D * 2;
   // Units lie request by request, head by head; with 64-element heads head by head, request by request: the
   // heads of the same tokens, 128 bytes each next to one another in tokens-first pages, of which L2 fetches
@@ -145,7 +156,7 @@ struct AttnSmem {
   // 128-element heads stay in the first: generations the same within 1 %, four chunks of 1,200 over 9,000
   // 409 us, 421 in the other.
   static constexpr bool kHeadsOuter = D == 64;
-  static constexpr int kStages = D == 128 ? 5 : 10;
+  static constexpr int kStages = (kMode & kQ8 ? 3 : 5) * (D == 128 ? 1 : 2);
   // (with 64-element rows the transposed products also read the tile's size of
   // bytes after a V tile, for lanes that nothing reads: the Q tiles, after the last)
   uint8_t kv[kStages][kTileBytes];
@@ -166,7 +177,11 @@ struct AttnSmem {
   int abort_flag;
   uint32_t tmem_slot;
 };
-static_assert(sizeof(AttnSmem<64>) <= 227 * 1024 && sizeof(AttnSmem<128>) <= 227 * 1024, "shared memory of a CTA");
+template <int D, int kMode>
+struct AttnSmem : AttnSmemBase<D, kMode>, RawTiles<D, (kMode & kQ8) != 0> {};
+static_assert(sizeof(AttnSmem<64, kPlain>) <= 227 * 1024 && sizeof(AttnSmem<128, kPlain>) <= 227 * 1024 &&
+                  sizeof(AttnSmem<64, kQ8>) <= 227 * 1024 && sizeof(AttnSmem<128, kQ8>) <= 227 * 1024,
+              "shared memory of a CTA");
 
 // ---- waits, bounded -------------------------------------------------------------
 
@@ -663,8 +678,8 @@ __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, 
 // Order of an entry's tiles in the ring: A K tiles ahead of V (A = 1 for a full unit;
 // 2 for the others, whose sides work on two tiles at once).
 template <int D, int kMode>
-__device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>& sm) {
-  using S = AttnSmem<D>;
+__device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D, kMode>& sm) {
+  using S = AttnSmem<D, kMode>;
   const int lane = threadIdx.x & 31;
   const int box_shift = min(p.page_shift, 7);  // rows of a page box
   const int boxes = kRows >> box_shift;        // page boxes of a tile
@@ -683,8 +698,7 @@ __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>&
       const int k = t * kRows + (lane << box_shift);
       return t < t1 && lane < boxes && k < khi && k + (1 << box_shift) > klo ? row[k >> p.page_shift] : INT_MAX;
     };
-    int r0 = INT_MAX, r1 = INT_MAX, r2 = INT_MAX;
-    if (!(kMode & kQ8)) { r0 = page_of(t0); r1 = page_of(t0 + 1); r2 = page_of(t0 + 2); }
+    int r0 = page_of(t0), r1 = page_of(t0 + 1), r2 = page_of(t0 + 2);
     // ---- Q tiles ----
     const int sides = kind == kFull ? 2 : 1;
     for (int x = 0; ok && x < sides; ++x) {
@@ -698,35 +712,54 @@ __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>&
                           smem_u32(&sm.qfull[qs]));
       ++qn;
     }
-    if (kMode & kQ8) continue;  // (the pages are the converting warps')
     auto checked = [&](int id) {  // num_pages (loads zeros) for no page or one outside the pool
       if (static_cast<unsigned>(id) < static_cast<unsigned>(p.num_pages)) return id;
       if (id != INT_MAX) atomicOr(p.status, kStatusDevice);
       return p.num_pages;
     };
     auto load = [&](const CUtensorMap* map, int t, int page) {
-      ok = ok && attn_wait_warp(sm, &sm.empty[st], ph ^ 1, p.status);
-      if (!ok) return;
-      const uint32_t dst = smem_u32(sm.kv[st]), bar = smem_u32(&sm.full[st]);
-      mbar_expect_elect(&sm.full[st], S::kTileBytes);
-      const int y = (t * kRows) & ((1 << p.page_shift) - 1);  // a page is whole boxes, or a box whole pages
-      if (boxes == 1) {
-#pragma unroll
-        for (int c = 0; c < D / 64; ++c)
-          tma_load_4d_elect(dst + c * (kRows * 128), map, c * 64, y, h, uniform(page), bar);
-      } else {
-        for (int i = 0; i < boxes; i += 2) {  // an even number of them
-          const int pa = __shfl_sync(0xffffffffu, page, i), pb = __shfl_sync(0xffffffffu, page, i + 1);
-#pragma unroll
-          for (int c = 0; c < D / 64; ++c) {
-            const uint32_t at = dst + c * (kRows * 128) + (i << (box_shift + 7));
-            tma_load_4d_elect(at, map, c * 64, y, h, pa, bar);
-            tma_load_4d_elect(at + (1 << (box_shift + 7)), map, c * 64, y, h, pb, bar);
+      if constexpr ((kMode & kQ8) != 0) {  // codes, [128 keys][D]
+        ok = ok && attn_wait_warp(sm, &sm.rawempty[st], ph ^ 1, p.status);
+        if (!ok) return;
+        const uint32_t dst = smem_u32(sm.raw[st]), bar = smem_u32(&sm.rawfull[st]);
+        mbar_expect_elect(&sm.rawfull[st], S::kRawBytes);
+        const int y = (t * kRows) & ((1 << p.page_shift) - 1);
+        if (boxes == 1) {
+          tma_load_4d_elect(dst, map, 0, y, h, uniform(page), bar);
+        } else {
+          for (int i = 0; i < boxes; i += 2) {
+            const int pa = __shfl_sync(0xffffffffu, page, i), pb = __shfl_sync(0xffffffffu, page, i + 1);
+            tma_load_4d_elect(dst + (i << box_shift) * D, map, 0, y, h, pa, bar);
+            tma_load_4d_elect(dst + ((i + 1) << box_shift) * D, map, 0, y, h, pb, bar);
           }
         }
+        ++issued;
+        if (++st == S::kRaw) { st = 0; ph ^= 1; }
+        return;
+      } else {
+        ok = ok && attn_wait_warp(sm, &sm.empty[st], ph ^ 1, p.status);
+        if (!ok) return;
+        const uint32_t dst = smem_u32(sm.kv[st]), bar = smem_u32(&sm.full[st]);
+        mbar_expect_elect(&sm.full[st], S::kTileBytes);
+        const int y = (t * kRows) & ((1 << p.page_shift) - 1);  // a page is whole boxes, or a box whole pages
+        if (boxes == 1) {
+#pragma unroll
+          for (int c = 0; c < D / 64; ++c)
+            tma_load_4d_elect(dst + c * (kRows * 128), map, c * 64, y, h, uniform(page), bar);
+        } else {
+          for (int i = 0; i < boxes; i += 2) {  // an even number of them
+            const int pa = __shfl_sync(0xffffffffu, page, i), pb = __shfl_sync(0xffffffffu, page, i + 1);
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) {
+              const uint32_t at = dst + c * (kRows * 128) + (i << (box_shift + 7));
+              tma_load_4d_elect(at, map, c * 64, y, h, pa, bar);
+              tma_load_4d_elect(at + (1 << (box_shift + 7)), map, c * 64, y, h, pb, bar);
+            }
+          }
+        }
+        ++issued;
+        if (++st == S::kStages) { st = 0; ph ^= 1; }
       }
-      ++issued;
-      if (++st == S::kStages) { st = 0; ph ^= 1; }
     };
     const int A = kind == kFull ? 1 : 2;
     int p0 = checked(r0), p1 = checked(r1);  // pages of tiles t, t + 1
@@ -744,18 +777,41 @@ __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D>&
   // After an abort, wait (bounded) for the copies still landing before the CTA retires.
   if (!ok || ld_volatile(&sm.abort_flag)) {
     for (uint32_t b = 0; b < 2 && b < qn; ++b) attn_drain(&sm.qfull[(qn - 1 - b) & 1], ((qn - 1 - b) >> 1) & 1);
-    for (uint32_t b = 0; b < S::kStages && b < issued; ++b) {
-      const uint32_t n = issued - 1 - b;
-      attn_drain(&sm.full[n % S::kStages], (n / S::kStages) & 1);
+    if constexpr ((kMode & kQ8) != 0) {
+      for (uint32_t b = 0; b < S::kRaw && b < issued; ++b) {
+        const uint32_t n = issued - 1 - b;
+        attn_drain(&sm.rawfull[n % S::kRaw], (n / S::kRaw) & 1);
+      }
+    } else {
+      for (uint32_t b = 0; b < S::kStages && b < issued; ++b) {
+        const uint32_t n = issued - 1 - b;
+        attn_drain(&sm.full[n % S::kStages], (n / S::kStages) & 1);
+      }
     }
   }
 }
 
+// Barriers of four warps: the sides' softmax groups 0 and 1, and with kQ8 the converting warps 2.
+__device__ __forceinline__ void group_sync(int x) { named_bar_sync(1 + x, 128); }
+__device__ __forceinline__ bool group_any(int x, bool v) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred a, b;\n\t"
+      "setp.ne.u32 a, %1, 0;\n\t"
+      "barrier.cta.red.or.pred b, %2, 128, a;\n\t"
+      "selp.u32 %0, 1, 0, b;\n\t}"
+      : "=r"(r)
+      : "r"(static_cast<uint32_t>(v)), "r"(1 + x)
+      : "memory");
+  return r != 0;
+}
+
 // ---- kQ8: warps 12-15, pages of 8-bit codes to 16-bit tiles ---------------------------------
-// The tiles that warp 0 loads by TMA from 16-bit pages are made here, in the same order and places of the ring: a
-// thread has the codes of its 8 (4) vectors of the next tile in flight while it turns this tile's into 16-bit values,
-// which they and their row's power of two have exactly, so that nothing after this differs from 16-bit pages.
-// Rows without a key of the unit, and those of pages outside the pool, become zeros.
+// Warp 0 loads codes; the tiles that it would have loaded from 16-bit pages are made of them here, in the same order
+// and places of the ring.  The values are 16-bit ones exactly, so that nothing after this differs.  A thread has the
+// power of two of one row of the next tile in flight, and turns 16 codes at a time, of 8 (4) rows.  Rows without a key of
+// the unit become zeros, whatever the pool holds there.
+// Measured, the last 4K of a 32K prompt: %%D
 
 // Loads ahead of their use, under a condition, said in PTX: from a plain load with a constant in its place the compiler
 // makes one whose first use, a shift or a product, follows it at once and waits for it (an 8-bit tile's exponents, 4 chunks
@@ -767,15 +823,6 @@ __device__ __forceinline__ uint32_t load_byte_if(const uint8_t* at, bool there, 
       "setp.ne.b32 p, %2, 0;\n\t"
       "@p ld.global.u8 %0, [%1];\n\t}"
       : "+r"(v) : "l"(at), "r"(static_cast<uint32_t>(there)));
-  return v;
-}
-__device__ __forceinline__ uint4 load16_if(const uint8_t* at, bool there) {
-  uint4 v = make_uint4(0, 0, 0, 0);
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %5, 0;\n\t"
-      "@p ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
-      : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w) : "l"(at), "r"(static_cast<uint32_t>(there)));
   return v;
 }
 
@@ -805,18 +852,23 @@ __device__ __forceinline__ uint32_t power2(uint32_t b) {
   return kFp16 ? pack2<true>(__uint_as_float(b << 23), __uint_as_float(b << 23)) : b * 0x00800080u;
 }
 
-template <int D, bool kFp16>
-__device__ __forceinline__ void convert_group(const PagedAttnParams& p, AttnSmem<D>& sm) {
-  using S = AttnSmem<D>;
+template <int D, bool kFp16, int kMode>
+__device__ __forceinline__ void convert_group(const PagedAttnParams& p, AttnSmem<D, kMode>& sm) {
+  using S = AttnSmem<D, kMode>;
   constexpr int kLanes = D / 16;                  // threads of a row
   constexpr int kStep = 128 / kLanes, kV = kRows / kStep;  // rows of the group at a time, vectors of a thread
-  const int tid = threadIdx.x & 127, lane = threadIdx.x & 31;
-  const int r0 = tid / kLanes, c = tid % kLanes;
-  uint32_t st = 0, ph = 0;
+  const int tid = threadIdx.x & 127;
+  // Threads of the second 64-element block take the neighbouring row's chunks, whose place differs in one bit: the
+  // stores of a row's threads go to different banks.
+  const int c = tid % kLanes, block = c >> 2, r0 = (tid / kLanes) ^ block;
+  // 16 values: the 16-byte chunks 2 (c mod 4) and the next of the block (a step of rows leaves r mod 8 as it is)
+  const int to = block * (kRows * 128) + r0 * 128, j0 = (((c & 3) * 2) ^ (r0 & 7)) << 4, j1 = (((c & 3) * 2 + 1) ^ (r0 & 7)) << 4;
+  uint32_t st = 0, ph = 0, rs = 0, rph = 0, buf = 0;
   bool ok = true;
-  for (uint32_t e = 0; ok; ++e) {
+  for (uint32_t e = 0;; ++e) {
     const Entry en = take(p, sm, e);
-    if (uniform(en.n) == 0) break;
+    // (the warps agree, and after a wait that ran out they run on, so that each reaches the same barriers)
+    if (group_any(2, en.n == 0)) break;
     const int h = uniform(en.h), t0 = uniform(en.t0), n = uniform(en.t1) - t0, klo = uniform(en.klo), khi = uniform(en.khi);
     const int* row = p.table + static_cast<long long>(uniform(en.s)) * p.max_pages;
     const int A = min(uniform(en.kind) == kFull ? 1 : 2, n);
@@ -826,57 +878,49 @@ __device__ __forceinline__ void convert_group(const PagedAttnParams& p, AttnSmem
       *v = k >= 0 && ((k & 1) == 0 || k >= 2 * (n - A));
       return t0 + (k < 0 ? i : k >= 2 * (n - A) ? k - (n - A) : *v ? k >> 1 : A + (k >> 1));
     };
-    // lane b holds the page of the tile's 8 rows b
-    auto pages_of = [&](int t) {
-      const int k = t * kRows + lane * 8;
-      return lane < kRows / 8 && k < khi && k + 8 > klo ? row[k >> p.page_shift] : INT_MAX;
+    // of row `tid` of the i-th tile: its page, and its exponent's byte
+    auto page_at = [&](int i) {
+      bool v;
+      const int k = tile_of(i, &v) * kRows + tid;
+      return i < 2 * n && k >= klo && k < khi ? row[k >> p.page_shift] : -1;
     };
-    uint4 x[kV];
-    uint32_t b[kV];
-    bool v;
-    int t = tile_of(0, &v), ids = pages_of(t);
-    auto fetch = [&](int q, int t, bool v, int ids) {  // vector q of tile t
-      const int r = r0 + q * kStep, k = t * kRows + r;
-      const int page = __shfl_sync(0xffffffffu, ids, r >> 3);
-      const int in = k & ((1 << p.page_shift) - 1);
-      const bool key = k >= klo && k < khi, there = key && static_cast<unsigned>(page) < static_cast<unsigned>(p.num_pages);
-      if (key && !there) atomicOr(p.status, kStatusDevice);
-      x[q] = load16_if((v ? p.V : p.K) + page * p.page_stride + in * p.token_stride + h * p.head_stride + c * 16, there);
-      b[q] = load_byte_if((v ? p.V_scale : p.K_scale) + page * p.scale_page + (h << p.page_shift) + in, there, 0);
+    auto byte_at = [&](int i, int page) {
+      bool v;
+      const int k = tile_of(i, &v) * kRows + tid;
+      const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.num_pages);
+      return load_byte_if((v ? p.V_scale : p.K_scale) + page * p.scale_page + (h << p.page_shift) + (k & ((1 << p.page_shift) - 1)), there, 127u);
     };
-#pragma unroll
-    for (int q = 0; q < kV; ++q) fetch(q, t, v, ids);
-    int t1 = tile_of(1, &v);
-    int ids1 = 2 * n > 1 ? pages_of(t1) : 0;
-    for (int i = 0; ok && i < 2 * n; ++i) {
-      bool v2;
-      const int t2 = tile_of(i + 2, &v2);
-      const int ids2 = i + 2 < 2 * n ? pages_of(t2) : 0;
-      ok = attn_wait_warp(sm, &sm.empty[st], ph ^ 1, p.status);
-      if (!ok) break;
-      const bool more = i + 1 < 2 * n;
+    uint32_t byte = byte_at(0, page_at(0));
+    int page = page_at(1);
+    for (int i = 0; i < 2 * n; ++i) {
+      sm.power[buf][tid] = power2<kFp16>(byte);
+      byte = byte_at(i + 1, page);
+      page = page_at(i + 2);
+      ok = ok && attn_wait_warp(sm, &sm.rawfull[rs], rph, p.status);
+      ok = ok && attn_wait_warp(sm, &sm.empty[st], ph ^ 1, p.status);
+      group_sync(2);  // (the rows' powers are there, and nobody still reads the ones before the last)
+      bool v;
+      const int k0 = tile_of(i, &v) * kRows;
+      const bool edge = k0 < klo || k0 + kRows > khi;
 #pragma unroll
       for (int q = 0; q < kV; ++q) {
         const int r = r0 + q * kStep;
-        const uint32_t s2 = power2<kFp16>(b[q]);
-        const uint2 w0 = values4<kFp16>(x[q].x, s2), w1 = values4<kFp16>(x[q].y, s2);
-        const uint2 w2 = values4<kFp16>(x[q].z, s2), w3 = values4<kFp16>(x[q].w, s2);
-        if (more) fetch(q, t1, v, ids1);
-        // 16 values: the 16-byte chunks 2 (c mod 4) and the next of 64-element block c / 4; neighbours of the other
-        // block store theirs in the other order, on other banks
-        uint8_t* const at = sm.kv[st] + (c >> 2) * (kRows * 128) + r * 128;
-        const int j = (c & 3) * 2, f = c >> 2;
-        const uint4 lo = make_uint4(w0.x, w0.y, w1.x, w1.y), hi = make_uint4(w2.x, w2.y, w3.x, w3.y);
-        *reinterpret_cast<uint4*>(at + (((j + f) ^ (r & 7)) << 4)) = f ? hi : lo;
-        *reinterpret_cast<uint4*>(at + (((j + 1 - f) ^ (r & 7)) << 4)) = f ? lo : hi;
+        uint4 x = *reinterpret_cast<const uint4*>(sm.raw[rs] + r * D + c * 16);
+        const uint32_t s2 = sm.power[buf][r];
+        if (edge && (k0 + r < klo || k0 + r >= khi)) x = make_uint4(0, 0, 0, 0);
+        const uint2 w0 = values4<kFp16>(x.x, s2), w1 = values4<kFp16>(x.y, s2);
+        const uint2 w2 = values4<kFp16>(x.z, s2), w3 = values4<kFp16>(x.w, s2);
+        uint8_t* const at = sm.kv[st] + to + q * (kStep * 128);
+        *reinterpret_cast<uint4*>(at + j0) = make_uint4(w0.x, w0.y, w1.x, w1.y);
+        *reinterpret_cast<uint4*>(at + j1) = make_uint4(w2.x, w2.y, w3.x, w3.y);
       }
       fence_proxy_async();
       __syncwarp();
       mbar_arrive_elect(&sm.full[st]);
+      mbar_arrive_elect(&sm.rawempty[rs]);
       if (++st == S::kStages) { st = 0; ph ^= 1; }
-      t1 = t2;
-      ids1 = ids2;
-      v = v2;
+      if (++rs == S::kRaw) { rs = 0; rph ^= 1; }
+      buf ^= 1;
     }
   }
 }
@@ -895,9 +939,9 @@ __device__ __forceinline__ uint32_t o_col(int side) { return 256 + side * 128; }
 // for each side they interleave, and either side waits twice as long for its own).  What
 // steers it is broadcast from lane 0, so that the compiler sees one path for the warp and
 // keeps the MMAs' operands in uniform registers.
-template <int D, bool kFp16>
-__device__ __forceinline__ void mma_warp(const PagedAttnParams& p, AttnSmem<D>& sm, uint32_t tmem) {
-  using S = AttnSmem<D>;
+template <int D, bool kFp16, int kMode>
+__device__ __forceinline__ void mma_warp(const PagedAttnParams& p, AttnSmem<D, kMode>& sm, uint32_t tmem) {
+  using S = AttnSmem<D, kMode>;
   constexpr uint32_t kBlock = kRows * 128;  // bytes of a 64-element column block
   constexpr uint32_t kIdescQK = attn_idesc<kFp16, false, false>(128, 128);
   constexpr uint32_t kIdescPV = attn_idesc<kFp16, false, true>(128, D);
@@ -1033,20 +1077,6 @@ __device__ __forceinline__ void mma_warp(const PagedAttnParams& p, AttnSmem<D>& 
 template <int D>
 __device__ __forceinline__ size_t part_bytes() { return kRows * D * 4 + kRows * sizeof(float2); }
 
-__device__ __forceinline__ void group_sync(int x) { named_bar_sync(1 + x, 128); }
-__device__ __forceinline__ bool group_any(int x, bool v) {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred a, b;\n\t"
-      "setp.ne.u32 a, %1, 0;\n\t"
-      "barrier.cta.red.or.pred b, %2, 128, a;\n\t"
-      "selp.u32 %0, 1, 0, b;\n\t}"
-      : "=r"(r)
-      : "r"(static_cast<uint32_t>(v)), "r"(1 + x)
-      : "memory");
-  return r != 0;
-}
-
 // What a softmax warp keeps from entry to entry.
 struct SideState {
   uint32_t sph = 0, oph = 0, xph = 0, qn = 0;  // phases of its barriers, Q tiles before this entry
@@ -1058,15 +1088,15 @@ struct SideState {
 // rows of the V tile that hold no key of the unit, of which anything may be in the pool
 // (0 weight times NaN is NaN).  Only the rows of a page box that also holds keys need it,
 // the others were loaded as zeros.  In a full unit both sides write the same zeros.
-template <int D>
-__device__ __forceinline__ void mend_v(const PagedAttnParams& p, AttnSmem<D>& sm, const Entry& en, int j, SideState& st) {
+template <int D, int kMode>
+__device__ __forceinline__ void mend_v(const PagedAttnParams& p, AttnSmem<D, kMode>& sm, const Entry& en, int j, SideState& st) {
   const int k0 = j * kRows, a = max(en.klo - k0, 0), b = min(en.khi - k0, kRows);
   if (a == 0 && b == kRows) return;
   const int n = en.t1 - en.t0, i = j - en.t0;
   // the V tile's place in the ring's order (K tiles run 1 or 2 ahead)
   const uint32_t at = st.tiles + (en.kind == kFull ? 2 * i + 1 : min(2 * i + 2, 2 * n - 1));
-  const uint32_t stage = at % AttnSmem<D>::kStages;
-  st.ok = st.ok && attn_wait_warp(sm, &sm.full[stage], (at / AttnSmem<D>::kStages) & 1, p.status);
+  const uint32_t stage = at % AttnSmem<D, kMode>::kStages;
+  st.ok = st.ok && attn_wait_warp(sm, &sm.full[stage], (at / AttnSmem<D, kMode>::kStages) & 1, p.status);
   const int box = 1 << min(p.page_shift, 7);
   auto zero = [&](int r0, int r1) {
     for (int q = r0 * (D / 8) + static_cast<int>(threadIdx.x & 127); q < r1 * (D / 8); q += 128) {
@@ -1122,7 +1152,7 @@ __device__ __forceinline__ float finite_or_0(float m) { return m == -INFINITY ? 
 // its key's weights of R rows; they go to shared memory as the B operand of
 // O^T += V^T P^T.  All threads hold the rows' maxima; each sums its own keys' weights.
 template <int D, bool kFp16, int kMode, int R>
-__device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D>& sm, uint32_t tmem, int x, const Entry& en,
+__device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D, kMode>& sm, uint32_t tmem, int x, const Entry& en,
                                          SideState& st) {
   const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, key = warp * 32 + lane;
   const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
@@ -1198,7 +1228,7 @@ __device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D>& 
       l[r] += w;
       *reinterpret_cast<uint16_t*>(pw + r * 128 + ((chunk ^ r) & 7) * 16) = static_cast<uint16_t>(pack2<kFp16>(w, 0.f));
     }
-    if (!(kMode & kQ8)) mend_v<D>(p, sm, en, j, st);
+    if (!(kMode & kQ8)) mend_v<D, kMode>(p, sm, en, j, st);
     fence_proxy_async();
     tc_fence_before();
     __syncwarp();
@@ -1390,7 +1420,7 @@ __device__ __forceinline__ float max32u(const uint32_t (&u)[32]) {
 }
 
 template <int D, bool kFp16, int kMode>
-__device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>& sm, uint32_t tmem, int x, const Entry& en,
+__device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D, kMode>& sm, uint32_t tmem, int x, const Entry& en,
                                           SideState& st, int i0) {
   const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
   const int r = warp * 32 + lane;  // row of the side = TMEM lane
@@ -1490,7 +1520,7 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
             }
           }
         }
-        if (!(kMode & kQ8)) mend_v<D>(p, sm, en, j, st);
+        if (!(kMode & kQ8)) mend_v<D, kMode>(p, sm, en, j, st);
         float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll 1
         for (int q = 0; q < 4; ++q) {
@@ -1506,7 +1536,7 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
         l += sum.x + sum.y;
       }
     } else {
-      if (!(kMode & kQ8)) mend_v<D>(p, sm, en, j, st);
+      if (!(kMode & kQ8)) mend_v<D, kMode>(p, sm, en, j, st);
       hand_over(0);
       hand_over(1);
     }
@@ -1680,7 +1710,7 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D>&
 }
 
 template <int D, bool kFp16, int kMode>
-__device__ __forceinline__ void softmax_group(const PagedAttnParams& p, AttnSmem<D>& sm, uint32_t tmem, int x) {
+__device__ __forceinline__ void softmax_group(const PagedAttnParams& p, AttnSmem<D, kMode>& sm, uint32_t tmem, int x) {
   SideState st;
   const int i0 = static_cast<int>(threadIdx.x & 127) / p.G;  // the thread's row: its token in the side
   for (uint32_t e = 0;; ++e) {
@@ -1697,7 +1727,7 @@ __device__ __forceinline__ void softmax_group(const PagedAttnParams& p, AttnSmem
 template <int D, bool kFp16, int kMode>
 __global__ void __launch_bounds__(Split<kMode>::kThreads, 1) paged_attn_kernel(const __grid_constant__ PagedAttnParams p) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  using S = AttnSmem<D>;
+  using S = AttnSmem<D, kMode>;
   if (smem_u32(smem_raw) & 1023u) {  // the 128-byte swizzle needs 1024-byte aligned buffers
     if (threadIdx.x == 0) atomicOr(p.status, kStatusDevice);
     return;
@@ -1725,6 +1755,11 @@ __global__ void __launch_bounds__(Split<kMode>::kThreads, 1) paged_attn_kernel(c
       mbar_init(&sm.full[i], kMode & kQ8 ? 4 : 1);  // (the loads' bytes; or the converting warps)
       mbar_init(&sm.empty[i], 1);
     }
+    if constexpr ((kMode & kQ8) != 0)
+      for (int i = 0; i < S::kRaw; ++i) {
+        mbar_init(&sm.rawfull[i], 1);
+        mbar_init(&sm.rawempty[i], 4);
+      }
     for (int i = 0; i < kEntries; ++i) {
       mbar_init(&sm.efull[i], 1);
       mbar_init(&sm.eempty[i], kMode & kQ8 ? 14 : 10);  // the load and MMA warps, eight softmax and four converting ones
@@ -1738,7 +1773,7 @@ __global__ void __launch_bounds__(Split<kMode>::kThreads, 1) paged_attn_kernel(c
   }
   if (threadIdx.x == 64) {
     for (const CUtensorMap* m : {&p.qmap1, &p.kmap, &p.vmap, &p.qmap})
-      if (!(kMode & kQ8) || (m != &p.kmap && m != &p.vmap)) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
   }
   if (warp == 1) {
     tmem_alloc(&sm.tmem_slot, 512);
@@ -1762,16 +1797,18 @@ __global__ void __launch_bounds__(Split<kMode>::kThreads, 1) paged_attn_kernel(c
   if (warp < 4) {
     regs_dealloc<Split<kMode>::kControl>();
     if (warp == 0) load_warp<D, kMode>(p, sm);
-    if (warp == 1) mma_warp<D, kFp16>(p, sm, tmem);
+    if (warp == 1) mma_warp<D, kFp16, kMode>(p, sm, tmem);
     if (warp == 2) deal<kMode>(p, sm, sh, ordered);
     __syncwarp();
   } else if (!(kMode & kQ8) || warp < 12) {
     regs_alloc<Split<kMode>::kSoftmax>();
     softmax_group<D, kFp16, kMode>(p, sm, tmem, (warp - 4) >> 2);
   } else {
-    regs_dealloc<Split<kMode>::kConvert>();
-    convert_group<D, kFp16>(p, sm);
-    __syncwarp();
+    if constexpr ((kMode & kQ8) != 0) {
+      regs_dealloc<Split<kMode>::kConvert>();
+      convert_group<D, kFp16, kMode>(p, sm);
+      __syncwarp();
+    }
   }
   tc_fence_before();
   __syncthreads();
@@ -1789,7 +1826,8 @@ AttnFn attn_fn(int d, bool fp16) {
   if (d == 64) return fp16 ? paged_attn_kernel<64, true, kMode> : paged_attn_kernel<64, false, kMode>;
   return fp16 ? paged_attn_kernel<128, true, kMode> : paged_attn_kernel<128, false, kMode>;
 }
-size_t attn_smem(int d) { return d == 64 ? sizeof(AttnSmem<64>) : sizeof(AttnSmem<128>); }
+template <int kMode>
+size_t attn_smem(int d) { return d == 64 ? sizeof(AttnSmem<64, kMode>) : sizeof(AttnSmem<128, kMode>); }
 
 // CTAs to launch of a kernel, per device; 0: it is not ready there yet.
 struct AttnReady {
@@ -1822,7 +1860,7 @@ int ready_kernel(AttnReady& r, AttnFn fn, size_t smem, int threads, int register
 template <int kMode>
 int attn_ready(int d, bool fp16, int* grid) {
   static AttnReady ready[4];
-  return ready_kernel(ready[(d == 64 ? 0 : 2) + (fp16 ? 1 : 0)], attn_fn<kMode>(d, fp16), attn_smem(d), Split<kMode>::kThreads,
+  return ready_kernel(ready[(d == 64 ? 0 : 2) + (fp16 ? 1 : 0)], attn_fn<kMode>(d, fp16), attn_smem<kMode>(d), Split<kMode>::kThreads,
                       Split<kMode>::kNeeded, grid);
 }
 
@@ -1929,7 +1967,7 @@ int attn_launch(const PagedAttnParams& p, int d, bool fp16, cudaStream_t stream)
   int grid = 0;
   const int rc = attn_ready<kMode>(d, fp16, &grid);
   if (rc != KVEV_OK) return rc;
-  return launch_overlapped(attn_fn<kMode>(d, fp16), p, grid, Split<kMode>::kThreads, attn_smem(d), stream) == cudaSuccess ? KVEV_OK
+  return launch_overlapped(attn_fn<kMode>(d, fp16), p, grid, Split<kMode>::kThreads, attn_smem<kMode>(d), stream) == cudaSuccess ? KVEV_OK
                                                                                                                     : KVEV_ECUDA;
 }
 

@@ -32,6 +32,9 @@ extern "C" int kvev_paged_q8_attention(const kvev_paged_q8_cache* cache, const v
   p.scale_page = view.scale_page;
   const int few = kFewRows / p.G;  // most tokens of a request of few rows
   if (few > 0) rc = few_launch(p, cache, a.stream);
-  if (rc == KVEV_OK && T > few) rc = attn_launch<kQ8>(p, cache->d, view.fp16, a.stream);
+  if (rc == KVEV_OK && T > few) {
+    if (!q8_page_maps(cache, CU_TENSOR_MAP_SWIZZLE_NONE, &p)) return KVEV_ECUDA;
+    rc = attn_launch<kQ8>(p, cache->d, view.fp16, a.stream);
+  }
   return rc;
 }

@@ -687,6 +687,23 @@ AttnFn few_fn(int d, bool fp16) {
   return fp16 ? q8_few_kernel<128, true> : q8_few_kernel<128, false>;
 }
 
+// The maps of a cache's pages of codes.
+bool q8_page_maps(const kvev_paged_q8_cache* cache, CUtensorMapSwizzle swizzle, PagedAttnParams* p) {
+  auto encode = encode_fn();
+  if (!encode) return false;
+  const cuuint64_t dims[4] = {static_cast<cuuint64_t>(cache->d), static_cast<cuuint64_t>(cache->page_size),
+                              static_cast<cuuint64_t>(cache->H_kv), static_cast<cuuint64_t>(cache->num_pages)};
+  const cuuint64_t strides[3] = {static_cast<cuuint64_t>(cache->token_stride), static_cast<cuuint64_t>(cache->head_stride),
+                                 static_cast<cuuint64_t>(cache->page_stride)};
+  const cuuint32_t box[4] = {static_cast<cuuint32_t>(cache->d), static_cast<cuuint32_t>(cache->page_size < kRows ? cache->page_size : kRows), 1, 1};
+  const cuuint32_t ones[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 2; ++i)
+    if (encode(i ? &p->vmap : &p->kmap, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, i ? cache->V : cache->K, dims, strides, box, ones,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return false;
+  return true;
+}
+
 // The requests of few rows; p but for the maps of the pages.
 int few_launch(PagedAttnParams p, const kvev_paged_q8_cache* cache, cudaStream_t stream) {
   const int d = cache->d;
@@ -697,19 +714,7 @@ int few_launch(PagedAttnParams p, const kvev_paged_q8_cache* cache, cudaStream_t
   static AttnReady ready[4];
   const int rc = ready_kernel(ready[(d == 64 ? 0 : 2) + (fp16 ? 1 : 0)], fn, smem, kFewThreads, 0, &grid);
   if (rc != KVEV_OK) return rc;
-  auto encode = encode_fn();
-  if (!encode) return KVEV_ECUDA;
-  const cuuint64_t dims[4] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(cache->page_size), static_cast<cuuint64_t>(cache->H_kv),
-                              static_cast<cuuint64_t>(cache->num_pages)};
-  const cuuint64_t strides[3] = {static_cast<cuuint64_t>(cache->token_stride), static_cast<cuuint64_t>(cache->head_stride),
-                                 static_cast<cuuint64_t>(cache->page_stride)};
-  const cuuint32_t box[4] = {static_cast<cuuint32_t>(d), static_cast<cuuint32_t>(cache->page_size < kRows ? cache->page_size : kRows), 1, 1};
-  const cuuint32_t ones[4] = {1, 1, 1, 1};
-  for (int i = 0; i < 2; ++i)
-    if (encode(i ? &p.vmap : &p.kmap, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, i ? cache->V : cache->K, dims, strides, box, ones,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, d == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
-               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-      return KVEV_ECUDA;
+  if (!q8_page_maps(cache, d == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, &p)) return KVEV_ECUDA;
   static_assert(2 * kFewCtas * kMaxCtas * sizeof(int) <= KVEV_PAGED_SYNC_BYTES, "arrival counts");
   return launch_overlapped(fn, p, kFewCtas * grid, kFewThreads, smem, stream) == cudaSuccess ? KVEV_OK : KVEV_ECUDA;
 }
