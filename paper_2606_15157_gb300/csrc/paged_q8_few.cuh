@@ -208,7 +208,7 @@ __device__ __forceinline__ void few_load_warp(const PagedAttnParams& p, Q8Smem<D
     // lane i holds the page of the tile's box i: its entry of the table, read three tiles ahead and checked when used
     auto page_of = [&](int t) {
       const int k = t * kRows + (lane << box_shift);
-      return t < t1 && lane < boxes && k < khi && k + (1 << box_shift) > klo ? row[k >> p.page_shift] : INT_MAX;
+      return load_int_if(row + (k >> p.page_shift), t < t1 && lane < boxes && k < khi && k + (1 << box_shift) > klo, INT_MAX);
     };
     auto checked = [&](int id) {  // num_pages (loads zeros) for no page or one outside the pool
       if (static_cast<unsigned>(id) < static_cast<unsigned>(p.num_pages)) return id;
@@ -379,7 +379,7 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>&
   const int* row = p.table + static_cast<long long>(en.s) * p.max_pages;
   auto page_at = [&](int j) {
     const int k = j * kRows + key;
-    return j < en.t1 && k >= en.klo && k < en.khi ? row[k >> p.page_shift] : -1;
+    return load_int_if(row + (k >> p.page_shift), j < en.t1 && k >= en.klo && k < en.khi, -1);
   };
   auto exponents_at = [&](int j, int page) {  // (K's, V's; of a zero row where there is none)
     const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.num_pages);
