@@ -62,14 +62,15 @@ namespace {
 // What the kernel is compiled for, beside head size and type: kShared, groups of requests whose first keys are in
 // common pages, which a unit of the group's rows reads once (paged_shared.cu); kQ8, pages of 8-bit codes, which a
 // warpgroup of its own turns into 16-bit tiles (paged_q8_attn.cu).
-// kFewOnly: the requests of few rows, which the kernel of paged_q8_few.cu takes with the codes as they are; kQ8 alone
+// kFewOnly: the requests of few rows, which the kernel of paged_q8_few.cuh takes with the codes as they are; kQ8 alone
 // leaves those out.
 enum Mode : int { kPlain = 0, kShared = 1, kQ8 = 2, kFewOnly = 4 };
+constexpr int kConvertThreads = 256;
 template <int kMode>
 struct Split {  // threads, and the warpgroups' registers
-  static constexpr int kThreads = (kMode & kQ8) && !(kMode & kFewOnly) ? 512 : 384;
-  static constexpr int kControl = kMode & kQ8 ? 48 : 56, kSoftmax = kMode & kQ8 ? 184 : 224, kConvert = 96;
-  static constexpr int kNeeded = 128 * kControl + 256 * kSoftmax + (kMode & kQ8 ? 128 * kConvert : 0);
+  static constexpr int kThreads = kMode & kFewOnly ? 256 : kMode & kQ8 ? 384 + kConvertThreads : 384;
+  static constexpr int kControl = kMode & kQ8 ? 40 : 56, kSoftmax = kMode & kQ8 ? 168 : 224, kConvert = 48;
+  static constexpr int kNeeded = 128 * kControl + 256 * kSoftmax + (kMode & kQ8 ? kConvertThreads * kConvert : 0);
 };
 constexpr int kMaxCtas = 152;
 constexpr int kEntries = 4;         // ring of dealt entries
@@ -115,6 +116,7 @@ struct PagedAttnParams {
   int N;
   float *part_o, *part_lse;
   // kQ8: queries, codes and the rows' exponents, strides in bytes
+  int few;  // most tokens of a request of few rows
   const uint8_t* q;
   long long q_token, q_head;
   const uint8_t *K, *V, *K_scale, *V_scale;
@@ -171,7 +173,7 @@ struct AttnSmemBase {
   long long carry, start;
   union {
     float red[2][4][kFewRows];  // a side's warps' maxima or sums of a few rows
-    long long scan[16];  // the schedule's sums, at the start
+    long long scan[32];  // the schedule's sums, at the start
   };
   int last[2];
   int abort_flag;
@@ -386,7 +388,7 @@ template <int kMode>
 __device__ __forceinline__ Request request(const PagedAttnParams& p, int s, bool ordered, bool* bad) {
   if (!(kMode & kShared)) {
     Request r = own_request(p, s, bad);
-    if ((kMode & kQ8) && (r.q <= kFewRows / p.G) != ((kMode & kFewOnly) != 0)) r.q = 0;
+    if ((kMode & kQ8) && (r.q <= p.few) != ((kMode & kFewOnly) != 0)) r.q = 0;
     return r;
   }
   if (s < p.N) {
@@ -477,12 +479,28 @@ __device__ __forceinline__ long long block_prefix(S& sm, long long v, long long*
 struct Share {
   long long x0, x1, before, share;
   int s, h;  // (h: kHeadsOuter)
+  long long origin;  // shares are counted from here,
+  int cta0;          // the first of them this CTA's
 };
-// The CTA's share of `outer` rounds of cost `round`; before: the cost of the rounds before its own.
+// The CTA's share of `outer` rounds of cost `round`; before: the cost of the rounds before its own.  kFewOnly, where the CTAs
+// divide by the rounds: each round its own CTAs, so that all rounds, the KV heads, are at the same place at the same time.
+// (Codes of a token's heads are 64 or 128 bytes next to one another in tokens-first pages: 64 generations over 4,097 tokens, 64-element
+// heads, with shares that do not end with the heads 111 us, %%G so.)
+template <int kMode>
 __device__ __forceinline__ Share share_at(long long round, int outer, int least) {
-  Share r;
+  Share r = {};
+  const int grid = gridDim.x, per = grid / outer;
+  if ((kMode & kFewOnly) && per * outer == grid) {
+    r.h = blockIdx.x / per;
+    r.cta0 = r.h * per;
+    r.share = max(static_cast<long long>(least), divide(round + per - 1, per));
+    r.before = r.origin = r.h * round;
+    r.x0 = r.origin + min(round, r.share * (static_cast<int>(blockIdx.x) - r.cta0));
+    r.x1 = min(r.origin + round, r.x0 + r.share);
+    return r;
+  }
   const long long total = round * outer;
-  r.share = max(static_cast<long long>(least), divide(total + gridDim.x - 1, gridDim.x));
+  r.share = max(static_cast<long long>(least), divide(total + grid - 1, grid));
   r.x0 = min(total, r.share * blockIdx.x);
   r.x1 = min(total, r.x0 + r.share);
   r.h = outer > 1 && round > 0 ? static_cast<int>(divide(r.x0, round)) : 0;
@@ -506,7 +524,7 @@ __device__ __forceinline__ Share share_of(const PagedAttnParams& p, S& sm, bool 
     total += all;
   }
   if (bad && blockIdx.x == 0) atomicOr(p.status, kStatusDevice);
-  Share r = share_at(total, outer, kMinShare);
+  Share r = share_at<kMode>(total, outer, kMinShare);
   const long long x = r.x0 - r.before;
   // the thread whose request holds x0 says so
   if (p.segs <= kThreads) {
@@ -556,7 +574,7 @@ __device__ __forceinline__ Share share_of_warp(const PagedAttnParams& p, Request
     if (lane >= o) upto += x;
   }
   const bool rows = __any_sync(0xffffffffu, held.q * p.G > kFewRows);
-  Share r = share_at(__shfl_sync(0xffffffffu, upto, 31), S::kHeadsOuter ? p.H_kv : 1, rows ? kMinShareRows : kMinShare);
+  Share r = share_at<kMode>(__shfl_sync(0xffffffffu, upto, 31), S::kHeadsOuter ? p.H_kv : 1, rows ? kMinShareRows : kMinShare);
   const long long x = r.x0 - r.before;
   const uint32_t here = __ballot_sync(0xffffffffu, mine > 0 && upto - mine <= x && x < upto);
   r.s = here ? __ffs(here) - 1 : 0;  // (none: the share is empty)
@@ -629,8 +647,9 @@ __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, Share sh, 
         en.khi = u.hi;
         en.kind = u.kind;
         en.part = !(kMode & kShared) ? -1 : r.open ? 0 : r.lo > 0 ? 1 : -1;
-        en.first = static_cast<int>(divide(a, sh.share));
-        en.pieces = static_cast<int>(divide(a + static_cast<long long>(w) * (u.tiles - 1), sh.share)) - en.first + 1;
+        en.first = static_cast<int>(divide(a - sh.origin, sh.share));
+        en.pieces = static_cast<int>(divide(a - sh.origin + static_cast<long long>(w) * (u.tiles - 1), sh.share)) - en.first + 1;
+        en.first += sh.cta0;
         if (!put(en)) return;
       }
       a += cost_of(u);
@@ -791,7 +810,7 @@ __device__ __forceinline__ void load_warp(const PagedAttnParams& p, AttnSmem<D, 
   }
 }
 
-// Barriers of four warps: the sides' softmax groups 0 and 1, and with kQ8 the converting warps 2.
+// Barriers of four warps: the sides' softmax groups.
 __device__ __forceinline__ void group_sync(int x) { named_bar_sync(1 + x, 128); }
 __device__ __forceinline__ bool group_any(int x, bool v) {
   uint32_t r;
@@ -857,12 +876,25 @@ __device__ __forceinline__ void values16(uint4 x, uint32_t b, uint4& lo, uint4& 
   hi = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
+__device__ __forceinline__ bool convert_any(bool v) {  // over the converting warps
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred a, b;\n\t"
+      "setp.ne.u32 a, %1, 0;\n\t"
+      "barrier.cta.red.or.pred b, 3, %2, a;\n\t"
+      "selp.u32 %0, 1, 0, b;\n\t}"
+      : "=r"(r)
+      : "r"(static_cast<uint32_t>(v)), "n"(kConvertThreads)
+      : "memory");
+  return r != 0;
+}
+
 template <int D, bool kFp16, int kMode>
 __device__ __forceinline__ void convert_group(const PagedAttnParams& p, AttnSmem<D, kMode>& sm) {
   using S = AttnSmem<D, kMode>;
   constexpr int kLanes = D / 16;                  // threads of a row
-  constexpr int kStep = 128 / kLanes, kV = kRows / kStep;  // rows of the group at a time, vectors of a thread
-  const int tid = threadIdx.x & 127;
+  constexpr int kStep = kConvertThreads / kLanes, kV = kRows / kStep;  // rows of the group at a time, vectors of a thread
+  const int tid = threadIdx.x - 384;
   // Threads of the second 64-element block take the neighbouring row's chunks, whose place differs in one bit: the
   // stores of a row's threads go to different banks.
   const int c = tid % kLanes, block = c >> 2, r0 = (tid / kLanes) ^ block;
@@ -873,7 +905,7 @@ __device__ __forceinline__ void convert_group(const PagedAttnParams& p, AttnSmem
   for (uint32_t e = 0;; ++e) {
     const Entry en = take(p, sm, e);
     // (the warps agree, and after a wait that ran out they run on, so that each reaches the same barriers)
-    if (group_any(2, en.n == 0)) break;
+    if (convert_any(en.n == 0)) break;
     const int h = uniform(en.h), t0 = uniform(en.t0), n = uniform(en.t1) - t0, klo = uniform(en.klo), khi = uniform(en.khi);
     const int* row = p.table + static_cast<long long>(uniform(en.s)) * p.max_pages;
     const int A = min(uniform(en.kind) == kFull ? 1 : 2, n);
@@ -887,7 +919,7 @@ __device__ __forceinline__ void convert_group(const PagedAttnParams& p, AttnSmem
     auto page_at = [&](int i) {
       bool v;
       const int k = tile_of(i, &v) * kRows + tid;
-      return load_int_if(row + (k >> p.page_shift), i < 2 * n && k >= klo && k < khi, -1);
+      return load_int_if(row + (k >> p.page_shift), tid < kRows && i < 2 * n && k >= klo && k < khi, -1);
     };
     auto byte_at = [&](int i, int page) {
       bool v;
@@ -898,12 +930,12 @@ __device__ __forceinline__ void convert_group(const PagedAttnParams& p, AttnSmem
     uint32_t byte = byte_at(0, page_at(0));
     int page = page_at(1);
     for (int i = 0; i < 2 * n; ++i) {
-      sm.power[buf][tid] = byte;
+      if (tid < kRows) sm.power[buf][tid] = byte;
       byte = byte_at(i + 1, page);
       page = page_at(i + 2);
       ok = ok && attn_wait_warp(sm, &sm.rawfull[rs], rph, p.status);
       ok = ok && attn_wait_warp(sm, &sm.empty[st], ph ^ 1, p.status);
-      group_sync(2);  // (the rows' powers are there, and nobody still reads the ones before the last)
+      named_bar_sync(3, kConvertThreads);  // (the rows' powers are there, and nobody still reads the ones before the last)
       bool v;
       const int k0 = tile_of(i, &v) * kRows;
       const bool edge = k0 < klo || k0 + kRows > khi;
@@ -1750,7 +1782,7 @@ __global__ void __launch_bounds__(Split<kMode>::kThreads, 1) paged_attn_kernel(c
     bool some = false;
     for (int s = threadIdx.x; s < p.B; s += Split<kMode>::kThreads) {
       const int c0 = p.cu[s], c1 = p.cu[s + 1];
-      some |= c0 < 0 || c1 > p.T || c1 < c0 || c1 - c0 > kFewRows / p.G;  // (what is out of range is said by the schedule)
+      some |= c0 < 0 || c1 > p.T || c1 < c0 || c1 - c0 > p.few;  // (what is out of range is said by the schedule)
     }
     if (!__syncthreads_or(some)) return;
   }
@@ -1763,17 +1795,17 @@ __global__ void __launch_bounds__(Split<kMode>::kThreads, 1) paged_attn_kernel(c
       mbar_init(&sm.ofull[i], 1);
     }
     for (int i = 0; i < S::kStages; ++i) {
-      mbar_init(&sm.full[i], kMode & kQ8 ? 4 : 1);  // (the loads' bytes; or the converting warps)
+      mbar_init(&sm.full[i], kMode & kQ8 ? kConvertThreads / 32 : 1);  // (the loads' bytes; or the converting warps)
       mbar_init(&sm.empty[i], 1);
     }
     if constexpr ((kMode & kQ8) != 0)
       for (int i = 0; i < S::kRaw; ++i) {
         mbar_init(&sm.rawfull[i], 1);
-        mbar_init(&sm.rawempty[i], 4);
+        mbar_init(&sm.rawempty[i], kConvertThreads / 32);
       }
     for (int i = 0; i < kEntries; ++i) {
       mbar_init(&sm.efull[i], 1);
-      mbar_init(&sm.eempty[i], kMode & kQ8 ? 14 : 10);  // the load and MMA warps, eight softmax and four converting ones
+      mbar_init(&sm.eempty[i], kMode & kQ8 ? 10 + kConvertThreads / 32 : 10);  // the load and MMA warps, eight softmax warps and the converting ones
     }
     mbar_init(&sm.xfull, 8);
     mbar_init(&sm.xfree, 8);

@@ -30,9 +30,10 @@ extern "C" int kvev_paged_q8_attention(const kvev_paged_q8_cache* cache, const v
   p.token_stride = view.token_stride;
   p.head_stride = view.head_stride;
   p.scale_page = view.scale_page;
-  const int few = kFewRows / p.G;  // most tokens of a request of few rows
-  if (few > 0) rc = few_launch(p, cache, a.stream);
-  if (rc == KVEV_OK && T > few) {
+  const int rows = few_rows_of(p.G, B, T);
+  p.few = rows / p.G;
+  if (p.few > 0) rc = few_launch(p, cache, rows, a.stream);
+  if (rc == KVEV_OK && T > p.few) {
     if (!q8_page_maps(cache, CU_TENSOR_MAP_SWIZZLE_NONE, &p)) return KVEV_ECUDA;
     rc = attn_launch<kQ8>(p, cache->d, view.fp16, a.stream);
   }

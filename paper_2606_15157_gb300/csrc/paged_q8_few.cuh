@@ -13,8 +13,10 @@
 // weight may hold values that outweigh all others'.
 //
 // Layout as in paged_attn.cuh: keys on the lanes, S^T = A q^T (K-major codes as loaded), a thread per key forms
-// its key's weights, O^T += B^T w^T with the codes of V as the operand whose key index runs slowest.  Two sides take
-// the key tiles in turn; the schedule, its pieces and their merge are the same.
+// its key's weights, O^T += B^T w^T with the codes of V as the operand whose key index runs slowest; the schedule is the
+// same, and so are pieces and their merge.  A CTA has one softmax warpgroup and takes its units one after another; what hides a
+// tile's chain of latencies (scores, weights, products) and a unit's start and end is the other CTAs of the SM.
+// (%%F)
 #pragma once
 #include "paged_attn.cuh"
 
@@ -29,37 +31,43 @@ constexpr float kFewRaise = 3.f; // a maximum is raised when a tile's is this mu
 constexpr float kFewUp = 5.f;    // and the weights are 2^kFewUp larger: up to 2^8
 constexpr int kRowGroup = 4;     // rows that a thread works on at once:
 constexpr int kGroupCols = kQParts * kRowGroup;  // columns [part][row] of such a group
-constexpr int kFewCols = kQParts * kFewRows;     // columns of a side's scores, and of its output: group after group
-constexpr int kFewCtas = 2;      // CTAs of an SM
+// CTAs of an SM, by the most rows of a unit (4, 8 or 16): what shared memory and registers allow.
+constexpr int few_ctas(int M) { return M <= 8 ? 3 : 2; }
 
-template <int D>
+template <int D, int M>
 struct Q8Smem {
   // rows of 64 or 128 bytes: as for 16-bit rows of 64 elements
   static constexpr bool kHeadsOuter = true;
-  static constexpr int kTileBytes = kRows * D;
-  static constexpr int kStages = D == 128 ? 5 : 10;
+  static constexpr int kTileBytes = kRows * D, kCols = kQParts * M;
+  static constexpr int kStages = (M <= 4 ? 4 : M == 8 ? 3 : 5) * (D == 128 ? 1 : 2);
   uint8_t kv[kStages][kTileBytes];
-  uint8_t p[2][kFewCols * kRows];  // the sides' weights [column][128 keys]
-  uint8_t q[kFewCols * D];         // [column][D]
-  float qscale[2][kFewRows];       // of an entry's rows: log2(e) scale over their power of two
-  float m[2][kFewRows], mz[2][kFewRows], l[2][kFewRows];  // the sides' maxima, the weights' maxima, sums
+  uint8_t p[2][kCols * kRows];  // weights of every other tile [column][128 keys]
+  uint8_t q[kCols * D];         // [column][D]
+  float qscale[2][M];           // of an entry's rows: log2(e) scale over their power of two
+  float m[M], mz[M];            // the rows' maxima, the weights' maxima
   Entry ring[kEntries];
   uint64_t qfull[2], qempty, full[kStages], empty[kStages];  // (qfull: of every other entry)
-  uint64_t sfull[2], pfull[2], ofull[2];
-  uint64_t efull[kEntries], eempty[kEntries];
-  uint64_t xfull, xfree, done;
+  uint64_t sfull, pfull;
+  // the output holds another tile, its last.  (Told apart: whoever waits for a tile to be in knows that the one before it
+  // is, as a phase's parity tells no more; of the last two nobody waits for the first.)
+  uint64_t odone, ofull;
+  uint64_t efull[kEntries], eempty[kEntries], done;
   long long carry, start;
   union {
-    float red[2][2][4][kFewRows];  // a side's warps' maxima, or sums, of the rows
-    long long scan[16];
+    float red[2][4][M];  // the warps' maxima, or sums, of the rows
+    long long scan[Split<kQ8 | kFewOnly>::kThreads / 32];
+    float2 ml[128];      // (m, l) of pieces
   };
-  int last[2];
+  int last[1];
   int abort_flag;
   uint32_t tmem_slot;
 };
 // (1 KB of an SM's 228 goes to each CTA beside what it asks for)
-static_assert(kFewCtas * (sizeof(Q8Smem<64>) + 1024) <= 228 * 1024 && kFewCtas * (sizeof(Q8Smem<128>) + 1024) <= 228 * 1024,
-              "shared memory of an SM");
+template <int M>
+constexpr bool fits() {
+  return few_ctas(M) * (sizeof(Q8Smem<64, M>) + 1024) <= 228 * 1024 && few_ctas(M) * (sizeof(Q8Smem<128, M>) + 1024) <= 228 * 1024;
+}
+static_assert(fits<4>() && fits<8>() && fits<16>(), "shared memory of an SM");
 
 // D(tmem) (+)= A B, e4m3 operands in shared memory, fp32 sums.  From a whole converged warp.
 __device__ __forceinline__ void umma8_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
@@ -118,14 +126,14 @@ __device__ __forceinline__ void parts2(float a, float b, uint32_t (&c)[kQParts])
 }
 
 // Rows in whole groups: 4, 8 or 16.
-__device__ __forceinline__ int rows_held(int rows) { return rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
+__host__ __device__ inline int rows_held(int rows) { return rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
 // The column of part q of row r.
 __device__ __forceinline__ int column_of(int q, int r) { return r / kRowGroup * kGroupCols + q * kRowGroup + r % kRowGroup; }
 
 // ---- warp 3: the rows of q in parts --------------------------------------------------------
 
-template <int D, bool kFp16>
-__device__ __forceinline__ void split_queries(const PagedAttnParams& p, Q8Smem<D>& sm) {
+template <int D, bool kFp16, int M>
+__device__ __forceinline__ void split_queries(const PagedAttnParams& p, Q8Smem<D, M>& sm) {
   constexpr int kLanes = D / 16;
   const int lane = threadIdx.x & 31, c = lane % kLanes;
   uint32_t qn = 0;
@@ -192,9 +200,9 @@ __device__ __forceinline__ void split_queries(const PagedAttnParams& p, Q8Smem<D
 
 // ---- warp 0: pages -----------------------------------------------------------------------
 // Tiles in the order K t, K t + 1, V t, K t + 2, V t + 1, ...
-template <int D>
-__device__ __forceinline__ void few_load_warp(const PagedAttnParams& p, Q8Smem<D>& sm) {
-  using S = Q8Smem<D>;
+template <int D, int M>
+__device__ __forceinline__ void few_load_warp(const PagedAttnParams& p, Q8Smem<D, M>& sm) {
+  using S = Q8Smem<D, M>;
   const int lane = threadIdx.x & 31;
   const int box_shift = min(p.page_shift, 7);
   const int boxes = kRows >> box_shift;
@@ -257,13 +265,11 @@ __device__ __forceinline__ void few_load_warp(const PagedAttnParams& p, Q8Smem<D
 
 // ---- warp 1: MMAs ------------------------------------------------------------------------
 
-__device__ __forceinline__ uint32_t few_s_col(int side) { return side * kFewCols; }
-__device__ __forceinline__ uint32_t few_o_col(int side) { return (2 + side) * kFewCols; }
-
-template <int D>
-__device__ __forceinline__ void few_mma_warp(const PagedAttnParams& p, Q8Smem<D>& sm, uint32_t tmem) {
-  using S = Q8Smem<D>;
-  uint32_t st = 0, ph = 0, qn = 0, pph[2] = {0, 0};
+// Tensor memory: scores, then the output.
+template <int D, int M>
+__device__ __forceinline__ void few_mma_warp(const PagedAttnParams& p, Q8Smem<D, M>& sm, uint32_t tmem) {
+  using S = Q8Smem<D, M>;
+  uint32_t st = 0, ph = 0, qn = 0, pph = 0;
   bool ok = true;
   auto advance = [&] { if (++st == S::kStages) { st = 0; ph ^= 1; } };
   auto tile = [&] { ok = ok && attn_wait_warp(sm, &sm.full[st], ph, p.status); };
@@ -275,38 +281,36 @@ __device__ __forceinline__ void few_mma_warp(const PagedAttnParams& p, Q8Smem<D>
     const uint64_t qdesc = rows_desc<D>(smem_u32(sm.q));
     const uint32_t idesc_kq = idesc8<false>(128, 0) | static_cast<uint32_t>(N >> 3) << 17;
     const uint32_t idesc_vp = idesc8<true>(128, 0) | static_cast<uint32_t>(N >> 3) << 17;
-    auto kq = [&](int x) {
+    auto kq = [&](int j) {
       tile();
       if (!ok) return;
       tc_fence_after();
       const uint64_t kdesc = rows_desc<D>(smem_u32(sm.kv[st]));
 #pragma unroll
-      for (int k = 0; k < D / 32; ++k) umma8_ss(tmem + few_s_col(x), kdesc + 2 * k, qdesc + 2 * k, idesc_kq, k > 0);
-      umma_commit_elect(&sm.sfull[x]);
+      for (int k = 0; k < D / 32; ++k) umma8_ss(tmem, kdesc + 2 * k, qdesc + 2 * k, idesc_kq, k > 0);
+      umma_commit_elect(&sm.sfull);
       umma_commit_elect(&sm.empty[st]);
+      if (j == n - 1) umma_commit_elect(&sm.qempty);
       advance();
     };
-    for (int j = 0; j < 2 && j < n; ++j) kq(j);
+    kq(0);
     for (int j = 0; ok && j < n; ++j) {
-      const int x = j & 1;
-      tile();
-      ok = ok && attn_wait_warp(sm, &sm.pfull[x], pph[x], p.status);
+      // the next tile's scores go first: the softmax waits for them, and for the output only to raise a maximum
+      ok = ok && attn_wait_warp(sm, &sm.pfull, pph, p.status);
       if (!ok) break;
-      pph[x] ^= 1;
+      pph ^= 1;
+      if (j + 1 < n) kq(j + 1);
+      tile();
+      if (!ok) break;
       tc_fence_after();
-      const uint64_t vdesc = rows_desc<D>(smem_u32(sm.kv[st])), pdesc = rows_desc<128>(smem_u32(sm.p[x]));
+      const uint64_t vdesc = rows_desc<D>(smem_u32(sm.kv[st])), pdesc = rows_desc<128>(smem_u32(sm.p[j & 1]));
 #pragma unroll
       for (int k = 0; k < kRows / 32; ++k)
-        umma8_ss(tmem + few_o_col(x), vdesc + k * (32 * D / 16), pdesc + 2 * k, idesc_vp, j >= 2 || k > 0);
+        umma8_ss(tmem + S::kCols, vdesc + k * (32 * D / 16), pdesc + 2 * k, idesc_vp, j > 0 || k > 0);
       umma_commit_elect(&sm.empty[st]);
-      if (j + 2 >= n) umma_commit_elect(&sm.ofull[x]);
+      umma_commit_elect(j + 1 < n ? &sm.odone : &sm.ofull);
       advance();
-      if (j + 2 < n) {
-        kq(x);
-        if (j + 3 == n) umma_commit_elect(&sm.qempty);
-      }
     }
-    if (n <= 2) umma_commit_elect(&sm.qempty);
   }
   umma_commit_elect(&sm.done);
   attn_drain(&sm.done, 0);
@@ -315,14 +319,15 @@ __device__ __forceinline__ void few_mma_warp(const PagedAttnParams& p, Q8Smem<D>
 // ---- softmax: a thread per key -------------------------------------------------------------
 
 // As mend_v: zeroes the rows of the V tile that hold no key of the unit but lie in a page box that does.
-template <int D>
-__device__ __forceinline__ void few_mend_v(const PagedAttnParams& p, Q8Smem<D>& sm, const Entry& en, int j, SideState& st) {
+template <int D, int M>
+__device__ __forceinline__ void few_mend_v(const PagedAttnParams& p, Q8Smem<D, M>& sm, const Entry& en, int j, SideState& st) {
+  using S = Q8Smem<D, M>;
   const int k0 = j * kRows, a = max(en.klo - k0, 0), b = min(en.khi - k0, kRows);
   if (a == 0 && b == kRows) return;
   const int n = en.t1 - en.t0, i = j - en.t0;
   const uint32_t at = st.tiles + min(2 * i + 2, 2 * n - 1);  // the V tile's place in the ring's order
-  const uint32_t stage = at % Q8Smem<D>::kStages;
-  st.ok = st.ok && attn_wait_warp(sm, &sm.full[stage], (at / Q8Smem<D>::kStages) & 1, p.status);
+  const uint32_t stage = at % S::kStages;
+  st.ok = st.ok && attn_wait_warp(sm, &sm.full[stage], (at / S::kStages) & 1, p.status);
   const int box = 1 << min(p.page_shift, 7);
   auto zero = [&](int r0, int r1) {
     for (int q = r0 * (D / 16) + static_cast<int>(threadIdx.x & 127); q < r1 * (D / 16); q += 128)
@@ -344,12 +349,12 @@ __device__ __forceinline__ void load_rows(uint32_t taddr, float (&v)[kRowGroup])
   }
 }
 
-// A cut unit's piece, side x: its rows' outputs [row][D], then their (m, l).
+// A cut unit's piece: its rows' outputs [row][D], then their (m, l).
 template <int D>
-__device__ __forceinline__ Records<D> few_records(const PagedAttnParams& p, long long cta, bool first, int x) {
+__device__ __forceinline__ Records<D> few_record(const PagedAttnParams& p, long long cta, bool first) {
   constexpr size_t kBytes = kFewRows * (D * sizeof(float) + sizeof(float2));
-  static_assert(kFewCtas * kBytes <= kRows * (D * sizeof(float) + sizeof(float2)), "within the workspace");
-  return {p.parts + ((2 * cta + (first ? 1 : 0)) * 2 + x) * kBytes};
+  static_assert(2 * 3 * kBytes <= 4 * kRows * (D * sizeof(float) + sizeof(float2)), "within the workspace");
+  return {p.parts + (2 * cta + (first ? 1 : 0)) * kBytes};
 }
 template <int D>
 __device__ __forceinline__ float2* few_ml(const Records<D>& r) { return reinterpret_cast<float2*>(r.at + kFewRows * D * sizeof(float)); }
@@ -361,21 +366,21 @@ __device__ __forceinline__ float warp_max(float v) {
 }
 
 // kGroups groups of rows.
-template <int D, bool kFp16, int kGroups>
-__device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>& sm, uint32_t tmem, int x, const Entry& en,
-                                            SideState& st) {
+template <int D, bool kFp16, int M, int kGroups>
+__device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D, M>& sm, uint32_t tmem, const Entry& en, SideState& st,
+                                            uint32_t& done) {
   constexpr int R = kGroups * kRowGroup;
   const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, key = warp * 32 + lane;
   const uint32_t lanes = static_cast<uint32_t>(warp * 32) << 16;
-  const uint32_t ts = tmem + lanes + few_s_col(x), to = tmem + lanes + few_o_col(x);
+  const uint32_t ts = tmem + lanes, to = ts + Q8Smem<D, M>::kCols;
   const int rows = en.n * p.G;
   const int f1 = rows < R ? 0 : (en.pos0 + 1) >> 7;  // [f0, f1): every row sees every key
   const int f0 = p.window > 0 ? (max(0, en.pos0 + en.n - p.window) + 127) >> 7 : 0;
   float l[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) l[r] = 0.f;
-  if (key < R) sm.m[x][key] = sm.mz[x][key] = -INFINITY;
-  // the key's exponents, one tile of the side ahead, and its page, two
+  if (key < R) sm.m[key] = sm.mz[key] = -INFINITY;
+  // the key's exponents, one tile ahead, and its page, two
   const int* row = p.table + static_cast<long long>(en.s) * p.max_pages;
   auto page_at = [&](int j) {
     const int k = j * kRows + key;
@@ -386,18 +391,17 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>&
     const long long at = page * p.scale_page + (en.h << p.page_shift) + ((j * kRows + key) & ((1 << p.page_shift) - 1));
     return make_uint2(load_byte_if(p.K_scale + at, there, 127u), load_byte_if(p.V_scale + at, there, 127u));
   };
-  const int first = en.t0 + x;
+  const int first = en.t0;
   uint2 ex = exponents_at(first, page_at(first));
-  int page = page_at(first + 2);
-  // (The rows of the next entry but one come after this side has left this one: its phase cannot be missed.  A side without a
-  // tile needs none.)
-  if (first < en.t1) st.ok = st.ok && attn_wait_warp(sm, &sm.qfull[st.qn & 1], (st.qn >> 1) & 1, p.status);
+  int page = page_at(first + 1);
+  // (The rows of the next entry but one come after this one's are done with: a phase cannot be missed.)
+  st.ok = st.ok && attn_wait_warp(sm, &sm.qfull[st.qn & 1], (st.qn >> 1) & 1, p.status);
   const float* const qscale = sm.qscale[st.qn & 1];
-  group_sync(x);  // (the maxima are set)
-  for (int j = first; j < en.t1; j += 2) {
-    const uint2 next = exponents_at(j + 2, page);
-    page = page_at(j + 4);
-    st.ok = st.ok && attn_wait_warp(sm, &sm.sfull[x], st.sph, p.status);
+  group_sync(0);  // (the maxima are set)
+  for (int j = first; j < en.t1; ++j) {
+    const uint2 next = exponents_at(j + 1, page);
+    page = page_at(j + 2);
+    st.ok = st.ok && attn_wait_warp(sm, &sm.sfull, st.sph, p.status);
     st.sph ^= 1;
     tc_fence_after();
     const float k2 = __uint_as_float(ex.x << 23), b = static_cast<float>(static_cast<int>(ex.y) - 127);
@@ -423,9 +427,9 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>&
       logits(g, y);
 #pragma unroll
       for (int r = 0; r < kRowGroup; ++r)
-        up |= y[r] > sm.m[x][g * kRowGroup + r] + kFewRaise || y[r] + b > sm.mz[x][g * kRowGroup + r] + kFewRaise;
+        up |= y[r] > sm.m[g * kRowGroup + r] + kFewRaise || y[r] + b > sm.mz[g * kRowGroup + r] + kFewRaise;
     }
-    if (group_any(x, up)) {
+    if (group_any(0, up)) {
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
         if (kGroups > 1) logits(g, y);
@@ -433,27 +437,30 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>&
         for (int r = 0; r < kRowGroup; ++r) {
           const float a = warp_max(y[r]), z = warp_max(y[r] + b);
           if (lane == 0) {
-            sm.red[x][0][warp][g * kRowGroup + r] = a;
-            sm.red[x][1][warp][g * kRowGroup + r] = z;
+            sm.red[0][warp][g * kRowGroup + r] = a;
+            sm.red[1][warp][g * kRowGroup + r] = z;
           }
         }
       }
-      group_sync(x);
+      group_sync(0);
       auto raised = [&](int i, int r) {
-        const float* top = &sm.red[x][i][0][r];
-        return fmaxf(fmaxf(fmaxf(top[0], top[kFewRows]), fmaxf(top[2 * kFewRows], top[3 * kFewRows])), i ? sm.mz[x][r] : sm.m[x][r]);
+        const float* top = &sm.red[i][0][r];
+        return fmaxf(fmaxf(fmaxf(top[0], top[M]), fmaxf(top[2 * M], top[3 * M])), i ? sm.mz[r] : sm.m[r]);
       };
+      if (j != first) {  // the output holds the tile before this one (the one before that since this one's scores were formed)
+        st.ok = st.ok && attn_wait_warp(sm, &sm.odone, (done + 1) & 1, p.status);
+        tc_fence_after();
+      }
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
         float f[kRowGroup];
 #pragma unroll
         for (int r = 0; r < kRowGroup; ++r) {
           const int q = g * kRowGroup + r;
-          l[q] *= ex2_approx(sm.m[x][q] - finite_or_0(raised(0, q)));
-          f[r] = ex2_approx(sm.mz[x][q] - finite_or_0(raised(1, q)));
+          l[q] *= ex2_approx(sm.m[q] - finite_or_0(raised(0, q)));
+          f[r] = ex2_approx(sm.mz[q] - finite_or_0(raised(1, q)));
         }
         if (j != first) {
-          // S of this tile is complete, so is O of the side's tile before it, and the next waits for us
           uint32_t o[kGroupCols];
           tmem_ld_cols<kGroupCols>(to + g * kGroupCols, o);
 #pragma unroll
@@ -467,15 +474,15 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>&
         mn = raised(0, key);
         zn = raised(1, key);
       }
-      group_sync(x);  // (everyone has read the old ones)
+      group_sync(0);  // (everyone has read the old ones)
       if (key < R) {
-        sm.m[x][key] = mn;
-        sm.mz[x][key] = zn;
+        sm.m[key] = mn;
+        sm.mz[key] = zn;
       }
-      group_sync(x);
+      group_sync(0);
     }
     // this key's byte of a column is in the column's 128
-    uint8_t* const pw = sm.p[x] + (key & 15);
+    uint8_t* const pw = sm.p[(j - first) & 1] + (key & 15);
     const int chunk = key >> 4;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
@@ -486,8 +493,8 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>&
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int q = g * kRowGroup + r + i;
-          l[q] += ex2_approx(y[r + i] - finite_or_0(sm.m[x][q]));
-          w[i] = ex2_approx(y[r + i] + b - (finite_or_0(sm.mz[x][q]) - kFewUp));
+          l[q] += ex2_approx(y[r + i] - finite_or_0(sm.m[q]));
+          w[i] = ex2_approx(y[r + i] + b - (finite_or_0(sm.mz[q]) - kFewUp));
         }
         uint32_t c[kQParts];
         parts2(w[0], w[1], c);
@@ -498,60 +505,49 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>&
         }
       }
     }
-    few_mend_v<D>(p, sm, en, j, st);
+    few_mend_v(p, sm, en, j, st);
     fence_proxy_async();
     tc_fence_before();
     __syncwarp();
-    mbar_arrive_elect(&sm.pfull[x]);
+    mbar_arrive_elect(&sm.pfull);
+    if (j + 1 < en.t1) ++done;
     ex = next;
   }
-  // ---- the rows' output: sums over the keys, then both sides' accumulators ----
-  group_sync(x);  // (the maxima's readers are done)
+  // ---- the rows' output ----
+  group_sync(0);  // (the maxima's readers are done)
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     float v = l[r];
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if (lane == 0) sm.red[x][0][warp][r] = v;
+    if (lane == 0) sm.red[0][warp][r] = v;
   }
-  group_sync(x);
-  if (key < R) sm.l[x][key] = (sm.red[x][0][0][key] + sm.red[x][0][1][key]) + (sm.red[x][0][2][key] + sm.red[x][0][3][key]);
-  if (first < en.t1) {  // (side 1 of a single tile has no accumulator)
-    st.ok = st.ok && attn_wait_warp(sm, &sm.ofull[x], st.oph, p.status);
-    st.oph ^= 1;
-  }
-  tc_fence_before();
-  __syncwarp();
-  mbar_arrive_elect(&sm.xfull);
-  st.ok = st.ok && attn_wait_warp(sm, &sm.xfull, st.xph, p.status);
+  st.ok = st.ok && attn_wait_warp(sm, &sm.ofull, st.oph, p.status);
+  st.oph ^= 1;
+  group_sync(0);
   tc_fence_after();
-  const bool both = en.t0 + 1 < en.t1, whole = en.pieces == 1;
-  // side x writes the rows r with r mod 2 = x; the thread's element is d = key
+  const bool whole = en.pieces == 1;
+  const int i0 = en.h * p.G;
+  // row r's element d = key
   auto emit = [&](int r, float o, float mm, float ll) {
-    const int i = r / p.G, head = en.h * p.G + r - i * p.G;
-    if (key < D)
-      *reinterpret_cast<uint16_t*>(p.out + static_cast<long long>(en.tok0 + i) * p.out_token +
-                                   static_cast<long long>(head) * p.out_head + key * 2) = static_cast<uint16_t>(pack2<kFp16>(o, 0.f));
-    if (p.lse && key == r) p.lse[static_cast<long long>(en.tok0 + i) * p.H_q + head] = lse_of(mm, ll);
+    const int i = r < p.G ? 0 : r / p.G;
+    const long long tok = en.tok0 + i, head = i0 + r - i * p.G;
+    if (key < D) *reinterpret_cast<uint16_t*>(p.out + tok * p.out_token + head * p.out_head + key * 2) = static_cast<uint16_t>(pack2<kFp16>(o, 0.f));
+    if (p.lse && key == r) p.lse[tok * p.H_q + head] = lse_of(mm, ll);
   };
-  const Records<D> mine = few_records<D>(p, blockIdx.x, en.first == static_cast<int>(blockIdx.x), x);
+  const Records<D> mine = few_record<D>(p, blockIdx.x, en.first == static_cast<int>(blockIdx.x));
 #pragma unroll
   for (int g = 0; g < kGroups; ++g) {
-    float a[kRowGroup], c[kRowGroup];
-    load_rows(tmem + lanes + few_o_col(0) + g * kGroupCols, a);
-    if (both) load_rows(tmem + lanes + few_o_col(1) + g * kGroupCols, c);
-#pragma unroll
+    float a[kRowGroup];
+    load_rows(to + g * kGroupCols, a);
+#pragma unroll 1
     for (int r = 0; r < kRowGroup; ++r) {
       const int q = g * kRowGroup + r;
-      if ((q & 1) != x || q >= rows) continue;
-      const float ma = sm.m[0][q], mb = both ? sm.m[1][q] : -INFINITY, mm = fmaxf(ma, mb), base = finite_or_0(mm);
-      const float ll = fmaf(sm.l[0][q], ex2_approx(ma - base), both ? sm.l[1][q] * ex2_approx(mb - base) : 0.f);
+      if (q >= rows) break;
+      const float* s = &sm.red[0][0][q];
+      const float mm = sm.m[q], ll = (s[0] + s[M]) + (s[2 * M] + s[3 * M]);
       // the accumulators are 2^kFewUp sum 2^(y + b - mz) B
-      float v = 0.f;
-      if (ll != 0.f) {
-        v = a[r] * ex2_approx(sm.mz[0][q] - kFewUp - base);
-        if (both) v = fmaf(c[r], ex2_approx(sm.mz[1][q] - kFewUp - base), v);
-      }
+      const float v = ll == 0.f ? 0.f : (r == 0 ? a[0] : r == 1 ? a[1] : r == 2 ? a[2] : a[3]) * ex2_approx(sm.mz[q] - kFewUp - finite_or_0(mm));
       if (whole) {
         emit(q, v * (ll == 0.f ? 0.f : 1.f / ll), mm, ll);
       } else {
@@ -561,56 +557,74 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D>&
     }
   }
   tc_fence_before();
-  __syncwarp();
-  mbar_arrive_elect(&sm.xfree);
-  if (!whole && arrived_last(p, sm, en, x, st.ok)) {
-    // row by row, kU records in flight
-    constexpr int kU = 16;
+  if (!whole && arrived_last(p, sm, en, 0, st.ok)) {
+    // a group's pieces in rounds of 32: their maxima and sums by a thread each, then the outputs, kU pieces of all rows in flight
+    constexpr int kRound = 32, kU = 8;
 #pragma unroll 1
-    for (int q = x; q < rows; q += 2) {
-      float mm = -INFINITY, ll = 0.f, oo = 0.f;
-#pragma unroll 1
-      for (int q0 = 0; q0 < en.pieces; q0 += kU) {
-        float2 z[kU];
-        float o[kU];
+    for (int g = 0; g < rows; g += kRowGroup) {
+      float mm[kRowGroup], ll[kRowGroup], oo[kRowGroup];
 #pragma unroll
-        for (int i = 0; i < kU; ++i) {
-          z[i] = make_float2(-INFINITY, 0.f);
-          o[i] = 0.f;
-          if (q0 + i < en.pieces) {
-            const Records<D> rec = few_records<D>(p, en.first + q0 + i, q0 + i == 0, x);
-            z[i] = __ldcg(few_ml(rec) + q);
-            if (key < D) o[i] = __ldcg(reinterpret_cast<const float*>(rec.at) + q * D + key);
+      for (int r = 0; r < kRowGroup; ++r) { mm[r] = -INFINITY; ll[r] = oo[r] = 0.f; }
+#pragma unroll 1
+      for (int c = 0; c < en.pieces; c += kRound) {
+        const int n = min(kRound, en.pieces - c);
+        float o[kU][kRowGroup];
+        auto fetch = [&](int k) {
+#pragma unroll
+          for (int i = 0; i < kU; ++i) {
+            const float* at = reinterpret_cast<const float*>(few_record<D>(p, en.first + c + k + i, c + k + i == 0).at) + g * D + key;
+#pragma unroll
+            for (int r = 0; r < kRowGroup; ++r) o[i][r] = k + i < n && g + r < rows && key < D ? __ldcg(at + r * D) : 0.f;
           }
-        }
-        float mn = mm;
+        };
+        fetch(0);
+        const int pr = key / kRowGroup, q = g + key % kRowGroup;
+        const float2 mine2 = pr < n && q < rows ? __ldcg(few_ml(few_record<D>(p, en.first + c + pr, c + pr == 0)) + q) : make_float2(-INFINITY, 0.f);
+        group_sync(0);  // (the last round's readers are done)
+        sm.ml[key] = mine2;
+        group_sync(0);
+        float bs[kRowGroup];
 #pragma unroll
-        for (int i = 0; i < kU; ++i) mn = fmaxf(mn, z[i].x);
-        const float bs = finite_or_0(mn), f0 = ex2_approx(mm - bs);
-        ll *= f0;
-        oo *= f0;
-#pragma unroll
-        for (int i = 0; i < kU; ++i) {
-          const float f = ex2_approx(z[i].x - bs);
-          ll = fmaf(z[i].y, f, ll);
-          oo = fmaf(o[i], f, oo);
+        for (int r = 0; r < kRowGroup; ++r) {
+          float mn = mm[r];
+#pragma unroll 8
+          for (int i = 0; i < n; ++i) mn = fmaxf(mn, sm.ml[i * kRowGroup + r].x);
+          bs[r] = finite_or_0(mn);
+          const float f = ex2_approx(mm[r] - bs[r]);
+          ll[r] *= f;
+          oo[r] *= f;
+          mm[r] = mn;
         }
-        mm = mn;
+#pragma unroll 1
+        for (int k = 0; k < n; k += kU) {
+#pragma unroll
+          for (int i = 0; i < kU; ++i) {
+            if (k + i >= n) break;
+#pragma unroll
+            for (int r = 0; r < kRowGroup; ++r) {
+              const float2 z = sm.ml[(k + i) * kRowGroup + r];
+              const float f = ex2_approx(z.x - bs[r]);
+              ll[r] = fmaf(z.y, f, ll[r]);
+              oo[r] = fmaf(o[i][r], f, oo[r]);
+            }
+          }
+          if (k + kU < n) fetch(k + kU);
+        }
       }
-      emit(q, ll == 0.f ? 0.f : oo * (1.f / ll), mm, ll);
+#pragma unroll
+      for (int r = 0; r < kRowGroup; ++r)
+        if (g + r < rows) emit(g + r, ll[r] == 0.f ? 0.f : oo[r] * (1.f / ll[r]), mm[r], ll[r]);
     }
   }
-  // both sides have read both accumulators and their maxima and sums before either goes on
-  st.ok = st.ok && attn_wait_warp(sm, &sm.xfree, st.xph, p.status);
-  st.xph ^= 1;
-  tc_fence_after();
+  group_sync(0);  // (maxima and sums have been read)
   ++st.qn;
 }
 
-template <int D, bool kFp16>
-__global__ void __launch_bounds__(kFewThreads, kFewCtas) q8_few_kernel(const __grid_constant__ PagedAttnParams p) {
+template <int D, bool kFp16, int M>
+__global__ void __launch_bounds__(kFewThreads, few_ctas(M)) q8_few_kernel(const __grid_constant__ PagedAttnParams p) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  using S = Q8Smem<D>;
+  using S = Q8Smem<D, M>;
+  constexpr int kTmem = 2 * S::kCols < 32 ? 32 : 2 * S::kCols;
   if (smem_u32(smem_raw) & 1023u) {  // the swizzles need 1024-byte aligned buffers
     if (threadIdx.x == 0) atomicOr(p.status, kStatusDevice);
     return;
@@ -618,23 +632,20 @@ __global__ void __launch_bounds__(kFewThreads, kFewCtas) q8_few_kernel(const __g
   S& sm = *reinterpret_cast<S*>(smem_raw);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&sm.sfull[i], 1);
-      mbar_init(&sm.pfull[i], 4);
-      mbar_init(&sm.ofull[i], 1);
-    }
     for (int i = 0; i < S::kStages; ++i) {
       mbar_init(&sm.full[i], 1);
       mbar_init(&sm.empty[i], 1);
     }
     for (int i = 0; i < kEntries; ++i) {
       mbar_init(&sm.efull[i], 1);
-      mbar_init(&sm.eempty[i], 11);  // the load, MMA and query warps and eight softmax warps
+      mbar_init(&sm.eempty[i], 7);  // the load, MMA and query warps and four softmax warps
     }
     for (int i = 0; i < 2; ++i) mbar_init(&sm.qfull[i], 1);
     mbar_init(&sm.qempty, 1);
-    mbar_init(&sm.xfull, 8);
-    mbar_init(&sm.xfree, 8);
+    mbar_init(&sm.sfull, 1);
+    mbar_init(&sm.pfull, 4);
+    mbar_init(&sm.odone, 1);
+    mbar_init(&sm.ofull, 1);
     mbar_init(&sm.done, 1);
     sm.abort_flag = 0;
     fence_barrier_init();
@@ -645,7 +656,7 @@ __global__ void __launch_bounds__(kFewThreads, kFewCtas) q8_few_kernel(const __g
       asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
   }
   if (warp == 1) {
-    tmem_alloc(&sm.tmem_slot, 4 * kFewCols);
+    tmem_alloc(&sm.tmem_slot, kTmem);
     tmem_relinquish();
   }
   pdl_wait();
@@ -656,20 +667,20 @@ __global__ void __launch_bounds__(kFewThreads, kFewCtas) q8_few_kernel(const __g
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sm.tmem_slot;
-  if (warp == 0) few_load_warp<D>(p, sm);
-  if (warp == 1) few_mma_warp<D>(p, sm, tmem);
+  if (warp == 0) few_load_warp(p, sm);
+  if (warp == 1) few_mma_warp(p, sm, tmem);
   if (warp == 2) deal<kFewMode>(p, sm, sh, true);
   if (warp == 3) split_queries<D, kFp16>(p, sm);
   if (warp >= 4) {
-    const int x = (warp - 4) >> 2;
     SideState st;
+    uint32_t done = 0;  // tiles but the last ones that have been handed over
     for (uint32_t e = 0;; ++e) {
       const Entry en = take(p, sm, e);
-      if (group_any(x, en.n == 0)) break;  // no more, or a warp's wait for the entry ran out
+      if (group_any(0, en.n == 0)) break;  // no more, or a warp's wait for the entry ran out
       const int rows = en.n * p.G;
-      if (rows <= 4) q8_few_rows<D, kFp16, 1>(p, sm, tmem, x, en, st);
-      else if (rows <= 8) q8_few_rows<D, kFp16, 2>(p, sm, tmem, x, en, st);
-      else q8_few_rows<D, kFp16, 4>(p, sm, tmem, x, en, st);
+      if (M == 4 || rows <= 4) q8_few_rows<D, kFp16, M, 1>(p, sm, tmem, en, st, done);
+      else if (M == 8 || rows <= 8) q8_few_rows<D, kFp16, M, M >= 8 ? 2 : 1>(p, sm, tmem, en, st, done);
+      else q8_few_rows<D, kFp16, M, M / kRowGroup>(p, sm, tmem, en, st, done);
       st.tiles += 2 * (en.t1 - en.t0);
     }
   }
@@ -678,13 +689,24 @@ __global__ void __launch_bounds__(kFewThreads, kFewCtas) q8_few_kernel(const __g
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem, 4 * kFewCols);
+    tmem_dealloc(tmem, kTmem);
   }
 }
 
-AttnFn few_fn(int d, bool fp16) {
-  if (d == 64) return fp16 ? q8_few_kernel<64, true> : q8_few_kernel<64, false>;
-  return fp16 ? q8_few_kernel<128, true> : q8_few_kernel<128, false>;
+struct FewKernel {
+  AttnFn fn;
+  size_t smem;
+  AttnReady* ready;
+};
+template <int D, bool kFp16, int M>
+FewKernel few_kernel() {
+  static AttnReady ready;
+  return {q8_few_kernel<D, kFp16, M>, sizeof(Q8Smem<D, M>), &ready};
+}
+template <int M>
+FewKernel few_kernel(int d, bool fp16) {
+  if (d == 64) return fp16 ? few_kernel<64, true, M>() : few_kernel<64, false, M>();
+  return fp16 ? few_kernel<128, true, M>() : few_kernel<128, false, M>();
 }
 
 // The maps of a cache's pages of codes.
@@ -704,19 +726,21 @@ bool q8_page_maps(const kvev_paged_q8_cache* cache, CUtensorMapSwizzle swizzle, 
   return true;
 }
 
+// Rows of a unit that the launch takes: one token's where the batch has no more rows than requests, else up to 16.  (What has
+// more is left to the other kernel.)
+int few_rows_of(int G, int B, int T) { return T > B || G > 8 ? kFewRows : rows_held(G); }
+
 // The requests of few rows; p but for the maps of the pages.
-int few_launch(PagedAttnParams p, const kvev_paged_q8_cache* cache, cudaStream_t stream) {
+int few_launch(PagedAttnParams p, const kvev_paged_q8_cache* cache, int M, cudaStream_t stream) {
   const int d = cache->d;
   const bool fp16 = cache->dtype == KVEV_FP16;
-  const size_t smem = d == 64 ? sizeof(Q8Smem<64>) : sizeof(Q8Smem<128>);
+  const FewKernel k = M == 4 ? few_kernel<4>(d, fp16) : M == 8 ? few_kernel<8>(d, fp16) : few_kernel<16>(d, fp16);
   int grid = 0;
-  const AttnFn fn = few_fn(d, fp16);
-  static AttnReady ready[4];
-  const int rc = ready_kernel(ready[(d == 64 ? 0 : 2) + (fp16 ? 1 : 0)], fn, smem, kFewThreads, 0, &grid);
+  const int rc = ready_kernel(*k.ready, k.fn, k.smem, kFewThreads, 0, &grid);
   if (rc != KVEV_OK) return rc;
   if (!q8_page_maps(cache, d == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, &p)) return KVEV_ECUDA;
-  static_assert(2 * kFewCtas * kMaxCtas * sizeof(int) <= KVEV_PAGED_SYNC_BYTES, "arrival counts");
-  return launch_overlapped(fn, p, kFewCtas * grid, kFewThreads, smem, stream) == cudaSuccess ? KVEV_OK : KVEV_ECUDA;
+  static_assert(2 * few_ctas(4) * kMaxCtas * sizeof(int) <= KVEV_PAGED_SYNC_BYTES, "arrival counts");
+  return launch_overlapped(k.fn, p, few_ctas(M) * grid, kFewThreads, k.smem, stream) == cudaSuccess ? KVEV_OK : KVEV_ECUDA;
 }
 
 }  // namespace
