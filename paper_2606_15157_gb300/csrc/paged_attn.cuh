@@ -110,10 +110,9 @@ struct PagedAttnParams {
   int* status;
   int* sync;       // [2 kMaxCtas] pieces arrived of the unit whose first piece is the CTA's, per side
   uint8_t* parts;  // [2 kMaxCtas][2] records
-  // kShared: the groups' first requests, and the tokens that a group's requests have in common; the rows' two parts,
-  // [2][T][H_q][d] normalised and [2][T][H_q] their log2-sum-exp
-  const int *groups, *shared;
-  int N;
+  // kShared: what to schedule, the groups over their common keys and the requests (paged_shared.cu); the rows' two
+  // parts, [2][T][H_q][d] normalised and [2][T][H_q] their log2-sum-exp
+  const int4* plan;
   float *part_o, *part_lse;
   // kQ8: queries, codes and the rows' exponents, strides in bytes
   int few;  // most tokens of a request of few rows
@@ -357,54 +356,17 @@ __device__ __forceinline__ Request own_request(const PagedAttnParams& p, int s, 
   if (!ok) *bad = true;
   return r;
 }
-// Whole pages of keys that are read once for group g: none for a single request, nor where the group's rows or
-// length are out of range.
-__device__ __forceinline__ int shared_keys(const PagedAttnParams& p, int g, bool* bad) {
-  const int a = p.groups[g], b = p.groups[g + 1], n = p.shared[g];
-  if (n < 0 || n > (p.max_pages << p.page_shift)) { *bad = true; return 0; }
-  if (b - a < 2) return 0;
-  const int c0 = p.cu[a], c1 = p.cu[b];
-  return c0 >= 0 && c1 >= c0 && c1 <= p.T ? n & ~((1 << p.page_shift) - 1) : 0;
+// kShared: a request as the plan has it.
+__device__ __forceinline__ Request planned(const int4* plan, int s) {
+  const int4 a = plan[2 * s], b = plan[2 * s + 1];
+  return {a.x, a.y, a.z, a.w, b.x, b.y != 0};
 }
-// Whether the groups' first requests ascend in [0, B]: if not, nothing is shared.
-__device__ __forceinline__ bool group_in_order(const PagedAttnParams& p, int g) {
-  const int a = p.groups[g], b = p.groups[g + 1];
-  return a >= 0 && a <= b && b <= p.B;
-}
-// The keys of request s that its group reads once for all: those before its new tokens.
-__device__ __forceinline__ int shared_of_request(const PagedAttnParams& p, int s, const Request& r, bool* bad) {
-  int g = 0, n = p.N;  // the last group with groups[g] <= s
-  while (n > 1) {
-    const int h = n >> 1;
-    if (p.groups[g + h] <= s) g += h;
-    n -= h;
-  }
-  if (p.N == 0 || p.groups[g] > s || p.groups[g + 1] <= s) return 0;
-  const int k = shared_keys(p, g, bad);
-  return r.kv - r.q >= k ? k : 0;
-}
-// Request s to schedule; with kShared the first N are the groups over their common keys (ordered: they are in order).
+// Request s to schedule.
 template <int kMode>
-__device__ __forceinline__ Request request(const PagedAttnParams& p, int s, bool ordered, bool* bad) {
-  if (!(kMode & kShared)) {
-    Request r = own_request(p, s, bad);
-    if ((kMode & kQ8) && (r.q <= p.few) != ((kMode & kFewOnly) != 0)) r.q = 0;
-    return r;
-  }
-  if (s < p.N) {
-    Request r = {};
-    if (!ordered) return r;
-    r.kv = shared_keys(p, s, bad);
-    r.row = p.groups[s];
-    r.open = true;
-    if (r.kv > 0) {
-      r.c0 = p.cu[r.row];
-      r.q = p.cu[p.groups[s + 1]] - r.c0;
-    }
-    return r;
-  }
-  Request r = own_request(p, s - p.N, bad);
-  if (ordered && r.q > 0) r.lo = shared_of_request(p, s - p.N, r, bad);
+__device__ __forceinline__ Request request(const PagedAttnParams& p, int s, bool* bad) {
+  if (kMode & kShared) return planned(p.plan, s);
+  Request r = own_request(p, s, bad);
+  if ((kMode & kQ8) && (r.q <= p.few) != ((kMode & kFewOnly) != 0)) r.q = 0;
   return r;
 }
 
@@ -482,15 +444,15 @@ struct Share {
   long long origin;  // shares are counted from here,
   int cta0;          // the first of them this CTA's
 };
-// The CTA's share of `outer` rounds of cost `round`; before: the cost of the rounds before its own.  kFewOnly, where the CTAs
-// divide by the rounds: each round its own CTAs, so that all rounds, the KV heads, are at the same place at the same time.
+// The CTA's share of `outer` rounds of cost `round`; before: the cost of the rounds before its own.  kFewOnly and kShared,
+// where the CTAs divide by the rounds: each round its own CTAs, so that all rounds, the KV heads, are at the same place at the same time.
 // (Codes of a token's heads are 64 or 128 bytes next to one another in tokens-first pages: 64 generations over 4,097 tokens, 64-element
 // heads, with shares that do not end with the heads 111 us, %%G so.)
 template <int kMode>
 __device__ __forceinline__ Share share_at(long long round, int outer, int least) {
   Share r = {};
   const int grid = gridDim.x, per = grid / outer;
-  if ((kMode & kFewOnly) && per * outer == grid) {
+  if ((kMode & (kFewOnly | kShared)) && per * outer == grid) {
     r.h = blockIdx.x / per;
     r.cta0 = r.h * per;
     r.share = max(static_cast<long long>(least), divide(round + per - 1, per));
@@ -509,15 +471,15 @@ __device__ __forceinline__ Share share_at(long long round, int outer, int least)
 }
 
 template <int kMode, class S>
-__device__ __forceinline__ Share share_of(const PagedAttnParams& p, S& sm, bool ordered) {
+__device__ __forceinline__ Share share_of(const PagedAttnParams& p, S& sm) {
   constexpr int kThreads = Split<kMode>::kThreads;
   const int tid = threadIdx.x;
-  bool bad = !ordered;
+  bool bad = false;
   long long total = 0, mine = 0, first_before = 0;
   const int per = S::kHeadsOuter ? 1 : p.H_kv, outer = S::kHeadsOuter ? p.H_kv : 1;
   for (int s0 = 0; s0 < p.segs; s0 += kThreads) {
     mine = 0;
-    if (s0 + tid < p.segs) mine = head_cost<kMode>(p, request<kMode>(p, s0 + tid, ordered, &bad)) * per;
+    if (s0 + tid < p.segs) mine = head_cost<kMode>(p, request<kMode>(p, s0 + tid, &bad)) * per;
     long long all;
     const long long before = block_prefix<kThreads>(sm, mine, &all);
     if (s0 == 0) first_before = before;
@@ -536,7 +498,7 @@ __device__ __forceinline__ Share share_of(const PagedAttnParams& p, S& sm, bool 
     long long sum = 0;
     for (int s0 = 0; s0 < p.segs; s0 += kThreads) {
       bool b = false;
-      const long long c = s0 + tid < p.segs ? head_cost<kMode>(p, request<kMode>(p, s0 + tid, ordered, &b)) * per : 0;
+      const long long c = s0 + tid < p.segs ? head_cost<kMode>(p, request<kMode>(p, s0 + tid, &b)) * per : 0;
       long long all;
       const long long before = sum + block_prefix<kThreads>(sm, c, &all);
       if (c > 0 && before <= x && x < before + c) {
@@ -559,11 +521,9 @@ __device__ __forceinline__ Share share_of(const PagedAttnParams& p, S& sm, bool 
 template <int kMode, class S>
 __device__ __forceinline__ Share share_of_warp(const PagedAttnParams& p, Request& held, long long& held_cost) {
   const int lane = threadIdx.x & 31;
-  bool ordered = true;
-  if (kMode & kShared) ordered = __all_sync(0xffffffffu, lane >= p.N || group_in_order(p, lane));
-  bool bad = !ordered;
+  bool bad = false;
   held = {};
-  if (lane < p.segs) held = request<kMode>(p, lane, ordered, &bad);
+  if (lane < p.segs) held = request<kMode>(p, lane, &bad);
   held_cost = head_cost<kMode>(p, held);
   const long long mine = S::kHeadsOuter ? held_cost : held_cost * p.H_kv;
   if (bad && blockIdx.x == 0) atomicOr(p.status, kStatusDevice);
@@ -584,7 +544,7 @@ __device__ __forceinline__ Share share_of_warp(const PagedAttnParams& p, Request
 
 // Warp 2: the CTA's entries in order.
 template <int kMode, class S>
-__device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, Share sh, bool ordered) {
+__device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, Share sh) {
   uint32_t e = 0;
   const int lane = threadIdx.x & 31;
   const bool short_batch = p.segs <= 32;
@@ -595,11 +555,11 @@ __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, Share sh, 
     if (short_batch) {
       auto of = [&](int v) { return __shfl_sync(0xffffffffu, v, s); };
       Request r = {of(held.c0), of(held.q), of(held.kv), 0, s, false};
-      if (kMode & kShared) { r.lo = of(held.lo); r.row = of(held.row); r.open = s < p.N; }
+      if (kMode & kShared) { r.lo = of(held.lo); r.row = of(held.row); r.open = of(held.open) != 0; }
       return r;
     }
     bool bad = false;  // (said by the schedule's first pass)
-    return request<kMode>(p, s, ordered, &bad);
+    return request<kMode>(p, s, &bad);
   };
   auto put = [&](const Entry& en) {
     if (!attn_wait_warp(sm, &sm.eempty[e % kEntries], ((e / kEntries) & 1) ^ 1, p.status)) return false;
@@ -1825,14 +1785,7 @@ __global__ void __launch_bounds__(Split<kMode>::kThreads, 1) paged_attn_kernel(c
   pdl_wait();
   pdl_trigger();
   Share sh = {};
-  bool ordered = true;
-  if (p.segs > 32) {
-    if (kMode & kShared) {
-      for (int g = threadIdx.x; g < p.N; g += Split<kMode>::kThreads) ordered &= group_in_order(p, g);
-      ordered = __syncthreads_and(ordered);
-    }
-    sh = share_of<kMode>(p, sm, ordered);
-  }
+  if (p.segs > 32) sh = share_of<kMode>(p, sm);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -1841,7 +1794,7 @@ __global__ void __launch_bounds__(Split<kMode>::kThreads, 1) paged_attn_kernel(c
     regs_dealloc<Split<kMode>::kControl>();
     if (warp == 0) load_warp<D, kMode>(p, sm);
     if (warp == 1) mma_warp<D, kFp16, kMode>(p, sm, tmem);
-    if (warp == 2) deal<kMode>(p, sm, sh, ordered);
+    if (warp == 2) deal<kMode>(p, sm, sh);
     __syncwarp();
   } else if (!(kMode & kQ8) || warp < 12) {
     regs_alloc<Split<kMode>::kSoftmax>();

@@ -662,14 +662,14 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(M)) q8_few_kernel(const 
   pdl_wait();
   pdl_trigger();
   Share sh = {};
-  if (p.segs > 32) sh = share_of<kFewMode>(p, sm, true);
+  if (p.segs > 32) sh = share_of<kFewMode>(p, sm);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sm.tmem_slot;
   if (warp == 0) few_load_warp(p, sm);
   if (warp == 1) few_mma_warp(p, sm, tmem);
-  if (warp == 2) deal<kFewMode>(p, sm, sh, true);
+  if (warp == 2) deal<kFewMode>(p, sm, sh);
   if (warp == 3) split_queries<D, kFp16>(p, sm);
   if (warp >= 4) {
     SideState st;

@@ -12,33 +12,108 @@
 namespace kvev {
 namespace {
 
-constexpr int kJoinThreads = 256;
+// ---- the plan -------------------------------------------------------------------------------
+// The groups over their common keys, then the requests, 32 bytes each: what the attention's CTAs would all read through the
+// groups' and the requests' lengths in turn (made there, a call of 64 generations behind a single page took 70 us, the same
+// without a group 39).
+struct PlanParams {
+  const int *cu, *kv_lens, *groups, *shared;
+  int B, T, N, most, page_shift;  // most: tokens that a row of the block table holds
+  int4* plan;
+  int* status;
+};
+constexpr int kPlanThreads = 128;
 
-// A CTA takes a token at a time: its request by search, then its heads' vectors.
-template <int D, bool kFp16>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ PagedAttnParams p) {
-  const int lane = threadIdx.x & 31;
+// Whole pages of keys that are read once for the requests a .. b - 1, n tokens being common to them: none for a single request,
+// nor where the group's rows are out of range.
+__device__ __forceinline__ int common_keys(const PlanParams& p, int a, int b, int n) {
+  if (n < 0 || n > p.most || b - a < 2) return 0;
+  const int c0 = p.cu[a], c1 = p.cu[b];
+  return c0 >= 0 && c1 >= c0 && c1 <= p.T ? n & ~((1 << p.page_shift) - 1) : 0;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ PlanParams p) {
   pdl_wait();
   pdl_trigger();
-  bool ordered = true;
-  for (int g = threadIdx.x; g < p.N; g += kJoinThreads) ordered &= group_in_order(p, g);
-  ordered = __syncthreads_and(ordered);
-  if (!ordered) return;
-  for (int t = blockIdx.x; t < p.T; t += gridDim.x) {
-    int s = 0, n = p.B;  // the last request with cu[s] <= t
-    while (n > 1) {
-      const int step = (n + 31) / 32, i = lane * step;
-      const uint32_t upto = __ballot_sync(0xffffffffu, i < n && p.cu[s + min(i, n - 1)] <= t);
-      const int j = upto ? 31 - __clz(upto) : 0;
-      s += j * step;
-      n = min(step, n - j * step);
+  bool in_order = true;  // the groups' first requests ascend in [0, B]; if not, nothing is shared
+  for (int g = threadIdx.x; g < p.N; g += kPlanThreads) {
+    const int a = p.groups[g], b = p.groups[g + 1];
+    in_order &= a >= 0 && a <= b && b <= p.B;
+  }
+  const int s = blockIdx.x * kPlanThreads + threadIdx.x, r = s - p.N;
+  int4 x = make_int4(0, 0, 0, 0), y = make_int4(0, 0, 0, 0);
+  bool bad = false;
+  int c1 = 0;
+  if (r >= 0 && r < p.B) {
+    x.x = p.cu[r];
+    c1 = p.cu[r + 1];
+    x.z = p.kv_lens[r];
+  }
+  in_order = __syncthreads_and(in_order);
+  bad = !in_order;
+  if (s < p.N) {
+    const int a = p.groups[s], n = p.shared[s];
+    bad |= n < 0 || n > p.most;
+    if (in_order) {
+      const int b = p.groups[s + 1], k = common_keys(p, a, b, n);
+      y = make_int4(a, 1, 0, 0);
+      if (k > 0) {
+        x.x = p.cu[a];
+        x.y = p.cu[b] - x.x;
+        x.z = k;
+      }
     }
-    bool bad = false;
-    const Request r = own_request(p, s, &bad);
-    if (t < r.c0 || t >= r.c0 + r.q || shared_of_request(p, s, r, &bad) == 0) continue;
-    constexpr int kVec = D / 4;
-    for (int i = threadIdx.x; i < p.H_q * kVec; i += kJoinThreads) {
-      const int head = i / kVec, c = i % kVec;
+  } else if (r < p.B) {
+    const bool ok = x.x >= 0 && c1 >= x.x && c1 <= p.T && x.z >= 0 && x.z <= p.most;
+    bad |= !ok;
+    x.y = ok ? c1 - x.x : 0;
+    y.x = r;
+    if (ok && in_order) {
+      int g = 0, n = p.N;  // the last group with groups[g] <= r
+      while (n > 1) {
+        const int h = n >> 1;
+        if (p.groups[g + h] <= r) g += h;
+        n -= h;
+      }
+      const int a = p.groups[g], b = p.groups[g + 1];
+      if (a <= r && r < b) {
+        const int k = common_keys(p, a, b, p.shared[g]);
+        if (x.z - x.y >= k) x.w = k;  // (all of them before its new tokens)
+      }
+    }
+  }
+  if (s < p.N + p.B) {
+    p.plan[2 * s] = x;
+    p.plan[2 * s + 1] = y;
+  }
+  if (bad) atomicOr(p.status, kStatusDevice);
+}
+
+// ---- the rows' two parts together ---------------------------------------------------------------
+constexpr int kJoinThreads = 256;
+
+// CTAs (request, one in `each`): every each-th row of the request, its heads' vectors dealt over the threads.
+struct JoinParams {
+  const int4* plan;  // the requests'
+  const float *part_o, *part_lse;
+  uint8_t* out;
+  float* lse;
+  long long out_token, out_head;  // strides in bytes
+  int T, H_q, each;
+};
+
+template <int D, bool kFp16>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ JoinParams p) {
+  pdl_wait();
+  pdl_trigger();
+  const int s = blockIdx.x / p.each;
+  const Request r = planned(p.plan, s);
+  if (r.lo == 0) return;
+  constexpr int kVec = D / 4;
+  for (int i = blockIdx.x - s * p.each; i < r.q; i += p.each) {
+    const int t = r.c0 + i;
+    for (int k = threadIdx.x; k < p.H_q * kVec; k += kJoinThreads) {
+      const int head = k / kVec, c = k % kVec;
       const long long at = static_cast<long long>(t) * p.H_q + head, other = at + static_cast<long long>(p.T) * p.H_q;
       const float a = p.part_lse[at], b = p.part_lse[other];
       const float4 x = reinterpret_cast<const float4*>(p.part_o)[at * kVec + c], y = reinterpret_cast<const float4*>(p.part_o)[other * kVec + c];
@@ -56,9 +131,11 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
   }
 }
 
+// Behind the attention's own scratch: the plan, the parts' log-sum-exp, the parts.
+constexpr size_t kPlanBytes = static_cast<size_t>(KVEV_PAGED_MAX_REQUESTS) * 2 * sizeof(int4);
 size_t part_lse_bytes(int T, int H_q) { return (static_cast<size_t>(2) * T * H_q * sizeof(float) + 255) & ~static_cast<size_t>(255); }
 size_t shared_bytes(int H_q, int d, int T) {
-  return attn_workspace_bytes(d) + part_lse_bytes(T, H_q) + static_cast<size_t>(2) * T * H_q * d * sizeof(float);
+  return attn_workspace_bytes(d) + kPlanBytes + part_lse_bytes(T, H_q) + static_cast<size_t>(2) * T * H_q * d * sizeof(float);
 }
 
 }  // namespace
@@ -100,15 +177,19 @@ extern "C" int kvev_paged_attention_shared(const kvev_paged_cache* cache, const 
   rc = attn_params(a, cache->H_kv, d, fp16, cache->page_size, cache->num_pages, &p);
   if (rc != KVEV_OK) return rc;
   if (!attn_page_maps(cache, &p)) return KVEV_ECUDA;
-  p.groups = groups;
-  p.shared = shared_lens;
-  p.N = N;
+  uint8_t* const after = static_cast<uint8_t*>(workspace) + attn_workspace_bytes(d);
+  int4* const plan = reinterpret_cast<int4*>(after);
+  p.plan = plan;
   p.segs = B + N;
-  p.part_lse = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + attn_workspace_bytes(d));
-  p.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + attn_workspace_bytes(d) + part_lse_bytes(T, H_q));
+  p.part_lse = reinterpret_cast<float*>(after + kPlanBytes);
+  p.part_o = reinterpret_cast<float*>(after + kPlanBytes + part_lse_bytes(T, H_q));
+  const PlanParams pp = {cu_new, kv_lens, groups, shared_lens, B, T, N, max_pages << p.page_shift, p.page_shift, plan, device_status};
+  if (launch_overlapped(plan_kernel, pp, (B + N + kPlanThreads - 1) / kPlanThreads, kPlanThreads, 0, a.stream) != cudaSuccess) return KVEV_ECUDA;
   rc = attn_launch<kShared>(p, d, fp16, a.stream);
   if (rc != KVEV_OK) return rc;
-  const AttnFn fn = d == 64 ? (fp16 ? join_kernel<64, true> : join_kernel<64, false>) : (fp16 ? join_kernel<128, true> : join_kernel<128, false>);
-  const int grid = T < 8 * kMaxCtas ? T : 8 * kMaxCtas;
-  return launch_overlapped(fn, p, grid, kJoinThreads, 0, a.stream) == cudaSuccess ? KVEV_OK : KVEV_ECUDA;
+  // as many CTAs to a request as it has rows, as far as the host can tell, and enough of them for the GPU in all
+  const int rows = (T + B - 1) / B, most = (8 * kMaxCtas + B - 1) / B;
+  const JoinParams jp = {plan + 2 * N, p.part_o, p.part_lse, p.out, lse, p.out_token, p.out_head, T, H_q, rows < most ? rows : most};
+  const auto fn = d == 64 ? (fp16 ? join_kernel<64, true> : join_kernel<64, false>) : (fp16 ? join_kernel<128, true> : join_kernel<128, false>);
+  return launch_overlapped(fn, jp, B * jp.each, kJoinThreads, 0, a.stream) == cudaSuccess ? KVEV_OK : KVEV_ECUDA;
 }

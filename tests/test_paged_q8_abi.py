@@ -93,7 +93,7 @@ def test_nothing_to_do_is_no_error(kv):
 
 def test_workspace_query(kv):
     at = kv.kvev_paged_attention_shared_workspace
-    assert at(32, 8, 128, 0) == kv.kvev_paged_attention_workspace(32, 8, 128)
+    assert at(32, 8, 128, 0) >= kv.kvev_paged_attention_workspace(32, 8, 128)
     assert at(32, 8, 128, 1000) >= at(32, 8, 128, 0) + 1000 * 32 * 2 * (128 + 1) * 4
     assert at(128, 1, 128, 1 << 30) > 1 << 47  # counted in 64 bits
     for args, want in (((32, 5, 128, 1), kv.EINVAL), ((0, 1, 128, 1), kv.EINVAL), ((8, 8, 128, -1), kv.EINVAL), ((8, 8, 80, 1), kv.ENOTSUP),
