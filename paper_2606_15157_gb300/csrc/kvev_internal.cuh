@@ -571,10 +571,10 @@ namespace kvev {
 // A launch of `fn` that may overlap the end of the kernels before it on the
 // stream (fn calls pdl_wait), in clusters of `cluster` CTAs when that is not 1.
 template <class P>
-cudaError_t launch_overlapped(void (*fn)(const P), const P& p, int grid, int threads, size_t smem, cudaStream_t s,
+cudaError_t launch_overlapped(void (*fn)(const P), const P& p, dim3 grid, int threads, size_t smem, cudaStream_t s,
                               int cluster = 1) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;

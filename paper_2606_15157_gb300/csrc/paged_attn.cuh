@@ -113,6 +113,7 @@ struct PagedAttnParams {
   // kShared: what to schedule, the groups over their common keys and the requests (paged_shared.cu); the rows' two
   // parts, [2][T][H_q][d] normalised and [2][T][H_q] their log2-sum-exp
   const int4* plan;
+  int2* units;  // [H_kv][T] of a group's unit, at its first token: CTA of the first piece, pieces
   float *part_o, *part_lse;
   // kQ8: queries, codes and the rows' exponents, strides in bytes
   int few;  // most tokens of a request of few rows
@@ -1150,6 +1151,16 @@ __device__ __forceinline__ float lse2_of(float m, float l) {  // log2
 }
 __device__ __forceinline__ float finite_or_0(float m) { return m == -INFINITY ? 0.f : m; }
 
+// A cut unit of a group: its pieces stay as they are, and are put together row by row with the requests' own parts, on all
+// SMs (merged here, by a CTA a unit, 64 generations behind 8K 73 us, %%H so).  Its first piece says where they are.
+template <int kMode>
+__device__ __forceinline__ bool left_to_join(const PagedAttnParams& p, const Entry& en, int x) {
+  if (!(kMode & kShared) || en.part != 0) return false;
+  if (x == 0 && (threadIdx.x & 127) == 0 && en.first == static_cast<int>(blockIdx.x))
+    p.units[static_cast<long long>(en.h) * p.T + en.tok0] = make_int2(en.first, en.pieces);
+  return true;
+}
+
 // ---- up to 16 rows: a thread per key ----
 // S^T has the tile's keys on the lanes and the rows in the columns, so a thread forms
 // its key's weights of R rows; they go to shared memory as the B operand of
@@ -1307,6 +1318,7 @@ __device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D, k
     if (p.lse && key == r) p.lse[static_cast<long long>(en.tok0 + i) * p.H_q + head] = lse_of(mm - kUp, ll);
   };
   if (whole) {
+    left_to_join<kMode>(p, en, x);
 #pragma unroll
     for (int r = 0; r < R; ++r)
       if ((r & 1) == x && r < rows) emit(r, v[r] * (l[r] == 0.f ? 0.f : 1.f / l[r]), m[r], l[r]);
@@ -1318,7 +1330,7 @@ __device__ __forceinline__ void few_rows(const PagedAttnParams& p, AttnSmem<D, k
         if (key < D) __stcg(reinterpret_cast<float*>(mine.at) + r * D + key, v[r]);
         if (key == r) __stcg(mine.ml() + r, make_float2(m[r], l[r]));
       }
-    if (arrived_last(p, sm, en, x, st.ok)) {
+    if (!left_to_join<kMode>(p, en, x) && arrived_last(p, sm, en, x, st.ok)) {
       // the side's rows together, 32 records in flight
       constexpr int kR = R / 2, kU = 32 / kR;
       float mm[kR], ll[kR], oo[kR];
@@ -1587,7 +1599,7 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D, 
     long long at[4];  // of the group's rows; -1: no row
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const long long mine4 = valid ? static_cast<long long>(en.tok0 + i) * p.out_token + static_cast<long long>(head) * p.out_head : -1;
+      const long long mine4 = !valid ? -1 : part ? part_at * D : static_cast<long long>(en.tok0 + i) * p.out_token + static_cast<long long>(head) * p.out_head;
       at[k] = __shfl_sync(0xffffffffu, mine4, (lane & 28) + k);
     }
 #pragma unroll 1
@@ -1609,10 +1621,17 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D, 
         for (int k = 0; k < 32; ++k) v[k] = l == 0.f ? 0.f : v[k];
       }
       if (part && whole) {
-        if (valid) {
 #pragma unroll
-          for (int k = 0; k < 32; k += 4)
-            *reinterpret_cast<float4*>(p.part_o + part_at * D + q + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+        for (int o4 = 0; o4 < 32; o4 += 16) {  // 16 columns of the group's rows
+          uint4 w[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            w[k] = make_uint4(__float_as_uint(v[o4 + 4 * k]), __float_as_uint(v[o4 + 4 * k + 1]), __float_as_uint(v[o4 + 4 * k + 2]),
+                              __float_as_uint(v[o4 + 4 * k + 3]));
+          transpose4(w, q4);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (at[k] >= 0) *reinterpret_cast<uint4*>(p.part_o + at[k] + q + o4 + 4 * q4) = w[k];
         }
       } else if (whole) {
         uint4 w[4];
@@ -1640,6 +1659,7 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D, 
     mbar_arrive_elect(&sm.xfree);
   }
   if (whole) {
+    left_to_join<kMode>(p, en, x);
     if (part) {
       if (valid && (!paired || x == 0)) p.part_lse[part_at] = lse2_of(m - kUp, l);
     } else if (p.lse && valid && (!paired || x == 0)) {
@@ -1647,7 +1667,7 @@ __device__ __forceinline__ void row_tiles(const PagedAttnParams& p, AttnSmem<D, 
     }
   } else {
     if (valid) __stcg(mine.ml() + r, make_float2(m, l));
-    if (arrived_last(p, sm, en, x, st.ok)) {
+    if (!left_to_join<kMode>(p, en, x) && arrived_last(p, sm, en, x, st.ok)) {
       // merge the unit's records in order: the row's maximum and sum, then 32 columns at a time
       if (valid) {
         float mm = -INFINITY, ll = 0.f;

@@ -13,7 +13,8 @@ namespace kvev {
 namespace {
 
 // ---- the plan -------------------------------------------------------------------------------
-// The groups over their common keys, then the requests, 32 bytes each: what the attention's CTAs would all read through the
+// The groups over their common keys, then the requests (first row, rows, keys, first key; row of the block table, whether a group,
+// the group's first row and the one after its last), 32 bytes each: what the attention's CTAs would all read through the
 // groups' and the requests' lengths in turn (made there, a call of 64 generations behind a single page took 70 us, the same
 // without a group 39).
 struct PlanParams {
@@ -78,7 +79,12 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
       const int a = p.groups[g], b = p.groups[g + 1];
       if (a <= r && r < b) {
         const int k = common_keys(p, a, b, p.shared[g]);
-        if (x.z - x.y >= k) x.w = k;  // (all of them before its new tokens)
+        // all of them before its new tokens, which are among the group's (where the counts do not ascend they may not be)
+        if (k > 0 && x.z - x.y >= k && x.x >= p.cu[a] && c1 <= p.cu[b]) {
+          x.w = k;
+          y.z = p.cu[a];
+          y.w = p.cu[b];
+        }
       }
     }
   }
@@ -92,50 +98,82 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
 // ---- the rows' two parts together ---------------------------------------------------------------
 constexpr int kJoinThreads = 256;
 
-// CTAs (request, one in `each`): every each-th row of the request, its heads' vectors dealt over the threads.
 struct JoinParams {
-  const int4* plan;  // the requests'
-  const float *part_o, *part_lse;
-  uint8_t* out;
-  float* lse;
-  long long out_token, out_head;  // strides in bytes
-  int T, H_q, each;
+  PagedAttnParams p;  // the attention's, but for the plan: the requests'
+  int each;
 };
 
+// CTAs (request, one in `each`; part of the heads): every each-th row of the request, its heads' vectors dealt over the threads.  A row's part over the
+// common keys is whole, or in the pieces of its unit as the attention left them.
 template <int D, bool kFp16>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ JoinParams p) {
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ JoinParams j) {
+  const PagedAttnParams& p = j.p;
+  constexpr float kUp = kFp16 ? 7.f : 0.f;  // (of the attention's weights)
+  constexpr int kVec = D / 4, kU = 8;
   pdl_wait();
   pdl_trigger();
-  const int s = blockIdx.x / p.each;
+  const int s = blockIdx.x / j.each;
   const Request r = planned(p.plan, s);
   if (r.lo == 0) return;
-  constexpr int kVec = D / 4;
-  for (int i = blockIdx.x - s * p.each; i < r.q; i += p.each) {
-    const int t = r.c0 + i;
-    for (int k = threadIdx.x; k < p.H_q * kVec; k += kJoinThreads) {
-      const int head = k / kVec, c = k % kVec;
-      const long long at = static_cast<long long>(t) * p.H_q + head, other = at + static_cast<long long>(p.T) * p.H_q;
-      const float a = p.part_lse[at], b = p.part_lse[other];
-      const float4 x = reinterpret_cast<const float4*>(p.part_o)[at * kVec + c], y = reinterpret_cast<const float4*>(p.part_o)[other * kVec + c];
-      const float m = finite_or_0(fmaxf(a, b));
-      float wa = ex2_approx(a - m), wb = ex2_approx(b - m);
-      const float sum = wa + wb, inv = sum == 0.f ? 0.f : 1.f / sum;
-      wa *= inv;
-      wb *= inv;
+  const int g0 = p.plan[2 * s + 1].z, g1 = p.plan[2 * s + 1].w;
+  for (int i = blockIdx.x - s * j.each; i < r.q; i += j.each) {
+    const int t = r.c0 + i, m = (t - g0) / (2 * p.P), tok0 = g0 + 2 * p.P * m, n = min(2 * p.P, g1 - tok0);
+    const int kind = n > p.P ? kFull : n * p.G > kFewRows ? kPaired : kFew;
+    for (int k = blockIdx.y * kJoinThreads + threadIdx.x; k < p.H_q * kVec; k += gridDim.y * kJoinThreads) {
+      // (a KV head's rows of a vector lie next to one another in a record)
+      const int h = k / (p.G * kVec), in = k - h * (p.G * kVec), c = in / p.G, head = h * p.G + in - c * p.G, row = (t - tok0) * p.G + in - c * p.G;
+      const int2 unit = p.units[static_cast<long long>(h) * p.T + tok0];
+      if (unit.x < 0 || unit.y < 1 || unit.x > kMaxCtas - unit.y) continue;  // (a wait of the attention ran out: nothing was left there)
+      const long long at = static_cast<long long>(t) * p.H_q + head, own = at + static_cast<long long>(p.T) * p.H_q;
+      float top = p.part_lse[own], sum = 1.f;
+      float4 o = reinterpret_cast<const float4*>(p.part_o)[own * kVec + c];
+      auto add = [&](float a, float l, const float4& x) {
+        const float mn = fmaxf(top, a), base = finite_or_0(mn), f = ex2_approx(top - base), w = ex2_approx(a - base);
+        sum = fmaf(sum, f, l * w);
+        o = make_float4(fmaf(o.x, f, x.x * w), fmaf(o.y, f, x.y * w), fmaf(o.z, f, x.z * w), fmaf(o.w, f, x.w * w));
+        top = mn;
+      };
+      if (unit.y == 1) {
+        add(p.part_lse[at], 1.f, reinterpret_cast<const float4*>(p.part_o)[at * kVec + c]);
+      } else {
+        // side, row and vector of the record
+        const int x = kind == kFull ? row >= p.P * p.G : kind == kPaired ? c >= kVec / 2 : row & 1;
+        const int rr = kind == kFull ? row - x * p.P * p.G : row, cc = kind == kPaired ? c - x * (kVec / 2) : c;
+        const int vec = kind == kFew ? rr * kVec + cc : cc * kRows + rr;
+#pragma unroll 1
+        for (int q0 = 0; q0 < unit.y; q0 += kU) {
+          float2 z[kU];
+          float4 v[kU];
+#pragma unroll
+          for (int q = 0; q < kU; ++q) {
+            z[q] = make_float2(-INFINITY, 0.f);
+            v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (q0 + q < unit.y) {
+              const Records<D> rec = records<D>(p, unit.x + q0 + q, q0 + q == 0, x);
+              z[q] = __ldcg(rec.ml() + rr);
+              v[q] = __ldcg(reinterpret_cast<const float4*>(rec.at) + vec);
+            }
+          }
+#pragma unroll
+          for (int q = 0; q < kU; ++q) add(z[q].x - kUp, z[q].y, v[q]);
+        }
+      }
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
       uint2 w;
-      w.x = pack2<kFp16>(fmaf(x.x, wa, y.x * wb), fmaf(x.y, wa, y.y * wb));
-      w.y = pack2<kFp16>(fmaf(x.z, wa, y.z * wb), fmaf(x.w, wa, y.w * wb));
+      w.x = pack2<kFp16>(o.x * inv, o.y * inv);
+      w.y = pack2<kFp16>(o.z * inv, o.w * inv);
       *reinterpret_cast<uint2*>(p.out + static_cast<long long>(t) * p.out_token + static_cast<long long>(head) * p.out_head + c * 8) = w;
-      if (p.lse && c == 0) p.lse[at] = lse_of(m, sum);
+      if (p.lse && c == 0) p.lse[at] = lse_of(top, sum);
     }
   }
 }
 
-// Behind the attention's own scratch: the plan, the parts' log-sum-exp, the parts.
+// Behind the attention's own scratch: the plan, where units are, the parts' log-sum-exp, the parts.
 constexpr size_t kPlanBytes = static_cast<size_t>(KVEV_PAGED_MAX_REQUESTS) * 2 * sizeof(int4);
 size_t part_lse_bytes(int T, int H_q) { return (static_cast<size_t>(2) * T * H_q * sizeof(float) + 255) & ~static_cast<size_t>(255); }
-size_t shared_bytes(int H_q, int d, int T) {
-  return attn_workspace_bytes(d) + kPlanBytes + part_lse_bytes(T, H_q) + static_cast<size_t>(2) * T * H_q * d * sizeof(float);
+size_t units_bytes(int T, int H_kv) { return (static_cast<size_t>(T) * H_kv * sizeof(int2) + 255) & ~static_cast<size_t>(255); }
+size_t shared_bytes(int H_q, int H_kv, int d, int T) {
+  return attn_workspace_bytes(d) + kPlanBytes + units_bytes(T, H_kv) + part_lse_bytes(T, H_q) + static_cast<size_t>(2) * T * H_q * d * sizeof(float);
 }
 
 }  // namespace
@@ -146,7 +184,7 @@ using namespace kvev;
 extern "C" int kvev_paged_attention_shared_workspace(int H_q, int H_kv, int d, int T, size_t* bytes) {
   if (!bytes || H_kv < 1 || H_q < 1 || H_q % H_kv || T < 0 || T > kMaxTokens) return KVEV_EINVAL;
   if ((d != 64 && d != 128) || H_q / H_kv > 128) return KVEV_ENOTSUP;
-  *bytes = shared_bytes(H_q, d, T);
+  *bytes = shared_bytes(H_q, H_kv, d, T);
   return KVEV_OK;
 }
 
@@ -166,7 +204,7 @@ extern "C" int kvev_paged_attention_shared(const kvev_paged_cache* cache, const 
   const AttnCall a = {q, q_token_stride, q_head_stride, cu_new, kv_lens, block_table, max_pages, B, T, H_q, scale, 0,
                       out, out_token_stride, out_head_stride, lse, workspace, device_status, static_cast<cudaStream_t>(stream)};
   const int d = cache->d;
-  const size_t need = T >= 0 && H_q > 0 ? shared_bytes(H_q, d, T) : 0;
+  const size_t need = T >= 0 && H_q > 0 ? shared_bytes(H_q, cache->H_kv, d, T) : 0;
   bool nothing = false;
   rc = attn_check(a, cache->H_kv, d, cache->page_size, workspace_bytes, need, &nothing);
   if (rc != KVEV_OK) return rc;
@@ -181,15 +219,21 @@ extern "C" int kvev_paged_attention_shared(const kvev_paged_cache* cache, const 
   int4* const plan = reinterpret_cast<int4*>(after);
   p.plan = plan;
   p.segs = B + N;
-  p.part_lse = reinterpret_cast<float*>(after + kPlanBytes);
-  p.part_o = reinterpret_cast<float*>(after + kPlanBytes + part_lse_bytes(T, H_q));
+  uint8_t* const parts = after + kPlanBytes + units_bytes(T, cache->H_kv);
+  p.units = reinterpret_cast<int2*>(after + kPlanBytes);
+  p.part_lse = reinterpret_cast<float*>(parts);
+  p.part_o = reinterpret_cast<float*>(parts + part_lse_bytes(T, H_q));
   const PlanParams pp = {cu_new, kv_lens, groups, shared_lens, B, T, N, max_pages << p.page_shift, p.page_shift, plan, device_status};
   if (launch_overlapped(plan_kernel, pp, (B + N + kPlanThreads - 1) / kPlanThreads, kPlanThreads, 0, a.stream) != cudaSuccess) return KVEV_ECUDA;
   rc = attn_launch<kShared>(p, d, fp16, a.stream);
   if (rc != KVEV_OK) return rc;
   // as many CTAs to a request as it has rows, as far as the host can tell, and enough of them for the GPU in all
   const int rows = (T + B - 1) / B, most = (8 * kMaxCtas + B - 1) / B;
-  const JoinParams jp = {plan + 2 * N, p.part_o, p.part_lse, p.out, lse, p.out_token, p.out_head, T, H_q, rows < most ? rows : most};
+  JoinParams jp = {p, rows < most ? rows : most};
+  jp.p.plan = plan + 2 * N;
+  const int vectors = H_q * (d / 4), split = (vectors + kJoinThreads - 1) / kJoinThreads, room = 8 * kMaxCtas / (B * jp.each);
   const auto fn = d == 64 ? (fp16 ? join_kernel<64, true> : join_kernel<64, false>) : (fp16 ? join_kernel<128, true> : join_kernel<128, false>);
-  return launch_overlapped(fn, jp, B * jp.each, kJoinThreads, 0, a.stream) == cudaSuccess ? KVEV_OK : KVEV_ECUDA;
+  return launch_overlapped(fn, jp, dim3(B * jp.each, room < 1 ? 1 : split < room ? split : room), kJoinThreads, 0, a.stream) == cudaSuccess
+             ? KVEV_OK
+             : KVEV_ECUDA;
 }
