@@ -82,13 +82,20 @@ constexpr int kFewRows = 16;
 // tiles of full and other units and their ends at
 //   5, 3; 16, 8     285  690  207  358        5, 3; 20, 10    285  692  206  384
 //   5, 2.5; 16, 5   283  745  190  365        5, 2; 16, 4     343  885  196  359
-__host__ __device__ constexpr int tile_cost(int kind) { return kind == kFull ? 5 : 3; }
-__host__ __device__ constexpr int unit_cost(int kind) { return kind == kFull ? 16 : 8; }
+// With kShared the groups' units run beside as many short ones, of a request's own keys, as keep HBM busy, and write their rows'
+// outputs in 32 bits: us of 64 generations behind 8K, 96 behind 5K, 12 requests' new rows behind 16K and 16 generations behind 16K at
+//   5, 16; 3, 8      63.4  52.9  673  47.3        8, 32; 3, 8     59.1  48.6  642  48.0
+//   6, 24; 3, 8      60.3  51.0  636  48.1        8, 40; 4, 6     58.9  48.3  624  49.0
+template <int kMode>
+__host__ __device__ constexpr int tile_cost(int kind) { return kMode & kShared ? (kind == kFull ? 8 : 4) : kind == kFull ? 5 : 3; }
+template <int kMode>
+__host__ __device__ constexpr int unit_cost(int kind) { return kMode & kShared ? (kind == kFull ? 40 : 6) : kind == kFull ? 16 : 8; }
 // Least cost of a share (a tile's or more: no piece of a cut unit is empty).  Records of
 // more than a few rows are up to 64 KB a side and piece, and one CTA merges them: a
 // chunk of 32 tokens over 4K 25.4 us with shares from 5 on, 21.9 from 20, 29 from 48.
 // (Batches of over 32 requests have larger shares anyway.)
-constexpr int kMinShare = 5, kMinShareRows = 20;
+template <int kMode>
+__host__ __device__ constexpr int min_share(bool rows) { return rows ? 20 : tile_cost<kMode>(kFull); }
 constexpr int kRows = 128;          // rows of a side
 constexpr int kParts = 2;           // halves of a tile's weights, which the second product takes as they come
                                     // (whole: 457 us for 449, four chunks of 1,200 over 9,000)
@@ -392,8 +399,9 @@ __device__ __forceinline__ Unit unit_of(const PagedAttnParams& p, const Request&
   u.kind = u.n > p.P ? kFull : u.n * p.G > kFewRows ? kPaired : kFew;
   return u;
 }
+template <int kMode>
 __device__ __forceinline__ long long cost_of(const Unit& u) {
-  return static_cast<long long>(tile_cost(u.kind)) * u.tiles + unit_cost(u.kind);
+  return static_cast<long long>(tile_cost<kMode>(u.kind)) * u.tiles + unit_cost<kMode>(u.kind);
 }
 __device__ __forceinline__ int units_of(const PagedAttnParams& p, int q) { return (q + 2 * p.P - 1) / (2 * p.P); }
 
@@ -410,7 +418,7 @@ __device__ __forceinline__ long long head_cost(const PagedAttnParams& p, const R
   const int M = units_of(p, r.q);
   for (int m = 0; m < M; ++m) {
     const Unit u = unit_of<kMode>(p, r, m);
-    c += cost_of(u);
+    c += cost_of<kMode>(u);
   }
   return c;
 }
@@ -487,7 +495,7 @@ __device__ __forceinline__ Share share_of(const PagedAttnParams& p, S& sm) {
     total += all;
   }
   if (bad && blockIdx.x == 0) atomicOr(p.status, kStatusDevice);
-  Share r = share_at<kMode>(total, outer, kMinShare);
+  Share r = share_at<kMode>(total, outer, min_share<kMode>(false));
   const long long x = r.x0 - r.before;
   // the thread whose request holds x0 says so
   if (p.segs <= kThreads) {
@@ -535,7 +543,7 @@ __device__ __forceinline__ Share share_of_warp(const PagedAttnParams& p, Request
     if (lane >= o) upto += x;
   }
   const bool rows = __any_sync(0xffffffffu, held.q * p.G > kFewRows);
-  Share r = share_at<kMode>(__shfl_sync(0xffffffffu, upto, 31), S::kHeadsOuter ? p.H_kv : 1, rows ? kMinShareRows : kMinShare);
+  Share r = share_at<kMode>(__shfl_sync(0xffffffffu, upto, 31), S::kHeadsOuter ? p.H_kv : 1, min_share<kMode>(rows));
   const long long x = r.x0 - r.before;
   const uint32_t here = __ballot_sync(0xffffffffu, mine > 0 && upto - mine <= x && x < upto);
   r.s = here ? __ffs(here) - 1 : 0;  // (none: the share is empty)
@@ -583,13 +591,13 @@ __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, Share sh) 
       a += h * hc;
     }
     Unit u = unit_of<kMode>(p, r, m);
-    while (a + cost_of(u) <= sh.x0) {
-      a += cost_of(u);
+    while (a + cost_of<kMode>(u) <= sh.x0) {
+      a += cost_of<kMode>(u);
       u = unit_of<kMode>(p, r, ++m);
     }
     while (a < sh.x1) {
       // boundary x cuts a unit before tile ceil((x - a) / cost of a tile)
-      const int w = tile_cost(u.kind);
+      const int w = tile_cost<kMode>(u.kind);
       auto cut = [&](long long x) {
         const long long o = x - a;
         return o <= 0 ? 0 : static_cast<int>(min(static_cast<long long>(u.tiles), (o + w - 1) / w));
@@ -613,7 +621,7 @@ __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, Share sh) 
         en.first += sh.cta0;
         if (!put(en)) return;
       }
-      a += cost_of(u);
+      a += cost_of<kMode>(u);
       if (a >= sh.x1) break;
       if (2 * p.P * ++m >= r.q) {
         m = 0;
