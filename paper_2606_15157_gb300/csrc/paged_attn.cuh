@@ -95,7 +95,7 @@ __host__ __device__ constexpr int unit_cost(int kind) { return kMode & kShared ?
 // chunk of 32 tokens over 4K 25.4 us with shares from 5 on, 21.9 from 20, 29 from 48.
 // (Batches of over 32 requests have larger shares anyway.)
 template <int kMode>
-__host__ __device__ constexpr int min_share(bool rows) { return rows ? 20 : tile_cost<kMode>(kFull); }
+__host__ __device__ constexpr int min_share(bool rows) { return rows && !(kMode & kFewOnly) ? 20 : tile_cost<kMode>(kFull); }
 constexpr int kRows = 128;          // rows of a side
 constexpr int kParts = 2;           // halves of a tile's weights, which the second product takes as they come
                                     // (whole: 457 us for 449, four chunks of 1,200 over 9,000)
@@ -123,7 +123,8 @@ struct PagedAttnParams {
   int2* units;  // [H_kv][T] of a group's unit, at its first token: CTA of the first piece, pieces
   float *part_o, *part_lse;
   // kQ8: queries, codes and the rows' exponents, strides in bytes
-  int few;  // most tokens of a request of few rows
+  int few;   // most tokens of a request of few rows, and of its units;
+  bool all;  // whatever a request's rows, it is cut into such units
   const uint8_t* q;
   long long q_token, q_head;
   const uint8_t *K, *V, *K_scale, *V_scale;
@@ -374,19 +375,23 @@ template <int kMode>
 __device__ __forceinline__ Request request(const PagedAttnParams& p, int s, bool* bad) {
   if (kMode & kShared) return planned(p.plan, s);
   Request r = own_request(p, s, bad);
-  if ((kMode & kQ8) && (r.q <= p.few) != ((kMode & kFewOnly) != 0)) r.q = 0;
+  if ((kMode & kQ8) && !p.all && (r.q <= p.few) != ((kMode & kFewOnly) != 0)) r.q = 0;
   return r;
 }
 
-// Unit m of a request: tokens [2 P m, 2 P m + n), keys [lo, hi), key tiles [t0, t0 + tiles).
+// Most tokens of a unit.
+template <int kMode>
+__device__ __forceinline__ int unit_tokens(const PagedAttnParams& p) { return kMode & kFewOnly ? p.few : 2 * p.P; }
+
+// Unit m of a request: tokens [m unit_tokens, m unit_tokens + n), keys [lo, hi), key tiles [t0, t0 + tiles).
 struct Unit {
   int n, lo, hi, t0, tiles, kind;
 };
 template <int kMode>
 __device__ __forceinline__ Unit unit_of(const PagedAttnParams& p, const Request& r, int m) {
   Unit u;
-  const int i0 = 2 * p.P * m;
-  u.n = min(2 * p.P, r.q - i0);
+  const int i0 = unit_tokens<kMode>(p) * m;
+  u.n = min(unit_tokens<kMode>(p), r.q - i0);
   const int pos0 = r.kv - r.q + i0;
   u.hi = max(0, pos0 + u.n);
   u.lo = p.window > 0 ? max(0, pos0 - p.window + 1) : 0;
@@ -403,7 +408,8 @@ template <int kMode>
 __device__ __forceinline__ long long cost_of(const Unit& u) {
   return static_cast<long long>(tile_cost<kMode>(u.kind)) * u.tiles + unit_cost<kMode>(u.kind);
 }
-__device__ __forceinline__ int units_of(const PagedAttnParams& p, int q) { return (q + 2 * p.P - 1) / (2 * p.P); }
+template <int kMode>
+__device__ __forceinline__ int units_of(const PagedAttnParams& p, int q) { return (q + unit_tokens<kMode>(p) - 1) / unit_tokens<kMode>(p); }
 
 // a / b for 0 <= a, 0 < b (a 64-bit division costs hundreds of cycles).
 __device__ __forceinline__ long long divide(long long a, long long b) {
@@ -415,7 +421,7 @@ __device__ __forceinline__ long long divide(long long a, long long b) {
 template <int kMode>
 __device__ __forceinline__ long long head_cost(const PagedAttnParams& p, const Request& r) {
   long long c = 0;
-  const int M = units_of(p, r.q);
+  const int M = units_of<kMode>(p, r.q);
   for (int m = 0; m < M; ++m) {
     const Unit u = unit_of<kMode>(p, r, m);
     c += cost_of<kMode>(u);
@@ -605,9 +611,9 @@ __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, Share sh) 
       const int c0 = cut(sh.x0), c1 = cut(sh.x1);
       if (c0 < c1) {
         Entry en;
-        en.tok0 = r.c0 + 2 * p.P * m;
+        en.tok0 = r.c0 + unit_tokens<kMode>(p) * m;
         en.n = u.n;
-        en.pos0 = (kMode & kShared) && r.open ? r.kv - 1 : r.kv - r.q + 2 * p.P * m;
+        en.pos0 = (kMode & kShared) && r.open ? r.kv - 1 : r.kv - r.q + unit_tokens<kMode>(p) * m;
         en.h = h;
         en.s = r.row;
         en.t0 = u.t0 + c0;
@@ -623,7 +629,7 @@ __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, Share sh) 
       }
       a += cost_of<kMode>(u);
       if (a >= sh.x1) break;
-      if (2 * p.P * ++m >= r.q) {
+      if (unit_tokens<kMode>(p) * ++m >= r.q) {
         m = 0;
         if (S::kHeadsOuter) {
           do {

@@ -213,6 +213,12 @@ def test_attention_chunks(paged, reqs, H_q, H, d, page, dtype, heads_first):
     check(paged, reqs, H_q, H, d, page, dtype, heads_first)
 
 
+@pytest.mark.parametrize("H_q,H,d,page,dtype,heads_first", [
+    (32, 8, 128, 16, BF16, False), (8, 8, 64, 32, FP16, True), (8, 1, 64, 8, BF16, False), (15, 1, 128, 128, FP16, False), (40, 2, 128, 16, BF16, True)])
+def test_attention_chunks_among_as_many_requests_as_rows(paged, H_q, H, d, page, dtype, heads_first):
+    check(paged, [(300, 40), (77, 5)] + [(50, 0)] * 45 + [(9, 1)], H_q, H, d, page, dtype, heads_first, window=70)
+
+
 @pytest.mark.parametrize("window", [1, 2, 16, 100, 128, 129, 1000, 10 ** 9])
 @pytest.mark.parametrize("H_q,H,d,page", [(8, 2, 128, 16), (5, 1, 64, 64)])
 def test_attention_windows(paged, window, H_q, H, d, page):
