@@ -117,9 +117,11 @@ struct PagedAttnParams {
   int* status;
   int* sync;       // [2 kMaxCtas] pieces arrived of the unit whose first piece is the CTA's, per side
   uint8_t* parts;  // [2 kMaxCtas][2] records
-  // kShared: what to schedule, the groups over their common keys and the requests (paged_shared.cu); the rows' two
-  // parts, [2][T][H_q][d] normalised and [2][T][H_q] their log2-sum-exp
-  const int4* plan;
+  // kShared: the groups' first requests and how many tokens their requests have in common; the plan, what to schedule: the N
+  // groups over their common keys, then the requests; the rows' two parts, [2][T][H_q][d] normalised and [2][T][H_q] their log2-sum-exp
+  const int *groups, *shared;
+  int N;
+  int4* plan;
   int2* units;  // [H_kv][T] of a group's unit, at its first token: CTA of the first piece, pieces
   float *part_o, *part_lse;
   // kQ8: queries, codes and the rows' exponents, strides in bytes
@@ -353,6 +355,7 @@ struct Request {
   int c0, q, kv;
   int lo, row;  // kShared: first key, row of the block table
   bool open;    // kShared: a group's rows over the keys they have in common, all of which every row sees
+  int g0, g1;   // kShared: the first row of the request's group, and the one after its last
 };
 __device__ __forceinline__ Request own_request(const PagedAttnParams& p, int s, bool* bad) {
   Request r = {};
@@ -365,15 +368,70 @@ __device__ __forceinline__ Request own_request(const PagedAttnParams& p, int s, 
   if (!ok) *bad = true;
   return r;
 }
-// kShared: a request as the plan has it.
-__device__ __forceinline__ Request planned(const int4* plan, int s) {
-  const int4 a = plan[2 * s], b = plan[2 * s + 1];
-  return {a.x, a.y, a.z, a.w, b.x, b.y != 0};
+// ---- kShared: the plan, 32 bytes a group or request
+constexpr int kPlannedByWarp = 32;  // groups and requests of a batch that the dealing warps plan
+
+__device__ __forceinline__ Request planned(const PagedAttnParams& p, int s) {
+  const int4 a = p.plan[2 * s], b = p.plan[2 * s + 1];
+  return {a.x, a.y, a.z, a.w, b.x, b.y != 0, b.z, b.w};
 }
+__device__ __forceinline__ void keep_plan(const PagedAttnParams& p, int s, const Request& r) {
+  p.plan[2 * s] = make_int4(r.c0, r.q, r.kv, r.lo);
+  p.plan[2 * s + 1] = make_int4(r.row, r.open, r.g0, r.g1);
+}
+// Whether the groups' first requests ascend in [0, B]: if not, nothing is shared.
+__device__ __forceinline__ bool group_in_order(const PagedAttnParams& p, int g) {
+  const int a = p.groups[g], b = p.groups[g + 1];
+  return a >= 0 && a <= b && b <= p.B;
+}
+// Whole pages of keys that are read once for the requests a .. b - 1, n tokens being common to them, and their rows [g0, g1): none
+// for a single request, nor where the rows or n are out of range.
+__device__ __forceinline__ int common_keys(const PagedAttnParams& p, int a, int b, int n, int* g0, int* g1) {
+  if (n < 0 || n > (p.max_pages << p.page_shift) || b - a < 2) return 0;
+  *g0 = p.cu[a];
+  *g1 = p.cu[b];
+  return *g0 >= 0 && *g1 >= *g0 && *g1 <= p.T ? n & ~((1 << p.page_shift) - 1) : 0;
+}
+__device__ __forceinline__ Request plan_of(const PagedAttnParams& p, int s, bool in_order, bool* bad) {
+  Request r = {};
+  int g0 = 0, g1 = 0;
+  if (s < p.N) {
+    const int n = p.shared[s];
+    if (n < 0 || n > (p.max_pages << p.page_shift)) *bad = true;
+    r.row = p.groups[s];
+    r.open = true;
+    if (in_order) r.kv = common_keys(p, r.row, p.groups[s + 1], n, &g0, &g1);
+    if (r.kv > 0) {
+      r.c0 = g0;
+      r.q = g1 - g0;
+    }
+    return r;
+  }
+  s -= p.N;
+  r = own_request(p, s, bad);
+  if (!in_order || r.q == 0) return r;
+  int g = 0, n = p.N;  // the last group with groups[g] <= s
+  while (n > 1) {
+    const int h = n >> 1;
+    if (p.groups[g + h] <= s) g += h;
+    n -= h;
+  }
+  const int a = p.groups[g], b = p.groups[g + 1];
+  if (a > s || b <= s) return r;
+  const int k = common_keys(p, a, b, p.shared[g], &g0, &g1);
+  // all of them before its new tokens, which are among the group's (where the counts do not ascend they may not be)
+  if (k > 0 && r.kv - r.q >= k && r.c0 >= g0 && r.c0 + r.q <= g1) {
+    r.lo = k;
+    r.g0 = g0;
+    r.g1 = g1;
+  }
+  return r;
+}
+
 // Request s to schedule.
 template <int kMode>
 __device__ __forceinline__ Request request(const PagedAttnParams& p, int s, bool* bad) {
-  if (kMode & kShared) return planned(p.plan, s);
+  if (kMode & kShared) return planned(p, s);
   Request r = own_request(p, s, bad);
   if ((kMode & kQ8) && !p.all && (r.q <= p.few) != ((kMode & kFewOnly) != 0)) r.q = 0;
   return r;
@@ -538,7 +596,16 @@ __device__ __forceinline__ Share share_of_warp(const PagedAttnParams& p, Request
   const int lane = threadIdx.x & 31;
   bool bad = false;
   held = {};
-  if (lane < p.segs) held = request<kMode>(p, lane, &bad);
+  if (kMode & kShared) {
+    const bool in_order = __all_sync(0xffffffffu, lane >= p.N || group_in_order(p, lane));
+    bad = !in_order;
+    if (lane < p.segs) {
+      held = plan_of(p, lane, in_order, &bad);
+      if (blockIdx.x == 0) keep_plan(p, lane, held);
+    }
+  } else if (lane < p.segs) {
+    held = request<kMode>(p, lane, &bad);
+  }
   held_cost = head_cost<kMode>(p, held);
   const long long mine = S::kHeadsOuter ? held_cost : held_cost * p.H_kv;
   if (bad && blockIdx.x == 0) atomicOr(p.status, kStatusDevice);
@@ -562,14 +629,14 @@ template <int kMode, class S>
 __device__ __forceinline__ void deal(const PagedAttnParams& p, S& sm, Share sh) {
   uint32_t e = 0;
   const int lane = threadIdx.x & 31;
-  const bool short_batch = p.segs <= 32;
+  const bool short_batch = p.segs <= kPlannedByWarp;
   Request held;
   long long held_cost;
   if (short_batch) sh = share_of_warp<kMode, S>(p, held, held_cost);
   auto get = [&](int s) {
     if (short_batch) {
       auto of = [&](int v) { return __shfl_sync(0xffffffffu, v, s); };
-      Request r = {of(held.c0), of(held.q), of(held.kv), 0, s, false};
+      Request r = {of(held.c0), of(held.q), of(held.kv), 0, s, false, 0, 0};
       if (kMode & kShared) { r.lo = of(held.lo); r.row = of(held.row); r.open = of(held.open) != 0; }
       return r;
     }
@@ -1819,7 +1886,7 @@ __global__ void __launch_bounds__(Split<kMode>::kThreads, 1) paged_attn_kernel(c
   pdl_wait();
   pdl_trigger();
   Share sh = {};
-  if (p.segs > 32) sh = share_of<kMode>(p, sm);
+  if (p.segs > kPlannedByWarp) sh = share_of<kMode>(p, sm);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();

@@ -662,7 +662,7 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(M)) q8_few_kernel(const 
   pdl_wait();
   pdl_trigger();
   Share sh = {};
-  if (p.segs > 32) sh = share_of<kFewMode>(p, sm);
+  if (p.segs > kPlannedByWarp) sh = share_of<kFewMode>(p, sm);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();

@@ -17,81 +17,18 @@ namespace {
 // the group's first row and the one after its last), 32 bytes each: what the attention's CTAs would all read through the
 // groups' and the requests' lengths in turn (made there, a call of 64 generations behind a single page took 70 us, the same
 // without a group 39).
-struct PlanParams {
-  const int *cu, *kv_lens, *groups, *shared;
-  int B, T, N, most, page_shift;  // most: tokens that a row of the block table holds
-  int4* plan;
-  int* status;
-};
+// Batches of up to 32 are planned by every CTA's dealing warp, a lane each, and the first CTA's leaves the plan to the join.
 constexpr int kPlanThreads = 128;
 
-// Whole pages of keys that are read once for the requests a .. b - 1, n tokens being common to them: none for a single request,
-// nor where the group's rows are out of range.
-__device__ __forceinline__ int common_keys(const PlanParams& p, int a, int b, int n) {
-  if (n < 0 || n > p.most || b - a < 2) return 0;
-  const int c0 = p.cu[a], c1 = p.cu[b];
-  return c0 >= 0 && c1 >= c0 && c1 <= p.T ? n & ~((1 << p.page_shift) - 1) : 0;
-}
-
-__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ PlanParams p) {
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ PagedAttnParams p) {
   pdl_wait();
   pdl_trigger();
-  bool in_order = true;  // the groups' first requests ascend in [0, B]; if not, nothing is shared
-  for (int g = threadIdx.x; g < p.N; g += kPlanThreads) {
-    const int a = p.groups[g], b = p.groups[g + 1];
-    in_order &= a >= 0 && a <= b && b <= p.B;
-  }
-  const int s = blockIdx.x * kPlanThreads + threadIdx.x, r = s - p.N;
-  int4 x = make_int4(0, 0, 0, 0), y = make_int4(0, 0, 0, 0);
-  bool bad = false;
-  int c1 = 0;
-  if (r >= 0 && r < p.B) {
-    x.x = p.cu[r];
-    c1 = p.cu[r + 1];
-    x.z = p.kv_lens[r];
-  }
+  bool in_order = true;
+  for (int g = threadIdx.x; g < p.N; g += kPlanThreads) in_order &= group_in_order(p, g);
+  const int s = blockIdx.x * kPlanThreads + threadIdx.x;
   in_order = __syncthreads_and(in_order);
-  bad = !in_order;
-  if (s < p.N) {
-    const int a = p.groups[s], n = p.shared[s];
-    bad |= n < 0 || n > p.most;
-    if (in_order) {
-      const int b = p.groups[s + 1], k = common_keys(p, a, b, n);
-      y = make_int4(a, 1, 0, 0);
-      if (k > 0) {
-        x.x = p.cu[a];
-        x.y = p.cu[b] - x.x;
-        x.z = k;
-      }
-    }
-  } else if (r < p.B) {
-    const bool ok = x.x >= 0 && c1 >= x.x && c1 <= p.T && x.z >= 0 && x.z <= p.most;
-    bad |= !ok;
-    x.y = ok ? c1 - x.x : 0;
-    y.x = r;
-    if (ok && in_order) {
-      int g = 0, n = p.N;  // the last group with groups[g] <= r
-      while (n > 1) {
-        const int h = n >> 1;
-        if (p.groups[g + h] <= r) g += h;
-        n -= h;
-      }
-      const int a = p.groups[g], b = p.groups[g + 1];
-      if (a <= r && r < b) {
-        const int k = common_keys(p, a, b, p.shared[g]);
-        // all of them before its new tokens, which are among the group's (where the counts do not ascend they may not be)
-        if (k > 0 && x.z - x.y >= k && x.x >= p.cu[a] && c1 <= p.cu[b]) {
-          x.w = k;
-          y.z = p.cu[a];
-          y.w = p.cu[b];
-        }
-      }
-    }
-  }
-  if (s < p.N + p.B) {
-    p.plan[2 * s] = x;
-    p.plan[2 * s + 1] = y;
-  }
+  bool bad = !in_order;
+  if (s < p.segs) keep_plan(p, s, plan_of(p, s, in_order, &bad));
   if (bad) atomicOr(p.status, kStatusDevice);
 }
 
@@ -99,7 +36,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
 constexpr int kJoinThreads = 256;
 
 struct JoinParams {
-  PagedAttnParams p;  // the attention's, but for the plan: the requests'
+  PagedAttnParams p;  // the attention's
   int each;
 };
 
@@ -113,9 +50,9 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
   pdl_wait();
   pdl_trigger();
   const int s = blockIdx.x / j.each;
-  const Request r = planned(p.plan, s);
+  const Request r = planned(p, p.N + s);
   if (r.lo == 0) return;
-  const int g0 = p.plan[2 * s + 1].z, g1 = p.plan[2 * s + 1].w;
+  const int g0 = r.g0, g1 = r.g1;
   for (int i = blockIdx.x - s * j.each; i < r.q; i += j.each) {
     const int t = r.c0 + i, m = (t - g0) / (2 * p.P), tok0 = g0 + 2 * p.P * m, n = min(2 * p.P, g1 - tok0);
     const int kind = n > p.P ? kFull : n * p.G > kFewRows ? kPaired : kFew;
@@ -216,21 +153,23 @@ extern "C" int kvev_paged_attention_shared(const kvev_paged_cache* cache, const 
   if (rc != KVEV_OK) return rc;
   if (!attn_page_maps(cache, &p)) return KVEV_ECUDA;
   uint8_t* const after = static_cast<uint8_t*>(workspace) + attn_workspace_bytes(d);
-  int4* const plan = reinterpret_cast<int4*>(after);
-  p.plan = plan;
+  p.plan = reinterpret_cast<int4*>(after);
+  p.groups = groups;
+  p.shared = shared_lens;
+  p.N = N;
   p.segs = B + N;
   uint8_t* const parts = after + kPlanBytes + units_bytes(T, cache->H_kv);
   p.units = reinterpret_cast<int2*>(after + kPlanBytes);
   p.part_lse = reinterpret_cast<float*>(parts);
   p.part_o = reinterpret_cast<float*>(parts + part_lse_bytes(T, H_q));
-  const PlanParams pp = {cu_new, kv_lens, groups, shared_lens, B, T, N, max_pages << p.page_shift, p.page_shift, plan, device_status};
-  if (launch_overlapped(plan_kernel, pp, (B + N + kPlanThreads - 1) / kPlanThreads, kPlanThreads, 0, a.stream) != cudaSuccess) return KVEV_ECUDA;
+  if (p.segs > kPlannedByWarp &&
+      launch_overlapped(plan_kernel, p, (B + N + kPlanThreads - 1) / kPlanThreads, kPlanThreads, 0, a.stream) != cudaSuccess)
+    return KVEV_ECUDA;
   rc = attn_launch<kShared>(p, d, fp16, a.stream);
   if (rc != KVEV_OK) return rc;
   // as many CTAs to a request as it has rows, as far as the host can tell, and enough of them for the GPU in all
   const int rows = (T + B - 1) / B, most = (8 * kMaxCtas + B - 1) / B;
-  JoinParams jp = {p, rows < most ? rows : most};
-  jp.p.plan = plan + 2 * N;
+  const JoinParams jp = {p, rows < most ? rows : most};
   const int vectors = H_q * (d / 4), split = (vectors + kJoinThreads - 1) / kJoinThreads, room = 8 * kMaxCtas / (B * jp.each);
   const auto fn = d == 64 ? (fp16 ? join_kernel<64, true> : join_kernel<64, false>) : (fp16 ? join_kernel<128, true> : join_kernel<128, false>);
   return launch_overlapped(fn, jp, dim3(B * jp.each, room < 1 ? 1 : split < room ? split : room), kJoinThreads, 0, a.stream) == cudaSuccess
