@@ -406,40 +406,33 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D, 
     tc_fence_after();
     const float k2 = __uint_as_float(ex.x << 23), b = static_cast<float>(static_cast<int>(ex.y) - 127);
     const bool edge = j < f0 || j >= f1;
-    // the logits of group g
-    auto logits = [&](int g, float (&y)[kRowGroup]) {
-      load_rows(ts + g * kGroupCols, y);
-#pragma unroll
-      for (int r = 0; r < kRowGroup; ++r) y[r] *= qscale[g * kRowGroup + r] * k2;
-      if (edge) {
-        const int k = j * kRows + key;
-#pragma unroll
-        for (int r = 0; r < kRowGroup; ++r) {
-          const int t = en.pos0 + (g * kRowGroup + r) / p.G;
-          if (g * kRowGroup + r >= rows || k > t || (p.window > 0 && k <= t - p.window)) y[r] = -INFINITY;
-        }
-      }
-    };
-    float y[kRowGroup];  // (of more groups: formed again where they are used)
-    bool up = false;
+    float y[R];
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
-      logits(g, y);
+      float v[kRowGroup];
+      load_rows(ts + g * kGroupCols, v);
 #pragma unroll
-      for (int r = 0; r < kRowGroup; ++r)
-        up |= y[r] > sm.m[g * kRowGroup + r] + kFewRaise || y[r] + b > sm.mz[g * kRowGroup + r] + kFewRaise;
+      for (int r = 0; r < kRowGroup; ++r) y[g * kRowGroup + r] = v[r] * (qscale[g * kRowGroup + r] * k2);
     }
+    if (edge) {
+      const int k = j * kRows + key;
+      int t = en.pos0, i = 0;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (r >= rows || k > t || (p.window > 0 && k <= t - p.window)) y[r] = -INFINITY;
+        if (++i == p.G) { i = 0; ++t; }
+      }
+    }
+    bool up = false;
+#pragma unroll
+    for (int r = 0; r < R; ++r) up |= y[r] > sm.m[r] + kFewRaise || y[r] + b > sm.mz[r] + kFewRaise;
     if (group_any(0, up)) {
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) {
-        if (kGroups > 1) logits(g, y);
-#pragma unroll
-        for (int r = 0; r < kRowGroup; ++r) {
-          const float a = warp_max(y[r]), z = warp_max(y[r] + b);
-          if (lane == 0) {
-            sm.red[0][warp][g * kRowGroup + r] = a;
-            sm.red[1][warp][g * kRowGroup + r] = z;
-          }
+      for (int r = 0; r < R; ++r) {
+        const float a = warp_max(y[r]), z = warp_max(y[r] + b);
+        if (lane == 0) {
+          sm.red[0][warp][r] = a;
+          sm.red[1][warp][r] = z;
         }
       }
       group_sync(0);
@@ -485,24 +478,19 @@ __device__ __forceinline__ void q8_few_rows(const PagedAttnParams& p, Q8Smem<D, 
     uint8_t* const pw = sm.p[(j - first) & 1] + (key & 15);
     const int chunk = key >> 4;
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      if (kGroups > 1) logits(g, y);
+    for (int r = 0; r < R; r += 2) {
+      float w[2];
 #pragma unroll
-      for (int r = 0; r < kRowGroup; r += 2) {
-        float w[2];
+      for (int i = 0; i < 2; ++i) {
+        l[r + i] += ex2_approx(y[r + i] - finite_or_0(sm.m[r + i]));
+        w[i] = ex2_approx(y[r + i] + b - (finite_or_0(sm.mz[r + i]) - kFewUp));
+      }
+      uint32_t c[kQParts];
+      parts2(w[0], w[1], c);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int q = g * kRowGroup + r + i;
-          l[q] += ex2_approx(y[r + i] - finite_or_0(sm.m[q]));
-          w[i] = ex2_approx(y[r + i] + b - (finite_or_0(sm.mz[q]) - kFewUp));
-        }
-        uint32_t c[kQParts];
-        parts2(w[0], w[1], c);
-#pragma unroll
-        for (int q = 0; q < kQParts; ++q) {
-          pw[chunk_at<128>(column_of(q, g * kRowGroup + r), chunk)] = static_cast<uint8_t>(c[q]);
-          pw[chunk_at<128>(column_of(q, g * kRowGroup + r + 1), chunk)] = static_cast<uint8_t>(c[q] >> 8);
-        }
+      for (int q = 0; q < kQParts; ++q) {
+        pw[chunk_at<128>(column_of(q, r), chunk)] = static_cast<uint8_t>(c[q]);
+        pw[chunk_at<128>(column_of(q, r + 1), chunk)] = static_cast<uint8_t>(c[q] >> 8);
       }
     }
     few_mend_v(p, sm, en, j, st);
