@@ -605,6 +605,8 @@ KVEV_API int kvev_paged_attention(const kvev_paged_cache *cache, const void *q, 
  *               those of a group of one request.
  *   N           0 .. KVEV_PAGED_MAX_REQUESTS - B.
  * Pages of the common tokens are taken from the block-table row of the group's first request.
+ * (kvev_paged_release() gives back every page of a request: the entries of shared pages are to be -1 in
+ * the rows of all requests but the last one released, which leaves them out, with status bit 2.)
  * A row's two parts are held as fp32 in the workspace and put together by their
  * log-sum-exp.  A shared length that is negative or more than max_pages * page_size
  * counts as 0, and groups that do not ascend as none, both with status bit 2; the rest, errors among it,
@@ -656,7 +658,9 @@ KVEV_API int kvev_paged_q8_gather(const kvev_paged_q8_cache *cache, const int32_
                                   int32_t *device_status, void *stream);
 
 /* kvev_paged_attention() over the values that the codes stand for; q and out in the cache's 16-bit type.
- * The workspace is that of kvev_paged_attention_workspace(). */
+ * Chunks attend as over 16-bit pages of those values.  Requests of up to 16 query rows to a KV head (single tokens) attend
+ * on the codes: query elements and softmax weights are held to 2^-9 of their own size four times over, down to 2^-32 of the row's
+ * largest element and 2^-30 of its largest weight.  The workspace is that of kvev_paged_attention_workspace(). */
 KVEV_API int kvev_paged_q8_attention(const kvev_paged_q8_cache *cache, const void *q, int64_t q_token_stride,
                                      int64_t q_head_stride, const int32_t *cu_new, const int32_t *kv_lens,
                                      const int32_t *block_table, int max_pages, int B, int T, int H_q,

@@ -28,7 +28,7 @@
 // workspace; the piece that arrives last merges them in order, so the result does
 // not depend on which that is.
 //
-// Roles (384 threads): warp 0 loads Q tiles and page boxes by TMA, warp 1 issues the
+// Roles (384 threads, 640 for pages of 8 bits): warp 0 loads Q tiles and page boxes by TMA, warp 1 issues the
 // MMAs, warp 2 deals the entries (pieces of units) to the others through a ring, warps 4-7
 // and 8-11 are the sides' softmax warpgroups.  S = Q K^T is read from tensor memory
 // into registers, and the weights go back into the same columns as the A operand of
@@ -520,7 +520,7 @@ struct Share {
 // The CTA's share of `outer` rounds of cost `round`; before: the cost of the rounds before its own.  kFewOnly and kShared,
 // where the CTAs divide by the rounds: each round its own CTAs, so that all rounds, the KV heads, are at the same place at the same time.
 // (Codes of a token's heads are 64 or 128 bytes next to one another in tokens-first pages: 64 generations over 4,097 tokens, 64-element
-// heads, with shares that do not end with the heads 111 us, %%G so.)
+// heads, with shares that do not end with the heads 111 us, 65 so.)
 template <int kMode>
 __device__ __forceinline__ Share share_at(long long round, int outer, int least) {
   Share r = {};
@@ -867,15 +867,17 @@ __device__ __forceinline__ bool group_any(int x, bool v) {
   return r != 0;
 }
 
-// ---- kQ8: warps 12-15, pages of 8-bit codes to 16-bit tiles ---------------------------------
+// ---- kQ8: warps 12-19, pages of 8-bit codes to 16-bit tiles ---------------------------------
 // Warp 0 loads codes; the tiles that it would have loaded from 16-bit pages are made of them here, in the same order
 // and places of the ring.  The values are 16-bit ones exactly, so that nothing after this differs.  A thread has the
-// power of two of one row of the next tile in flight, and turns 16 codes at a time, of 8 (4) rows.  Rows without a key of
+// exponent of one row of the next tile in flight, and turns 16 codes at a time, of 4 (2) rows.  Rows without a key of
 // the unit become zeros, whatever the pool holds there.
-// Measured, the last 4K of a 32K prompt: %%D
+// The last 4K of a 32K prompt takes 1.69 ms, 1.57 in half precision, and 1.23 from 16-bit pages: making a tile moves 64 KB
+// through shared memory beside the 96 KB that the products read of it, and issues a third as many instructions as the
+// softmax does; with four warps instead of eight the time is the same.  Measured on the way: codes loaded by the converting
+// warps themselves 2.73 ms, without a branch between one row and the next 2.18; by TMA 1.80; a tile's rows together 1.69.
 
-// Loads ahead of their use, under a condition, said in PTX: from a plain load with a constant in its place the compiler
-// makes one whose first use, a comparison or a shift, follows it at once and waits for it.
+// Loads under a condition without a branch.
 __device__ __forceinline__ int load_int_if(const int* at, bool there, int other) {
   int v = other;
   asm volatile(
@@ -896,7 +898,7 @@ __device__ __forceinline__ uint32_t load_byte_if(const uint8_t* at, bool there, 
 }
 
 // 16 codes times 2^(b - 127) as 16-bit values, exactly.  (By moving a code's bits to their place in the 16-bit type and one product,
-// with no conversion instruction, it is more instructions: 1.93 ms for 1.80, in half precision 1.98 for 1.59.)
+// with no conversion instruction, it is more instructions: 1.75 ms for 1.69, in half precision 1.76 for 1.56.)
 template <bool kFp16>
 __device__ __forceinline__ void values16(uint4 x, uint32_t b, uint4& lo, uint4& hi) {
   const uint32_t c[4] = {x.x, x.y, x.z, x.w};
@@ -1233,7 +1235,7 @@ __device__ __forceinline__ float lse2_of(float m, float l) {  // log2
 __device__ __forceinline__ float finite_or_0(float m) { return m == -INFINITY ? 0.f : m; }
 
 // A cut unit of a group: its pieces stay as they are, and are put together row by row with the requests' own parts, on all
-// SMs (merged here, by a CTA a unit, 64 generations behind 8K 73 us, %%H so).  Its first piece says where they are.
+// SMs (merged here, by a CTA a unit, 64 generations behind 8K 73 us, 62 so).  Its first piece says where they are.
 template <int kMode>
 __device__ __forceinline__ bool left_to_join(const PagedAttnParams& p, const Entry& en, int x) {
   if (!(kMode & kShared) || en.part != 0) return false;
@@ -1842,8 +1844,9 @@ __global__ void __launch_bounds__(Split<kMode>::kThreads, 1) paged_attn_kernel(c
     pdl_wait();
     bool some = false;
     for (int s = threadIdx.x; s < p.B; s += Split<kMode>::kThreads) {
-      const int c0 = p.cu[s], c1 = p.cu[s + 1];
-      some |= c0 < 0 || c1 > p.T || c1 < c0 || c1 - c0 > p.few;  // (what is out of range is said by the schedule)
+      const int c0 = p.cu[s], c1 = p.cu[s + 1], kv = p.kv_lens[s];
+      // (what is out of range is said by the schedule)
+      some |= c0 < 0 || c1 > p.T || c1 < c0 || c1 - c0 > p.few || kv < 0 || kv > (p.max_pages << p.page_shift);
     }
     if (!__syncthreads_or(some)) return;
   }

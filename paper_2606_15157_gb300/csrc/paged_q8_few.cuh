@@ -16,7 +16,14 @@
 // its key's weights, O^T += B^T w^T with the codes of V as the operand whose key index runs slowest; the schedule is the
 // same, and so are pieces and their merge.  A CTA has one softmax warpgroup and takes its units one after another; what hides a
 // tile's chain of latencies (scores, weights, products) and a unit's start and end is the other CTAs of the SM.
-// (%%F)
+//
+// Bounds and measurements (one GB300, 32 query and 8 KV heads of 128, pages of 16, tokens first): HBM, and each unit's start
+// and end.  16 generations at 16K (pages of 64) 88 us, 6.1 TB/s of codes; 64 at 4K 93 us, 5.8 TB/s; 64 ragged ones to 8K of 64-element
+// heads 57 us, 4.7 TB/s; each further 4K of 64 generations at HBM's rate.  One at 4K 13.4 us: schedule and first loads 4, two
+// tiles of a CTA 2, records and merge 3, the launch 2.  16 heads to a KV head: 64 at 4K 135 us, the threads' 64 codes a tile.
+// Measured on the way (16 at 16K and 64 ragged): two sides of a CTA, each with every other tile, as the 16-bit kernel has them
+// 95 and 97 us; scores of a side's next tile formed early 97 and 102; two such CTAs an SM 100 and 80; one side a CTA and three CTAs
+// 95 and 64 (100 and 107 before the KV heads were in step); without the other kernel's launch 88 and 57.
 #pragma once
 #include "paged_attn.cuh"
 
@@ -619,6 +626,15 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(M)) q8_few_kernel(const 
   }
   S& sm = *reinterpret_cast<S*>(smem_raw);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
+  if (!p.all) {  // (chunks alone leave nothing to do here; what is out of range is said by the other kernel's schedule too)
+    pdl_wait();
+    bool some = false;
+    for (int s = threadIdx.x; s < p.B; s += kFewThreads) {
+      const int n = p.cu[s + 1] - p.cu[s];
+      some |= n > 0 && n <= p.few;
+    }
+    if (!__syncthreads_or(some)) return;
+  }
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kStages; ++i) {
       mbar_init(&sm.full[i], 1);

@@ -438,3 +438,52 @@ def test_a_prompt_in_chunks_then_generations(paged):
         want = (codes.view(q8_ref.E4M3).double() * torch.exp2(e.double() - 127)[..., None]).to(BF16)
         assert torch.equal(oK[s, :, :done[s]].transpose(0, 1), want)
     assert c.status() == 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("new", [1, 17])
+def test_attention_many_small_weights(paged, dtype, new):
+    """One key has nearly all of the weight, 8,000 others 2^-20 each: together 2^-7 of the result.  Single tokens hold a weight to 2^-30 of the
+    largest, so all of them to 8,000 2^-30 |v| < 2^-17; chunks to the type's unit roundoff of each."""
+    n = 8001
+    c, q, cu, kv, table = attend_case(paged, [(n, new)], 4, 1, 128, 16, dtype, False, spread=0.0)
+    pos = torch.arange(n, device="cuda")
+    p = torch.tensor(table[0], device="cuda")[pos // 16]
+    q.fill_(1.0)
+    c.K.view(torch.uint8)[p, pos % 16, 0] = 0  # logits of 0, but for key 5:
+    c.K.view(torch.uint8)[p[5], 5, 0] = 0x38
+    c.K_scale[p[5], 0, 5] = 127
+    c.V.view(torch.uint8)[p, pos % 16, 0] = 0x38  # values 1, of key 5 one half
+    c.V_scale[p, 0, pos % 16] = 127
+    c.V_scale[p[5], 0, 5] = 126
+    scale = 20 * math.log(2) / 128  # key 5's logit is 20 ln 2 above
+    o, lse = run_attention(c, q, cu, kv, scale=scale)
+    q8_ref.check_attention(o, lse, plain(c, table, q, cu, kv, scale), dtype, small_weights=n * 2.0 ** -30 if new == 1 else 0.0)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_attention_of_codes_that_are_no_numbers(paged, new):
+    """A NaN in a row that is seen is the answer of its head's rows that see it, and of nobody else's."""
+    c, q, cu, kv, table = attend_case(paged, [(300, new), (200, 1)], 8, 2, 128, 16, BF16, False)
+    good, _ = run_attention(c, q, cu, kv)
+    c.V.view(torch.uint8)[table[0][3], 2, 1, 77] = 0xff
+    o, lse = run_attention(c, q, cu, kv)
+    assert torch.isnan(o[:new, 4:, 77]).all() and c.status() == 0
+    assert torch.equal(o[:, :4], good[:, :4]) and torch.equal(o[new:], good[new:])
+    c.K.view(torch.uint8)[table[0][5], 1, 0, 3] = 0x7f
+    o, lse = run_attention(c, q, cu, kv)
+    assert torch.isnan(o[:new, :4]).all() and torch.isnan(lse[:new, :4]).all() and torch.equal(o[new:], good[new:])
+
+
+@pytest.mark.parametrize("e", [-120, -60, 60, 115])
+@pytest.mark.parametrize("new", [1, 20])
+def test_attention_over_values_at_the_ends_of_the_type(paged, e, new):
+    c, q, cu, kv, table = attend_case(paged, [(500, new)], 4, 1, 128, 16, BF16, False, spread=0.0)
+    c.V_scale.fill_(127 + e)
+    o, lse = run_attention(c, q, cu, kv)
+    r = list(plain(c, table, q, cu, kv))
+    f = 2.0 ** -e  # (compared at 1: the tolerance has an absolute part)
+    if e > -110:  # (below, the results are subnormal)
+        q8_ref.check_attention(o.double() * f, lse, [r[0] * f, r[1], r[2] * f, r[3]], BF16)
+    else:
+        assert ((o.double() - r[0]).abs() <= 2.0 ** -126 + 2.0 ** -6 * r[2]).all()

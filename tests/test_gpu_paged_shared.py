@@ -249,3 +249,46 @@ def test_refused_tensors(paged):
     with pytest.raises(kvev.KvevError) as e:
         c.attention_shared(q[:, :3], cu, lens, groups, n)
     assert e.value.code == kvev.EINVAL and c.status() == 0
+
+
+def test_forks_of_a_prefilled_prefix(paged):
+    """As a serving program has it: the prefix goes through tables, write and attention once; requests take its pages into their rows of
+    the table; their prompts, and then generations, attend with the prefix shared."""
+    H_q, H, d, page, B, n = 8, 2, 128, 16, 6, 96
+    width = ref.pages_of(n + 60, page)
+    table = torch.full((B + 1, width), -1, dtype=torch.int32, device="cuda")
+    pool = paged.PagePool(200, page, table)
+    c = paged.PagedCache.empty(200, page, H, d, table)
+    c.K.zero_(), c.V.zero_()
+    g = torch.Generator(device="cuda").manual_seed(0)
+    lens = torch.zeros(B + 1, dtype=torch.int32, device="cuda")
+
+    def forward(new):
+        T = sum(new)
+        qkv = torch.randn((T, H_q + 2 * H, d), generator=g, device="cuda").to(BF16)
+        _, cu, slots, _, granted = pool.tables(lens, ints(new), T, kv_lens=lens)
+        assert bool(granted.all())
+        c.write(qkv[:, H_q:H_q + H], qkv[:, H_q + H:], slots)
+        return qkv[:, :H_q], cu
+
+    q, cu = forward([n] + [0] * B)  # request 0 holds the prefix
+    c.attention(q, cu, lens)
+    table[1:, :n // page] = table[0, :n // page]
+    lens[1:] = n
+    groups, shared = ints([1, 4, B + 1]), ints([n, n - 20])
+    for new in ([0, 30, 1, 17, 5, 40, 2], [0] + [1] * B, [0] + [1] * B):
+        q, cu = forward(new)
+        lse = torch.empty((q.shape[0], H_q), device="cuda")
+        o = c.attention_shared(q, cu, lens, groups, shared, lse=lse)
+        r = ref.attention(c.K, c.V, table.cpu().tolist(), q, cu.cpu().tolist(), lens.cpu().tolist())
+        q8_ref.check_attention(o, lse, r, BF16, parts=2)
+    assert c.status() == 0 and int(pool.device_status) == 0
+    # the pages go back once: the prefix's with request 0, the others' without it
+    own = table.clone()
+    own[1:, :n // page] = -1
+    taken = int((own >= 0).sum())
+    done = torch.ones(B + 1, dtype=torch.int32, device="cuda")
+    table.copy_(own)
+    pool.release(lens, done)
+    assert int(pool.free_count) == 200 and taken + 0 > n // page and int(pool.device_status) == 2
+    assert sorted(pool.free.cpu().tolist()) == list(range(200))
