@@ -604,7 +604,7 @@ KVEV_API int kvev_paged_attention(const kvev_paged_cache *cache, const void *q, 
  *               common tokens of a request that holds fewer before its new ones, and
  *               those of a group of one request.
  *   N           0 .. KVEV_PAGED_MAX_REQUESTS - B.
- * Pages of the common tokens are taken from the block-table row of the group's first request.
+ * Pages of the common tokens are taken from the block-table row of the group's first request that shares them.
  * (kvev_paged_release() gives back every page of a request: the entries of shared pages are to be -1 in
  * the rows of all requests but the last one released, which leaves them out, with status bit 2.)
  * A row's two parts are held as fp32 in the workspace and put together by their

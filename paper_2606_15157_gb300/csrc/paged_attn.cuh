@@ -392,18 +392,43 @@ __device__ __forceinline__ int common_keys(const PagedAttnParams& p, int a, int 
   *g1 = p.cu[b];
   return *g0 >= 0 && *g1 >= *g0 && *g1 <= p.T ? n & ~((1 << p.page_shift) - 1) : 0;
 }
+// Whether request r shares the group's k keys: it holds all of them before its new rows, which are among the group's (where the counts
+// do not ascend they may not be).
+__device__ __forceinline__ bool takes_part(const Request& r, int k, int g0, int g1) {
+  return r.q > 0 && r.kv - r.q >= k && r.c0 >= g0 && r.c0 + r.q <= g1;
+}
 __device__ __forceinline__ Request plan_of(const PagedAttnParams& p, int s, bool in_order, bool* bad) {
   Request r = {};
   int g0 = 0, g1 = 0;
   if (s < p.N) {
     const int n = p.shared[s];
     if (n < 0 || n > (p.max_pages << p.page_shift)) *bad = true;
-    r.row = p.groups[s];
     r.open = true;
-    if (in_order) r.kv = common_keys(p, r.row, p.groups[s + 1], n, &g0, &g1);
-    if (r.kv > 0) {
+    if (!in_order) return r;
+    const int a = p.groups[s], b = p.groups[s + 1];
+    // the pages are those of the first request that shares them: one before it may be long gone, and its row of the table with it
+    // (eight at a time, the first ones beside the group's rows)
+    constexpr int kAtOnce = 8;
+    Request m[kAtOnce];
+    bool unused = false;
+    auto load = [&](int i) {
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) m[j] = i + j < b ? own_request(p, i + j, &unused) : Request{};
+    };
+    load(a);
+    const int k = common_keys(p, a, b, n, &g0, &g1);
+    for (int i = a; k > 0 && i < b; i += kAtOnce) {
+      if (i > a) load(i);
+      int first = -1;
+#pragma unroll
+      for (int j = kAtOnce - 1; j >= 0; --j)
+        if (takes_part(m[j], k, g0, g1)) first = i + j;
+      if (first < 0) continue;
+      r.row = first;
+      r.kv = k;
       r.c0 = g0;
       r.q = g1 - g0;
+      break;
     }
     return r;
   }
@@ -419,8 +444,7 @@ __device__ __forceinline__ Request plan_of(const PagedAttnParams& p, int s, bool
   const int a = p.groups[g], b = p.groups[g + 1];
   if (a > s || b <= s) return r;
   const int k = common_keys(p, a, b, p.shared[g], &g0, &g1);
-  // all of them before its new tokens, which are among the group's (where the counts do not ascend they may not be)
-  if (k > 0 && r.kv - r.q >= k && r.c0 >= g0 && r.c0 + r.q <= g1) {
+  if (k > 0 && takes_part(r, k, g0, g1)) {
     r.lo = k;
     r.g0 = g0;
     r.g1 = g1;

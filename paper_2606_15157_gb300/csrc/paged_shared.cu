@@ -46,7 +46,7 @@ template <int D, bool kFp16>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ JoinParams j) {
   const PagedAttnParams& p = j.p;
   constexpr float kUp = kFp16 ? 7.f : 0.f;  // (of the attention's weights)
-  constexpr int kVec = D / 4, kU = 8;
+  constexpr int kVec = D / 4, kU = 4;
   pdl_wait();
   pdl_trigger();
   const int s = blockIdx.x / j.each;
@@ -82,15 +82,15 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
           float2 z[kU];
           float4 v[kU];
 #pragma unroll
-          for (int q = 0; q < kU; ++q) {
-            z[q] = make_float2(-INFINITY, 0.f);
-            v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (q0 + q < unit.y) {
-              const Records<D> rec = records<D>(p, unit.x + q0 + q, q0 + q == 0, x);
-              z[q] = __ldcg(rec.ml() + rr);
-              v[q] = __ldcg(reinterpret_cast<const float4*>(rec.at) + vec);
-            }
+          for (int q = 0; q < kU; ++q) {  // (past the last piece: the last one again, with no weight)
+            const int piece = min(q0 + q, unit.y - 1);
+            const Records<D> rec = records<D>(p, unit.x + piece, piece == 0, x);
+            z[q] = __ldcg(rec.ml() + rr);
+            v[q] = __ldcg(reinterpret_cast<const float4*>(rec.at) + vec);
           }
+#pragma unroll
+          for (int q = 0; q < kU; ++q)
+            if (q0 + q >= unit.y) z[q] = make_float2(-INFINITY, 0.f);
 #pragma unroll
           for (int q = 0; q < kU; ++q) add(z[q].x - kUp, z[q].y, v[q]);
         }

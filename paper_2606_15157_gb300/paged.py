@@ -69,8 +69,8 @@ _captured: dict = {}
 
 
 def _scratch(device: int, stream: int, need: int):
-    # what the largest call needs, and for a call with rows in parts a quarter more than those, so that it lasts
-    n = max(kvev.kvev_paged_attention_workspace(1, 1, 128), need + need // 4)
+    # what the largest call needs, and for a call with rows in parts some more than those, so that it lasts
+    n = max(kvev.kvev_paged_attention_workspace(1, 1, 128), need + min(need // 4, 1 << 26))
     with torch.cuda.device(device), torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
         t = torch.empty(n, dtype=torch.uint8, device="cuda")
         t[:kvev.PAGED_SYNC_BYTES].zero_()

@@ -136,6 +136,23 @@ def test_what_cannot_be_shared_is_left_to_the_request(paged):
     assert torch.equal(o, o2) and torch.equal(want, lse2) and c.status() == 0
 
 
+@pytest.mark.parametrize("gone", [[0], [0, 1, 2], list(range(11))])
+def test_requests_that_are_gone_keep_their_place_in_a_group(paged, gone):
+    """Finished requests have no rows, and their rows of the table name pages that are others' by now, or none."""
+    c, q, cu, kv, table, first, shared = shared_case(paged, [(256, ones(12))], 8, 2, 128, 16)
+    t2, kv2, cu2 = [list(r) for r in table], list(kv), [0]
+    for s in range(12):
+        cu2.append(cu2[-1] + (0 if s in gone else 1))
+    for s in gone:
+        kv2[s] = 0
+        t2[s][:16] = [-1] * 8 + table[11][17:18] * 8
+    c2 = paged.PagedCache(c.K, c.V, ints(t2))
+    q2 = q[[s for s in range(12) if s not in gone]]
+    o, lse = run(c2, q2, cu2, kv2, first, shared)
+    assert c2.status() == 0
+    q8_ref.check_attention(o, lse, ref.attention(c.K, c.V, table, q2, cu2, kv2), BF16, parts=2)
+
+
 def test_groups_and_lengths_out_of_range_are_flagged(paged):
     c, q, cu, kv, table, first, shared = shared_case(paged, [(512, ones(5)), (64, [(100, 50), (3, 1)])], 8, 2, 128, 16)
     r = ref.attention(c.K, c.V, table, q, cu, kv)
