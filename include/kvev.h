@@ -658,8 +658,8 @@ KVEV_API int kvev_paged_q8_gather(const kvev_paged_q8_cache *cache, const int32_
                                   int32_t *device_status, void *stream);
 
 /* kvev_paged_attention() over the values that the codes stand for; q and out in the cache's 16-bit type.
- * Chunks attend as over 16-bit pages of those values.  Requests of up to 16 query rows to a KV head (single tokens) attend
- * on the codes: query elements and softmax weights are held to 2^-9 of their own size four times over, down to 2^-32 of the row's
+ * Chunks attend as over 16-bit pages of those values.  Requests of up to 16 query rows to a KV head (single tokens), and all
+ * requests of a batch with T <= B, attend on the codes: query elements and softmax weights are held to 2^-9 of their own size four times over, down to 2^-32 of the row's
  * largest element and 2^-30 of its largest weight.  The workspace is that of kvev_paged_attention_workspace(). */
 KVEV_API int kvev_paged_q8_attention(const kvev_paged_q8_cache *cache, const void *q, int64_t q_token_stride,
                                      int64_t q_head_stride, const int32_t *cu_new, const int32_t *kv_lens,
