@@ -60,8 +60,8 @@ namespace kvev {
 namespace {
 
 // What the kernel is compiled for, beside head size and type: kShared, groups of requests whose first keys are in
-// common pages, which a unit of the group's rows reads once (paged_shared.cu); kQ8, pages of 8-bit codes, which a
-// warpgroup of its own turns into 16-bit tiles (paged_q8_attn.cu).
+// common pages, which a unit of the group's rows reads once (paged_shared.cu); kQ8, pages of 8-bit codes, which two
+// warpgroups of their own turn into 16-bit tiles (paged_q8_attn.cu).
 // kFewOnly: the requests of few rows, which the kernel of paged_q8_few.cuh takes with the codes as they are; kQ8 alone
 // leaves those out.
 enum Mode : int { kPlain = 0, kShared = 1, kQ8 = 2, kFewOnly = 4 };
@@ -897,8 +897,8 @@ __device__ __forceinline__ bool group_any(int x, bool v) {
 // exponent of one row of the next tile in flight, and turns 16 codes at a time, of 4 (2) rows.  Rows without a key of
 // the unit become zeros, whatever the pool holds there.
 // The last 4K of a 32K prompt takes 1.69 ms, 1.57 in half precision, and 1.23 from 16-bit pages: making a tile moves 64 KB
-// through shared memory beside the 96 KB that the products read of it, and issues a third as many instructions as the
-// softmax does; with four warps instead of eight the time is the same.  Measured on the way: codes loaded by the converting
+// through shared memory beside the 96 KB that the products read, and its instructions take turns with the softmax's; with
+// four warps instead of eight the time is the same.  Measured on the way: codes loaded by the converting
 // warps themselves 2.73 ms, without a branch between one row and the next 2.18; by TMA 1.80; a tile's rows together 1.69.
 
 // Loads under a condition without a branch.

