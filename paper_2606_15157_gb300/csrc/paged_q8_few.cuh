@@ -730,9 +730,12 @@ bool q8_page_maps(const kvev_paged_q8_cache* cache, CUtensorMapSwizzle swizzle, 
   return true;
 }
 
-// Rows of a unit that the launch takes: one token's where the batch has no more rows than requests, else up to 16.  (What has
-// more is left to the other kernel.)
-int few_rows_of(int G, int B, int T) { return T > B || G > 8 ? kFewRows : rows_held(G); }
+// Rows of a unit that the launch takes: those of as many tokens as the batch has to a request, up to 16, as three CTAs of up to 8
+// rows fit an SM and two of 16.  (What has more is left to the other kernel.)
+int few_rows_of(int G, int B, int T) {
+  const int tokens = (T - 1) / B + 1;
+  return G > kFewRows || tokens > kFewRows / G ? kFewRows : rows_held(G * tokens);
+}
 
 // The requests of few rows; p but for the maps of the pages.
 int few_launch(PagedAttnParams p, const kvev_paged_q8_cache* cache, int M, cudaStream_t stream) {
