@@ -33,10 +33,11 @@ extern "C" int kvev_paged_q8_attention(const kvev_paged_q8_cache* cache, const v
   const int rows = few_rows_of(p.G, B, T);
   p.few = rows / p.G;
   // With no more rows than requests the batch is taken for single tokens, and the first kernel takes whatever else there is,
-  // in units of as few rows: the second, which finds nothing to do in such a batch, costs 4 us.
-  p.all = p.few > 0 && T <= B;
+  // in units of as few rows: the second, which finds nothing to do in such a batch, costs 4 us.  Nor is there anything for the second
+  // where all rows together are few; what is out of range is then for the first to say.
+  p.all = p.few > 0 && (T <= B || T <= p.few);
   if (p.few > 0) rc = few_launch(p, cache, rows, a.stream);
-  if (rc == KVEV_OK && !p.all && T > p.few) {
+  if (rc == KVEV_OK && !p.all) {
     if (!q8_page_maps(cache, CU_TENSOR_MAP_SWIZZLE_NONE, &p)) return KVEV_ECUDA;
     rc = attn_launch<kQ8>(p, cache->d, view.fp16, a.stream);
   }

@@ -626,7 +626,7 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(M)) q8_few_kernel(const 
   }
   S& sm = *reinterpret_cast<S*>(smem_raw);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
-  if (!p.all) {  // (chunks alone leave nothing to do here; what is out of range is said by the other kernel's schedule too)
+  if (!p.all) {  // (chunks alone leave nothing to do here; what is out of range is said by the other kernel, which is launched whenever p.all is not set)
     pdl_wait();
     bool some = false;
     for (int s = threadIdx.x; s < p.B; s += kFewThreads) {

@@ -487,3 +487,22 @@ def test_attention_over_values_at_the_ends_of_the_type(paged, e, new):
         q8_ref.check_attention(o.double() * f, lse, [r[0] * f, r[1], r[2] * f, r[3]], BF16)
     else:
         assert ((o.double() - r[0]).abs() <= 2.0 ** -126 + 2.0 ** -6 * r[2]).all()
+
+
+@pytest.mark.parametrize("H_q,H", [(2, 2), (8, 2), (16, 1), (40, 2)])
+def test_attention_of_few_rows_flags_what_is_out_of_range(paged, H_q, H):
+    """Batches with no more rows than a request of few rows has: counts that decrease, are negative or past T, lengths past the table."""
+    for T, cus in ((1, ([0, 2], [0, -1], [-1, 0], [1, 0])), (3, ([0, 99], [2, 0], [0, -2 ** 31], [-7, 1], [0, 4])), (4, ([0, 5], [0, 2 ** 31 - 1], [4, 3]))):
+        c, q, cu, kv, table = attend_case(paged, [(100, T)], H_q, H, 64, 16, BF16, False)
+        good = run_attention(c, q, cu, kv)
+        assert c.status() == 0 and not (good[1] == 77).any()
+        for bad_cu, bad_kv in [(x, kv) for x in cus] + [(cu, [-1]), (cu, [10 ** 6])]:
+            out = torch.full_like(q, 3.0)
+            o, lse = run_attention(c, q, bad_cu, bad_kv, out=out)
+            assert c.status() == 2, (T, bad_cu, bad_kv)
+            assert (o == 3).all() and (lse == 77).all()
+        # beside a request in order
+        c, q, cu, kv, table = attend_case(paged, [(100, T), (60, 0)], H_q, H, 64, 16, BF16, False)
+        good = run_attention(c, q, cu, kv)
+        o, lse = run_attention(c, q, [0, T, T + 1], kv)
+        assert c.status() == 2 and torch.equal(o, good[0]) and torch.equal(lse, good[1])
