@@ -658,9 +658,14 @@ KVEV_API int kvev_paged_q8_gather(const kvev_paged_q8_cache *cache, const int32_
                                   int32_t *device_status, void *stream);
 
 /* kvev_paged_attention() over the values that the codes stand for; q and out in the cache's 16-bit type.
- * Chunks attend as over 16-bit pages of those values.  Requests of up to 16 query rows to a KV head (single tokens), and all
- * requests of a batch with T <= B, attend on the codes: query elements and softmax weights are held to 2^-9 of their own size four times over, down to 2^-32 of the row's
- * largest element and 2^-30 of its largest weight.  The workspace is that of kvev_paged_attention_workspace(). */
+ * A request of up to 16 query rows to a KV head (its new tokens times H_q / H_kv: single tokens, a few drafted ones) attends
+ * on the codes, every other request as over 16-bit pages of those values, its weights rounded to that type.  On the codes a
+ * query element is held to 2^-16 of its own size or 2^-32 of its row's largest, whichever is more, and a softmax weight
+ * to 2^-16 of its own size or 2^-30 of its row's largest.
+ * A batch with T == B is taken for single tokens: all of its requests attend on the codes.  One that has many rows there, among
+ * requests without any, gets the same answer, but its context is read once for every few of its rows (64 new tokens
+ * at 32K 320 us, 74 with T = B + 1 and a row of q and out behind the last request's, which is left as it is).
+ * The workspace is that of kvev_paged_attention_workspace(). */
 KVEV_API int kvev_paged_q8_attention(const kvev_paged_q8_cache *cache, const void *q, int64_t q_token_stride,
                                      int64_t q_head_stride, const int32_t *cu_new, const int32_t *kv_lens,
                                      const int32_t *block_table, int max_pages, int B, int T, int H_q,

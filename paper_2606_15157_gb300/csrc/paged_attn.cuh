@@ -125,8 +125,9 @@ struct PagedAttnParams {
   int2* units;  // [H_kv][T] of a group's unit, at its first token: CTA of the first piece, pieces
   float *part_o, *part_lse;
   // kQ8: queries, codes and the rows' exponents, strides in bytes
-  int few;   // most tokens of a request of few rows, and of its units;
-  bool all;  // whatever a request's rows, it is cut into such units
+  int most;   // most tokens of a request of few rows (0: none has few),
+  int few;    // and of its units
+  bool look;  // whether the kernel for few rows first looks if there are any
   const uint8_t* q;
   long long q_token, q_head;
   const uint8_t *K, *V, *K_scale, *V_scale;
@@ -457,7 +458,7 @@ template <int kMode>
 __device__ __forceinline__ Request request(const PagedAttnParams& p, int s, bool* bad) {
   if (kMode & kShared) return planned(p, s);
   Request r = own_request(p, s, bad);
-  if ((kMode & kQ8) && !p.all && (r.q <= p.few) != ((kMode & kFewOnly) != 0)) r.q = 0;
+  if ((kMode & kQ8) && (r.q <= p.most) != ((kMode & kFewOnly) != 0)) r.q = 0;
   return r;
 }
 
@@ -1870,7 +1871,7 @@ __global__ void __launch_bounds__(Split<kMode>::kThreads, 1) paged_attn_kernel(c
     for (int s = threadIdx.x; s < p.B; s += Split<kMode>::kThreads) {
       const int c0 = p.cu[s], c1 = p.cu[s + 1], kv = p.kv_lens[s];
       // (what is out of range is said by the schedule)
-      some |= c0 < 0 || c1 > p.T || c1 < c0 || c1 - c0 > p.few || kv < 0 || kv > (p.max_pages << p.page_shift);
+      some |= c0 < 0 || c1 > p.T || c1 < c0 || c1 - c0 > p.most || kv < 0 || kv > (p.max_pages << p.page_shift);
     }
     if (!__syncthreads_or(some)) return;
   }

@@ -626,12 +626,12 @@ __global__ void __launch_bounds__(kFewThreads, few_ctas(M)) q8_few_kernel(const 
   }
   S& sm = *reinterpret_cast<S*>(smem_raw);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
-  if (!p.all) {  // (chunks alone leave nothing to do here; what is out of range is said by the other kernel, which is launched whenever p.all is not set)
+  if (p.look) {  // (chunks alone leave nothing to do here; what is out of range is said by the other kernel, which is then launched too)
     pdl_wait();
     bool some = false;
     for (int s = threadIdx.x; s < p.B; s += kFewThreads) {
       const int n = p.cu[s + 1] - p.cu[s];
-      some |= n > 0 && n <= p.few;
+      some |= n > 0 && n <= p.most;
     }
     if (!__syncthreads_or(some)) return;
   }
@@ -730,8 +730,9 @@ bool q8_page_maps(const kvev_paged_q8_cache* cache, CUtensorMapSwizzle swizzle, 
   return true;
 }
 
-// Rows of a unit that the launch takes: those of as many tokens as the batch has to a request, up to 16, as three CTAs of up to 8
-// rows fit an SM and two of 16.  (What has more is left to the other kernel.)
+// Most rows of a unit: those of as many tokens as the batch has to a request, up to 16, as three CTAs of up to 8
+// rows fit an SM and two of 16.  (16 requests of two tokens at 8K 66 us, in units of 16 rows 90.  A request of few rows that has more
+// than others of its batch is cut into up to four units.)
 int few_rows_of(int G, int B, int T) {
   const int tokens = (T - 1) / B + 1;
   return G > kFewRows || tokens > kFewRows / G ? kFewRows : rows_held(G * tokens);

@@ -506,3 +506,51 @@ def test_attention_of_few_rows_flags_what_is_out_of_range(paged, H_q, H):
         good = run_attention(c, q, cu, kv)
         o, lse = run_attention(c, q, [0, T, T + 1], kv)
         assert c.status() == 2 and torch.equal(o, good[0]) and torch.equal(lse, good[1])
+
+
+@pytest.mark.parametrize("H_q,H,new,slots", [(8, 2, 30, 31), (8, 2, 5, 7), (2, 2, 17, 32), (40, 2, 3, 9)])
+def test_attention_of_a_long_request_among_idle_ones(paged, H_q, H, new, slots):
+    """A request of more than 16 query rows to a KV head attends as it does alone, also where there are no more rows than requests: the same bits
+    (up to 32 requests a warp makes the schedule, whose shares go by the rows there are)."""
+    c, q, cu, kv, table = attend_case(paged, [(1500, new)], H_q, H, 128, 16, BF16, False)
+    want = run_attention(c, q, cu, kv)
+    at = slots // 2
+    t = torch.full((slots, len(table[0])), -1, dtype=torch.int32, device="cuda")
+    t[at] = ints(table[0])
+    c2 = paged.QuantizedCache(c.K, c.V, c.K_scale, c.V_scale, t)
+    o, lse = run_attention(c2, q, [0] * (at + 1) + [new] * (slots - at), [0] * at + kv + [0] * (slots - 1 - at))
+    assert c2.status() == 0 and torch.equal(o, want[0]) and torch.equal(lse, want[1])
+
+
+@pytest.mark.parametrize("H_q,H,d", [(8, 2, 128), (2, 2, 64), (40, 2, 128)])
+@pytest.mark.parametrize("reqs", [[(300, 46)] + [(50, 0)] * 45, [(300, 30), (77, 4)] + [(50, 0)] * 32 + [(9, 1), (700, 1)], [(130, 5), (2, 0), (1, 1), (40, 0), (5, 0), (5, 0)]],
+                         ids=["one", "some", "six"])
+def test_attention_of_as_many_rows_as_requests(paged, reqs, H_q, H, d):
+    assert sum(n for _, n in reqs) == len(reqs)
+    check(paged, reqs, H_q, H, d, 16)
+
+
+@pytest.mark.parametrize("H_q,H,new", [(4, 1, 1), (4, 1, 3), (2, 2, 16), (16, 1, 1), (10, 2, 3)])
+@pytest.mark.parametrize("others", [0, 30])
+def test_attention_of_few_rows_is_on_the_codes_whatever_else_there_is(paged, H_q, H, new, others):
+    """Keys 0 and 1 have weights 1 and 2^-(2^-10) and values 1 and -1, the others weights under 2^-39: the result is 3.4e-4, and 0 where weights are
+    rounded to bf16.  32-bit logits of 20 err by 8 2^-24 20 at most, weights held in parts by 2^-16 of their own size, the result by half a step,
+    2^-9 of its own: (7e-6 + 2 x 1.6e-5) / 2 + 7e-7 < 2e-5."""
+    kv = new + 2
+    c, q, cu, kvs, table = attend_case(paged, [(kv, new)] + [(3, 1)] * others, H_q, H, 64, 16, BF16, False)
+    page = table[0][0]  # (one page: 18 keys at most)
+    p2 = table[0][1] if kv > 16 else page
+    q[:new] = 0
+    q[:new, :, 0], q[:new, :, 1] = 1.0, 2.0 ** -10
+    for p in {page, p2}:
+        c.K.view(torch.uint8)[p], c.V.view(torch.uint8)[p] = 0, 0
+        c.K_scale[p], c.V_scale[p] = 127, 127
+        c.K.view(torch.uint8)[p, :, :, 0] = 0x80 | 0x5a  # -20
+    code = lambda v: int(torch.tensor(v).to(q8_ref.E4M3).view(torch.uint8))  # noqa: E731
+    assert code(-20.0) == 0xda
+    c.K.view(torch.uint8)[page, :2, :, 0] = code(20.0)
+    c.K.view(torch.uint8)[page, 1, :, 1] = code(-1.0)
+    c.V.view(torch.uint8)[page, 0], c.V.view(torch.uint8)[page, 1] = code(1.0), code(-1.0)
+    o, lse = run_attention(c, q, cu, kvs, scale=math.log(2))
+    w = 2.0 ** -(2.0 ** -10)
+    assert c.status() == 0 and ((o[:new].double() - (1 - w) / (1 + w)).abs() <= 2e-5).all()
