@@ -20,6 +20,7 @@ import contextlib
 import ctypes as C
 import importlib.util
 import os
+import threading
 
 import torch
 
@@ -59,13 +60,15 @@ def _need(ok: bool, what: str):
 
 
 # Scratch of the attention calls made on a stream, (device, stream) -> (pointer, bytes, tensor): calls on a stream
-# follow one another, whatever layer they are for, so they share it.
+# follow one another, whatever layer they are for, so they share it.  Threads may: one's call may put a larger scratch in
+# the place of the one that another is about to hand to its launch, so a call holds the tensor until it has launched.
 _workspaces: dict = {}
 # Scratch of the calls that a capture on the stream records, (device, stream) -> (capture's id, the same).  A graph's
 # replays follow neither the stream's calls nor other graphs, so each capture has scratch of its own, from the
 # graph's memory pool, whose counts the graph itself zeroes before its first attention.  Only the last capture's is
 # kept: after a capture its memory is the graph's.
 _captured: dict = {}
+_scratches = threading.Lock()  # both of them
 
 
 def _scratch(device: int, stream: int, need: int):
@@ -79,22 +82,23 @@ def _scratch(device: int, stream: int, need: int):
 
 def _workspace(device: int, stream: int, capture: int, need: int = 0):
     """Scratch of at least `need` bytes.  A larger one takes the place of one that is too small: the calls on the
-    stream follow one another, so the old memory is the stream's to give out again."""
-    if capture:
-        held = _captured.get((device, stream))
-        if held is None or held[0] != capture or held[1][1] < need:
-            held = _captured[device, stream] = (capture, _scratch(device, stream, need))
-        return held[1]
-    ws = _workspaces.get((device, stream))
-    if ws is None or ws[1] < need:
-        ws = _workspaces[device, stream] = _scratch(device, stream, need)
-    return ws
+    stream follow one another, so the old memory is the stream's to give out again, once the calls that hold it have launched."""
+    with _scratches:
+        if capture:
+            held = _captured.get((device, stream))
+            if held is None or held[0] != capture or held[1][1] < need:
+                held = _captured[device, stream] = (capture, _scratch(device, stream, need))
+            return held[1]
+        ws = _workspaces.get((device, stream))
+        if ws is None or ws[1] < need:
+            ws = _workspaces[device, stream] = _scratch(device, stream, need)
+        return ws
 
 
 def _given(ws, device: int):
     _need(isinstance(ws, torch.Tensor) and ws.is_cuda and ws.get_device() == device and ws.is_contiguous(),
           "workspace: a contiguous tensor on the cache's GPU")
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws.data_ptr(), ws.numel() * ws.element_size(), ws
 
 
 _here = contextlib.nullcontext()
@@ -190,10 +194,10 @@ class _Cache:
         return _workspace(self._device, *self._lib.stream(self._device, None if stream is None else stream.cuda_stream))[2]
 
     def _scratch_of(self, workspace, stream, need: int = 0):
-        """(stream, the workspace's address, its bytes)"""
+        """(stream, the workspace's address, its bytes, its tensor: to be held until the launch)"""
         at, capture = self._lib.stream(self._device, None if stream is None else stream.cuda_stream)
         ws = _workspace(self._device, at, capture, need) if workspace is None else _given(workspace, self._device)
-        return at, ws[0], ws[1]
+        return at, *ws
 
     def status(self) -> int:
         """Waits for the GPU, whatever the calls' streams, then reads and clears the device status word (0: every
@@ -203,9 +207,10 @@ class _Cache:
         if v:
             self.device_status.zero_()
             if v & 1:  # a wait ran out: the pieces counted so far would be counted again (a graph zeroes its own)
-                for (device, _), ws in _workspaces.items():
-                    if device == self._device:
-                        ws[2][:kvev.PAGED_SYNC_BYTES].zero_()
+                with _scratches:
+                    for (device, _), ws in _workspaces.items():
+                        if device == self._device:
+                            ws[2][:kvev.PAGED_SYNC_BYTES].zero_()
             torch.cuda.synchronize(self._device)
         return v
 
@@ -257,7 +262,7 @@ class PagedCache(_Cache):
         if out is None:
             with _on(stream):
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        at, ws, n = self._scratch_of(workspace, stream)
+        at, ws, n, held = self._scratch_of(workspace, stream)  # noqa: F841
         rc = self._lib.attention(*self._call, at, q, cu, kv_lens, out, lse, scale, window, ws, n)
         if rc:
             raise kvev.KvevError(rc, "kvev_paged_attention")
@@ -275,7 +280,7 @@ class PagedCache(_Cache):
         if workspace is None:
             _need(isinstance(q, torch.Tensor) and q.dim() == 3 and q.shape[0] <= 1 << 30, "q: [tokens][heads][d]")
             need = kvev.kvev_paged_attention_shared_workspace(q.shape[1], self.H_kv, self.d, q.shape[0])
-        at, ws, n = self._scratch_of(workspace, stream, need)
+        at, ws, n, held = self._scratch_of(workspace, stream, need)  # noqa: F841
         rc = _bind_q8().attention_shared(*self._call, at, q, cu, kv_lens, groups, shared_lens, out, lse, scale, ws, n)
         if rc:
             raise kvev.KvevError(rc, "kvev_paged_attention_shared")
@@ -339,7 +344,7 @@ class QuantizedCache(_Cache):
         if out is None:
             with _on(stream):
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        at, ws, n = self._scratch_of(workspace, stream)
+        at, ws, n, held = self._scratch_of(workspace, stream)  # noqa: F841
         rc = self._q8.attention(*self._call, at, q, cu, kv_lens, out, lse, scale, window, ws, n)
         if rc:
             raise kvev.KvevError(rc, "kvev_paged_q8_attention")

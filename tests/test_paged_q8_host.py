@@ -149,3 +149,44 @@ def test_overlapped_kernels_load_nothing_as_constant(name):
     with open(os.path.join(build.CSRC, name)) as f:
         code = re.sub(r"//[^\n]*", "", f.read())
     assert not re.search(r"__ldg\s*\(|\.global[.\w]*\.nc\b|__restrict__", code)
+
+
+@pytest.mark.parametrize("call", ["attention", "shared", "q8"])
+@pytest.mark.parametrize("capture", [0, 7])
+def test_scratch_outlives_the_launch_that_it_was_looked_up_for(q8, call, capture, monkeypatch):
+    """Between one thread's look-up and its launch another's call on the stream may put a larger scratch in its place."""
+    import gc
+    import weakref
+
+    from paper_2606_15157_gb300 import paged
+    c, q, fake = q8
+    c.fake.capture = capture
+    x = torch.zeros((3, 1, 64), dtype=torch.bfloat16)
+    calls = {"attention": lambda: c.attention(x, None, None, out=x), "q8": lambda: q.attention(x, None, None, out=x),
+             "shared": lambda: c.attention_shared(x, None, None, None, None, out=x)}
+    calls[call]()  # (the stream's scratch)
+    tensors = [weakref.ref(t) for _, t in c.streams if t.dtype is torch.uint8]
+    del c.streams[:]
+    alive, inside = [], []
+
+    def launched(*a):
+        if not inside:
+            inside.append(a[-2])
+            shared(c, 100000, fake)  # the other thread's
+            del c.streams[:]
+            gc.collect()
+            alive.extend(t().data_ptr() for t in tensors if t() is not None)
+        return fake_calls(*a)
+
+    def fake_calls(*a):
+        fake.calls.append(a)
+        return 0
+
+    for f in (c.fake, fake):
+        for name in ("attention", "attention_shared"):
+            monkeypatch.setattr(f, name, launched, raising=False)
+    calls[call]()
+    assert inside and inside[0] in alive  # what the launch was given was still there
+    gc.collect()
+    assert all(t() is None for t in tensors)  # and is the allocator's afterwards
+    assert len(paged._workspaces) + len(paged._captured) == 1
