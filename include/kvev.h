@@ -518,8 +518,12 @@ KVEV_API int kvev_paged_tables(const int32_t *lens, const int32_t *new_lens, int
  * lens_out[s] = done[s] ? 0 : lens[s] (may be lens itself), *free_count_out = the
  * stack's new height (may be free_count).  block_table is only read.  Entries
  * outside the pool, and those that would not fit on a stack of num_pages, are left
- * out with status bit 2.
+ * out with status bit 2.  Entries of KVEV_PAGED_KEPT_PAGE are left out without it:
+ * pages that other requests hold too (a shared prefix) go back once, so before the
+ * call the rows of all holders that are done but the last one are to have it in their
+ * place; a page that comes back twice would be given out twice.
  * Errors as kvev_paged_tables. */
+#define KVEV_PAGED_KEPT_PAGE (-2)
 KVEV_API int kvev_paged_release(const int32_t *lens, const int32_t *done, int B, int page_size,
                                 int num_pages, const int32_t *block_table, int max_pages,
                                 int32_t *free_pages, const int32_t *free_count, int32_t *lens_out,
@@ -605,8 +609,8 @@ KVEV_API int kvev_paged_attention(const kvev_paged_cache *cache, const void *q, 
  *               those of a group of one request.
  *   N           0 .. KVEV_PAGED_MAX_REQUESTS - B.
  * Pages of the common tokens are taken from the block-table row of the group's first request that shares them.
- * (kvev_paged_release() gives back every page of a request: the entries of shared pages are to be -1 in
- * the rows of all requests but the last one released, which leaves them out, with status bit 2.)
+ * (kvev_paged_release() gives back every page of a request: the entries of shared pages are to be KVEV_PAGED_KEPT_PAGE in
+ * the rows of all requests but the last one released.)
  * A row's two parts are held as fp32 in the workspace and put together by their
  * log-sum-exp.  A shared length that is negative or more than max_pages * page_size
  * counts as 0, and groups that do not ascend as none, both with status bit 2; the rest, errors among it,

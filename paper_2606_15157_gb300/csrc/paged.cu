@@ -210,8 +210,9 @@ __global__ void __launch_bounds__(kTableThreads) release_kernel(const __grid_con
     __syncthreads();
   }
   const int room = p.num_pages - count;
-  bad |= carry > room;
-  const int total = static_cast<int>(min(carry, static_cast<long long>(room)));
+  const int all = static_cast<int>(min(carry, static_cast<long long>(INT_MAX)));
+  const bool cut = carry > all;
+  const int total = min(all, room);
   const int t0 = blockIdx.x * blockDim.x + tid, step = cluster_size() * blockDim.x;
   auto entry = [&](int k) {  // the k-th entry that comes back
     const int s = find_request(first, p.B, k);
@@ -220,14 +221,18 @@ __global__ void __launch_bounds__(kTableThreads) release_kernel(const __grid_con
   auto outside = [&](int page) { return static_cast<unsigned>(page) >= static_cast<unsigned>(p.num_pages); };
   // Entries outside the pool must not reach the stack: every entry is looked at before the first is put there, and
   // each CTA is told whether there was one, by the barrier after which outputs may be written.  A thread keeps its
-  // first four, in flight together.
+  // first four, in flight together.  Those for pages that others keep are outside too, and in order.
   int page[4];
   bool odd = false;
+  auto look = [&](int page) {
+    odd |= outside(page);
+    bad |= outside(page) && page != KVEV_PAGED_KEPT_PAGE;
+  };
 #pragma unroll
-  for (int q = 0; q < 4; ++q) page[q] = t0 + q * step < total ? entry(t0 + q * step) : 0;
+  for (int q = 0; q < 4; ++q) page[q] = t0 + q * step < all ? entry(t0 + q * step) : 0;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) odd |= outside(page[q]);
-  for (int k = t0 + 4 * step; k < total; k += step) odd |= outside(entry(k));
+  for (int q = 0; q < 4; ++q) look(page[q]);
+  for (long long k = t0 + 4 * step; k < all; k += step) look(entry(static_cast<int>(k)));
   __syncwarp();
   cluster_wait();
   if (odd) cluster_raise(&any_odd);
@@ -235,15 +240,15 @@ __global__ void __launch_bounds__(kTableThreads) release_kernel(const __grid_con
   cluster_sync();
   for (int s = t0; s < p.B; s += step) p.lens_out[s] = len[s];
   if (any_odd == 0) {
+    bad |= carry > room;
     if (t0 == 0) *p.count_out = count + total;
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       if (t0 + q * step < total) p.free_pages[count + t0 + q * step] = page[q];
     for (int k = t0 + 4 * step; k < total; k += step) p.free_pages[count + k] = entry(k);
   } else if (blockIdx.x == 0) {  // one CTA puts the others there, in order
-    const int all = static_cast<int>(min(carry, static_cast<long long>(INT_MAX)));
     long long kept = 0;
-    for (long long k0 = 0; k0 < all && kept < room; k0 += blockDim.x) {
+    for (long long k0 = 0; k0 < all; k0 += blockDim.x) {
       const int x = k0 + tid < all ? entry(static_cast<int>(k0 + tid)) : -1;
       const long long upto = kept + block_scan(outside(x) ? 0 : 1, 0, ws).x;
       if (!outside(x) && upto <= room) p.free_pages[count + upto - 1] = x;
@@ -252,9 +257,10 @@ __global__ void __launch_bounds__(kTableThreads) release_kernel(const __grid_con
       __syncthreads();
       kept = carry;
     }
+    bad |= kept > room || cut;
     if (tid == 0) *p.count_out = count + static_cast<int>(min(kept, static_cast<long long>(room)));
   }
-  if (bad || odd) atomicOr(p.status, kStatusDevice);
+  if (bad) atomicOr(p.status, kStatusDevice);
 }
 
 // ---------------------------------------------------------------------------

@@ -23,6 +23,7 @@ POOL_MAX, POOL_AVG = 0, 1
 T_IDENTITY, T_CAP_Q95 = 0, 1
 BF16, FP16 = 0, 1
 PAGED_SYNC_BYTES, PAGED_MAX_REQUESTS = 4096, 8192
+PAGED_KEPT_PAGE = -2  # block-table entry of a page that other requests keep at a release
 SCOPE_PREFILL, SCOPE_DECODE, SCOPE_BOTH = 1, 2, 3
 
 STATUS_NAMES = {OK: "OK", EINVAL: "EINVAL", ENOMEM: "ENOMEM", ECUDA: "ECUDA",

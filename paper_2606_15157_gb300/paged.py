@@ -172,7 +172,11 @@ class PagePool:
 
     def release(self, lens, done, *, lens_out=None, free_count=None, free_count_out=None, stream=None):
         """The pages of requests with done != 0 go back; returns the lengths, 0 for those (by default
-        ``lens`` itself and the pool's count are updated in place)."""
+        ``lens`` itself and the pool's count are updated in place).
+
+        All pages of a request go back.  Where requests share pages, write ``kvev.PAGED_KEPT_PAGE`` over them in the block-table
+        rows of those that are done while others hold them, and of all but one of those done at once: a page
+        that comes back twice is given out twice."""
         if lens_out is None:
             lens_out = lens
         if free_count is None:
@@ -272,7 +276,8 @@ class PagedCache(_Cache):
         """``attention`` without a window for groups of requests that begin with the same tokens: group g is the
         requests groups[g] .. groups[g + 1] - 1 (int32 [N + 1], ascending), whose block-table rows name the same
         pages for their first shared_lens[g] tokens (int32 [N]).  Their whole pages are read once for the
-        group.  A ``workspace`` of its own has ``kvev.kvev_paged_attention_shared_workspace`` bytes."""
+        group.  A ``workspace`` of its own has ``kvev.kvev_paged_attention_shared_workspace`` bytes.  (What to do with
+        shared pages when requests are done: ``PagePool.release``.)"""
         if out is None:
             with _on(stream):
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device)

@@ -309,3 +309,68 @@ def test_forks_of_a_prefilled_prefix(paged):
     pool.release(lens, done)
     assert int(pool.free_count) == 200 and taken + 0 > n // page and int(pool.device_status) == 2
     assert sorted(pool.free.cpu().tolist()) == list(range(200))
+
+
+@pytest.mark.parametrize("B,page,ctx,room", [(2, 16, 40, 0), (40, 8, 1500, 0), (700, 8, 1500, 0), (300, 8, 900, 0), (300, 8, 900, 50)])
+def test_release_of_requests_that_share_pages(paged, B, page, ctx, room):
+    """Entries of pages that others keep are left out and in order, on a stack with room for the others alone; where it has `room` pages less, or
+    beside an entry outside the pool, the status says so."""
+    rng = random.Random(B)
+    lens = [ctx] + [rng.randint(0, ctx) for _ in range(B - 1)]
+    done = [1] + [rng.choice([0, 1, 1]) for _ in range(B - 1)]
+    held = [ref.pages_of(n, page) for n in lens]
+    common = min(held[0], 70)
+    ids = list(range(sum(held)))
+    rng.shuffle(ids)
+    table = [[ids.pop() for _ in range(h)] for h in held]
+    for s in range(1, B):
+        if done[s]:
+            for j in range(min(common, held[s])):
+                table[s][j] = kvev.PAGED_KEPT_PAGE
+    back = [x for s in range(B) if done[s] for x in table[s] if x >= 0]
+    num_pages = sum(held)
+    rows = ints([r + [-1] * (max(held) + 1 - len(r)) for r in table])
+    count = num_pages - len(back) + room
+    free = [num_pages - 1] * count + [-7] * (num_pages - count)
+    for wrong in (False, True):
+        if wrong:
+            rows[0, 0] = -1
+            back = back[1:]
+        pool = paged.PagePool(num_pages, page, rows, ints(free), ints([count]))
+        dlens = ints(lens)
+        pool.release(dlens, ints(done))
+        want = (free[:count] + back)[:num_pages]
+        assert int(pool.free_count) == len(want) and pool.free.cpu().tolist()[:len(want)] == want
+        assert dlens.cpu().tolist() == [0 if f else n for n, f in zip(lens, done)]
+        assert int(pool.device_status) == (2 if wrong or room else 0)
+
+
+def test_kept_pages_are_in_order_for_a_release_alone(paged):
+    c, q, cu, kv, table, first, shared = shared_case(paged, [(32, [(20, 1), (5, 1)])], 4, 2, 64, 16)
+    rows = [list(r) for r in table]
+    rows[1][0] = kvev.PAGED_KEPT_PAGE  # of a request that still attends: no page
+    c2 = paged.PagedCache(c.K, c.V, ints(rows))
+    c2.attention(q, ints(cu), ints(kv))
+    assert c2.status() == 2
+
+
+def test_requests_of_a_group_are_done_one_after_another(paged):
+    """The last holder gives the prefix back; every page is on the stack once, and nothing is said."""
+    page, n, own, B = 16, 3, 2, 4
+    num_pages = n + own * B
+    table = torch.full((B, n + own), -1, dtype=torch.int32, device="cuda")
+    pool = paged.PagePool(num_pages, page, table)
+    lens = torch.zeros(B, dtype=torch.int32, device="cuda")
+    pool.tables(lens, ints([n * page] + [0] * (B - 1)), n * page, kv_lens=lens)
+    table[1:, :n] = table[0, :n]
+    lens[1:] = n * page
+    pool.tables(lens, ints([own * page] * B), B * own * page, kv_lens=lens)
+    assert int(pool.free_count) == 0
+    for done in ([0, 1, 0, 0], [1, 0, 0, 1], [0, 0, 1, 0]):
+        left = [s for s in range(B) if int(lens[s]) and not done[s]]
+        for s in range(B):
+            if done[s] and left:
+                table[s, :n] = kvev.PAGED_KEPT_PAGE
+        pool.release(lens, ints(done))
+        assert int(pool.free_count) == num_pages - len(left) * own - (n if left else 0) and int(pool.device_status) == 0
+    assert sorted(pool.free.cpu().tolist()) == list(range(num_pages))
