@@ -554,3 +554,11 @@ def test_attention_of_few_rows_is_on_the_codes_whatever_else_there_is(paged, H_q
     o, lse = run_attention(c, q, cu, kvs, scale=math.log(2))
     w = 2.0 ** -(2.0 ** -10)
     assert c.status() == 0 and ((o[:new].double() - (1 - w) / (1 + w)).abs() <= 2e-5).all()
+
+
+@pytest.mark.parametrize("H", [3, 5, 7, 10, 16, 32])
+@pytest.mark.parametrize("G,d,heads_first", [(1, 64, False), (4, 128, True), (12, 64, False)])
+def test_attention_of_any_number_of_kv_heads(paged, H, G, d, heads_first):
+    """Numbers of KV heads that do not divide the CTAs (456, or 304 for 16 rows) among them: shares that end inside a head."""
+    check(paged, [(n, 1) for n in (1, 129, 1000, 3000, 0, 257)], G * H, H, d, 16, BF16, heads_first)
+    check(paged, [(700, 2), (130, 3), (1, 1), (900, 40), (40, 0)], G * H, H, d, 32, FP16, heads_first)
