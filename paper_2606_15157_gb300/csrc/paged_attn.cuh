@@ -545,7 +545,8 @@ struct Share {
 // The CTA's share of `outer` rounds of cost `round`; before: the cost of the rounds before its own.  kFewOnly and kShared,
 // where the CTAs divide by the rounds: each round its own CTAs, so that all rounds, the KV heads, are at the same place at the same time.
 // (Codes of a token's heads are 64 or 128 bytes next to one another in tokens-first pages: 64 generations over 4,097 tokens, 64-element
-// heads, with shares that do not end with the heads 111 us, 65 so.)
+// heads, with shares that do not end with the heads 111 us, 65 so.  KV heads that do not divide the CTAs are taken one after
+// another instead: 32 generations at 4K, 128-element heads, 4 to a KV head, 32 and 53 us with 4 and 8 KV heads, 39, 62, 65, 133 and 254 with 5, 7, 10, 16 and 32.)
 template <int kMode>
 __device__ __forceinline__ Share share_at(long long round, int outer, int least) {
   Share r = {};

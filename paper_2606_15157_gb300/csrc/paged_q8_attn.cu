@@ -1,6 +1,7 @@
 // paged_q8_attn.cu -- attention over paged caches of 8-bit codes: a kernel for the requests of few rows, which is bound
 // by the cache's bytes (paged_q8_few.cuh), and one for the others, bound by the products (paged_attn.cuh).  Which
-// request is which only the device knows; the host leaves a kernel out where the number of rows says that it has none.
+// request is which only the device knows; the host leaves the second out where the numbers of rows and requests say, or suggest, that
+// it has none.
 #include "paged_q8_few.cuh"
 
 using namespace kvev;

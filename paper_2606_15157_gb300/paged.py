@@ -276,8 +276,10 @@ class PagedCache(_Cache):
         """``attention`` without a window for groups of requests that begin with the same tokens: group g is the
         requests groups[g] .. groups[g + 1] - 1 (int32 [N + 1], ascending), whose block-table rows name the same
         pages for their first shared_lens[g] tokens (int32 [N]).  Their whole pages are read once for the
-        group.  A ``workspace`` of its own has ``kvev.kvev_paged_attention_shared_workspace`` bytes.  (What to do with
-        shared pages when requests are done: ``PagePool.release``.)"""
+        group.  Worth it for single tokens from about 16 requests behind 2,048 common tokens or 8 behind 4,096 on;
+        ``attention`` on the same batch is faster for small groups and for chunks.  A ``workspace`` of its own has
+        ``kvev.kvev_paged_attention_shared_workspace`` bytes.  (What to do with shared pages when requests are done:
+        ``PagePool.release``.)"""
         if out is None:
             with _on(stream):
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
@@ -345,7 +347,8 @@ class QuantizedCache(_Cache):
             raise kvev.KvevError(rc, "kvev_paged_q8_write")
 
     def attention(self, q, cu, kv_lens, *, scale=0.0, window=0, out=None, lse=None, workspace=None, stream=None):
-        """``PagedCache.attention`` over the values that the codes stand for."""
+        """``PagedCache.attention`` over the values that the codes stand for.  As many rows as requests (q.shape[0] ==
+        kv_lens.numel()) are taken for single tokens: a chunk among idle requests is slow there, so give q a row more."""
         if out is None:
             with _on(stream):
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
