@@ -671,8 +671,8 @@ KVEV_API int kvev_paged_q8_gather(const kvev_paged_q8_cache *cache, const int32_
  * on the codes, every other request as over 16-bit pages of those values, its weights rounded to that type.  On the codes a
  * query element is held to 2^-16 of its own size or 2^-32 of its row's largest, whichever is more, and a softmax weight
  * to 2^-16 of its own size or 2^-30 of its row's largest.
- * A batch with T == B is taken for single tokens: all of its requests attend on the codes.  One that has many rows there, among
- * requests without any, gets the same answer, but its context is read once for every few of its rows (64 new tokens
+ * A batch with T == B (and H_q / H_kv up to 16) is taken for single tokens: all of its requests attend on the codes.  One that has many
+ * rows there, among requests without any, is answered so too, but its context is read once for every few of its rows (64 new tokens
  * at 32K 320 us, 74 with T = B + 1 and a row of q and out behind the last request's, which is left as it is).  Single
  * tokens among requests without any spare a launch, 5 us, with as many rows behind as make T = B.
  * Many new tokens over codes take longer than kvev_paged_q8_gather() into contiguous pages and kvev_paged_attention()
